@@ -701,6 +701,158 @@ fairy2i_status fairy2i_cpu_lut_wl_matmul(const uint8_t* codes_U, const float* sc
                                          void* workspace, size_t workspace_bytes, int32_t n_threads);
 
 /*
+ * Serving operators around the layers: several sequences of any lengths at
+ * once, between one widely-linear product and the next.
+ *
+ * fairy2i_add_rmsnorm_i8: the residual addition, RMSNorm and the int8
+ * activations of the product that follows, in one pass over a token:
+ *   h = x + delta (x alone where delta is NULL),
+ *   z = h * gain / sqrt(mean over the 2n reals of h^2 + eps),
+ *   g = max |z|,  q = clamp(rint(z * (127 / g)), -127, 127) (half to even),
+ *   x_scale = g / 127;  g < 2^-121 (zeros among it) gives q = 0, x_scale = 0.
+ * x, delta: complex64 [B][n].  gain: float32 [2n], the real parts' gains,
+ * then the imaginary parts' (as norm_attn of fairy2i_block_desc).  h:
+ * complex64 [B][n] output, or NULL (not stored); it may be x or delta.
+ * q: int8 [B][n][2] and x_scale: float32 [B], as fairy2i_wl_matmul takes
+ * them.  The squares are summed in double, the rest is float32.  A token
+ * with a value that is not finite (or whose h * gain is not) gets q = 0 and
+ * a NaN x_scale.
+ * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for B < 1 or above 2^31 - 1,
+ * n < 1 or above 2^24, eps not positive and finite.
+ */
+fairy2i_status fairy2i_add_rmsnorm_i8(const float* x, const float* delta, const float* gain, float eps, int64_t B,
+                                      int64_t n, float* h, int8_t* q, float* x_scale, void* stream);
+
+/*
+ * Paged cache of keys and values in microscaled 4-bit floating point.
+ *
+ * A head has dc complex entries, dc a multiple of 16 up to 128.  Sixteen
+ * neighbouring entries of a position's key (or value) are a block of 32 reals
+ * with one power of two 2^e: each real is held as the e2m1 value (0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives) nearest to real / 2^e, ties to the
+ * even code, magnitudes above 6 as 6.  e is the smallest with
+ * max |real| <= 7 * 2^e, within [-125, 125], so what saturates is off by at
+ * most 2^e, as what is rounded is.  A position's head whose key or value
+ * holds a real that is not finite is stored with a NaN key (scale byte 255;
+ * value blocks that are not finite as zeros): every query that attends to it
+ * gets NaN, no other does.
+ *
+ * data: fairy2i_kv_cache_bytes bytes of device memory, 16-byte aligned, laid
+ * out as [n_pages][n_kv_heads][page_size / 32] tiles of 32 positions.  What
+ * it holds at first does not matter.  With nb = dc / 16, U = 4 for even nb
+ * and 2 for odd, and sb = nb for nb <= 2, else nb rounded up to a multiple
+ * of 4, a tile is 1024 nb + 64 sb bytes:
+ *   keys    [2 nb / U][g 4][r 16][U / 2][s 2][k 4]: the byte of block
+ *           b = ([2 nb / U], [U / 2]), entry 16 b + 4 g + k of position 16 s + r;
+ *   values  the same axes: entry 16 b + r of position 16 s + 4 g + k;
+ *   scales  of keys [position 32][sb], of values [g 4][s 2][k 4][sb]
+ *           (position 16 s + 4 g + k): e + 127.
+ * A code byte holds an entry's real part in its low nibble and the imaginary
+ * part in its high one; a nibble is sign, two exponent bits, one mantissa bit.
+ * These are the matrix cores' operands: a lane loads its own codes 16 (8 for
+ * odd nb) bytes at a time.
+ *
+ * fairy2i_kv_batch names the sequences of a call, all device memory:
+ *   cu_new  int32 [n_seqs + 1]: sequence i's rows of q, k, v and out are
+ *           cu_new[i] .. cu_new[i + 1] - 1; from 0 to n_new, never decreasing
+ *           (a sequence without rows is left alone);
+ *   lens    int32 [n_seqs]: positions of the sequence, its rows included: row
+ *           j stands at position lens - rows + j;
+ *   pages   int32 [n_seqs][max_pages]: the page of positions
+ *           page_size * m .. page_size * (m + 1) - 1 is pages[i][m].
+ * The arrays are read by the kernels, nothing is copied to the host, so a
+ * captured graph follows what they hold.  They are bounded before use: rows
+ * outside [0, n_new), positions past max_pages * page_size and page numbers
+ * outside [0, n_pages) are neither read nor written.
+ */
+typedef struct fairy2i_kv_cache {
+  uint8_t* data;
+  int64_t n_pages;
+  int32_t page_size;   /* positions of a page: a multiple of 32 */
+  int32_t n_kv_heads;
+  int32_t dc;          /* complex entries of a head */
+  int32_t reserved;    /* 0 */
+} fairy2i_kv_cache;
+
+typedef struct fairy2i_kv_batch {
+  const int32_t* pages;
+  const int32_t* cu_new;
+  const int32_t* lens;
+  int64_t n_new;       /* rows in all */
+  int32_t n_seqs;
+  int32_t max_pages;
+} fairy2i_kv_batch;
+
+/* Bytes of a cache; 0 for sizes that are not supported (n_pages < 1,
+ * page_size not a multiple of 32 in [32, 2^20], n_kv_heads outside [1, 65535],
+ * dc not a multiple of 16 in [16, 128]). */
+size_t fairy2i_kv_cache_bytes(int64_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t dc);
+
+/*
+ * out: float32 [n_pos][dc][2] = (cos, sin) of p * base^(-j / dc) for position
+ * p and entry j of a head (theta_j = base^(-2 j / dh), dh = 2 dc), computed in
+ * double and rounded once.
+ * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for n_pos outside [1, 2^30], dc
+ * outside [1, 4096], a base that is not positive and finite.
+ */
+fairy2i_status fairy2i_rope_table(int64_t n_pos, int32_t dc, double base, float* out, void* stream);
+
+/*
+ * Rotates q and k by their positions' entries of `rope` (a complex product,
+ * each product and sum rounded once in float32), writes q rounded to bf16 and
+ * appends k and v to the cache.
+ * k, v: complex64 rows of n_kv_heads * dc entries, k_ld and v_ld entries
+ * apart; q: rows of n_heads * dc entries, q_ld apart (so all three may be
+ * columns of one product).  q_out: bf16 pairs [n_new][n_heads][dc][2].  q and
+ * q_out may both be NULL.  rope: float32 [rope_len][dc][2]
+ * (fairy2i_rope_table).  A row at a position past rope_len is not stored, its
+ * q_out is NaN.  Each position is to be written by one row of a call.
+ * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for a cache of unsupported
+ * sizes, n_seqs outside [1, 2^20], n_new outside [1, 2^26], max_pages < 1,
+ * max_pages * page_size above 2^30, n_heads, rope_len < 1 or an ld below its
+ * row; FAIRY2I_ERR_UNSUPPORTED for a misaligned cache or more work than a
+ * launch takes.
+ */
+fairy2i_status fairy2i_kv_append(const fairy2i_kv_cache* cache, const fairy2i_kv_batch* batch, const float* q,
+                                 int64_t q_ld, int32_t n_heads, const float* k, int64_t k_ld, const float* v,
+                                 int64_t v_ld, const float* rope, int64_t rope_len, void* q_out, void* stream);
+
+/*
+ * The values that the cache stands for at the positions of a batch's rows
+ * (with cu_new over whole sequences: all of them).  k_out, v_out: bf16 pairs
+ * [n_new][n_kv_heads][dc][2], exact.  Positions without a page read as NaN.
+ * Errors: as fairy2i_kv_append.
+ */
+fairy2i_status fairy2i_kv_read(const fairy2i_kv_cache* cache, const fairy2i_kv_batch* batch, void* k_out, void* v_out,
+                               void* stream);
+
+/*
+ * Hermitian-score attention (Sec. 3.1, Eq. hermitian-score) of a batch's rows
+ * over the cache, causal: row j of a sequence sees positions 0 .. lens - rows
+ * + j.  With query head h reading key head h / (n_heads / n_kv_heads):
+ *   s_m = scale * Re(q^H k_m),  p = softmax(s),  out = sum_m p_m v_m.
+ * q: bf16 pairs [n_new][n_heads][dc][2], rotated (fairy2i_kv_append's q_out);
+ * out: the same shape, rounded to bf16 once; it may be q's memory only where
+ * they are the same array.  A row that sees nothing (a length of zero, or
+ * only positions without a page) is zero.  The rows' own keys and values have
+ * to be in the cache.
+ * Scores, maximum, sum and the weighted sums are float32; the weights enter
+ * the matrix cores as bf16 (as two bf16 parts where few rows share a pass).
+ * The result of a call does not depend on the order in which its blocks run.
+ * workspace: fairy2i_kv_attend_workspace_bytes(cache, n_new, n_seqs, n_heads)
+ * bytes, 16-byte aligned, contents ignored (cache->data is not looked at; 0
+ * for sizes that are not supported).
+ * Errors: as fairy2i_kv_append; FAIRY2I_ERR_SHAPE for n_heads that is not a
+ * multiple of n_kv_heads or a scale outside (0, 1e30];
+ * FAIRY2I_ERR_WORKSPACE.
+ */
+size_t fairy2i_kv_attend_workspace_bytes(const fairy2i_kv_cache* cache, int64_t n_new, int64_t n_seqs,
+                                         int32_t n_heads);
+fairy2i_status fairy2i_kv_attend(const fairy2i_kv_cache* cache, const fairy2i_kv_batch* batch, const void* q,
+                                 int32_t n_heads, float scale, void* out, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/*
  * Matrix-core rate probe, for the roofline figures (not part of the method):
  * the sustained rate of the prefill GEMM's instruction (kind
  * FAIRY2I_PROBE_MFMA_I8: v_mfma_i32_16x16x64_i8, 32768 operations), of the

@@ -14,3 +14,4 @@ from .fairy2i import (CODEWORDS, axis_scales, code_planes, combine_accumulators,
 from . import block  # noqa: F401,E402
 from . import groups  # noqa: F401,E402
 from . import qat  # noqa: F401,E402
+from . import serving  # noqa: F401,E402

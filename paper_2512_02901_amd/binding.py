@@ -70,6 +70,14 @@ _SIGNATURES = {
                                         _c_i64, _c_p, _c_size, _c_p, _c_p]),
     "fairy2i_gemm_bf16": (_c_i32, [_c_p, _c_i64, _c_i32, _c_p, _c_i64, _c_i32, _c_i64, _c_i64, _c_i64, _c_p, _c_i64,
                                    _c_p, _c_size, _c_p]),
+    "fairy2i_add_rmsnorm_i8": (_c_i32, [_c_p, _c_p, _c_p, ctypes.c_float, _c_i64, _c_i64, _c_p, _c_p, _c_p, _c_p]),
+    "fairy2i_kv_cache_bytes": (_c_size, [_c_i64, _c_i32, _c_i32, _c_i32]),
+    "fairy2i_rope_table": (_c_i32, [_c_i64, _c_i32, ctypes.c_double, _c_p, _c_p]),
+    "fairy2i_kv_append": (_c_i32, [_c_p, _c_p, _c_p, _c_i64, _c_i32, _c_p, _c_i64, _c_p, _c_i64, _c_p, _c_i64, _c_p,
+                                   _c_p]),
+    "fairy2i_kv_read": (_c_i32, [_c_p, _c_p, _c_p, _c_p, _c_p]),
+    "fairy2i_kv_attend_workspace_bytes": (_c_size, [_c_p, _c_i64, _c_i64, _c_i32]),
+    "fairy2i_kv_attend": (_c_i32, [_c_p, _c_p, _c_p, _c_i32, ctypes.c_float, _c_p, _c_p, _c_size, _c_p]),
     "fairy2i_cpu_lut_workspace_bytes": (_c_size, [_c_i32, _c_i64, _c_i64, _c_i32]),
     "fairy2i_cpu_lut_wl_matmul": (_c_i32, [_c_p, _c_p, _c_p, _c_p, _c_i32, _c_i64, _c_i64, _c_p, _c_p, _c_i64,
                                            _c_p, _c_p, _c_p, _c_size, _c_i32]),
@@ -95,6 +103,18 @@ class BlockDesc(ctypes.Structure):
                 ("eps", ctypes.c_float), ("reserved", _c_i32), ("rope_base", ctypes.c_double),
                 ("codes_U", _c_p * 7), ("scales_U", _c_p * 7), ("codes_W", _c_p * 7), ("scales_W", _c_p * 7),
                 ("norm_attn", _c_p), ("norm_mlp", _c_p)]
+
+
+class KvCacheDesc(ctypes.Structure):
+    """fairy2i_kv_cache of include/fairy2i.h."""
+    _fields_ = [("data", _c_p), ("n_pages", _c_i64), ("page_size", _c_i32), ("n_kv_heads", _c_i32), ("dc", _c_i32),
+                ("reserved", _c_i32)]
+
+
+class KvBatchDesc(ctypes.Structure):
+    """fairy2i_kv_batch of include/fairy2i.h."""
+    _fields_ = [("pages", _c_p), ("cu_new", _c_p), ("lens", _c_p), ("n_new", _c_i64), ("n_seqs", _c_i32),
+                ("max_pages", _c_i32)]
 
 
 class Fairy2iError(RuntimeError):
@@ -901,4 +921,237 @@ class WlBlock:
                 raise ValueError(f"out must hold {self.n} complex entries")
         _check(lib.fairy2i_block_decode(ctypes.byref(self._plan), _ptr(self.plan_device), _ptr(x), _ptr(k_cache),
                                         _ptr(v_cache), int(pos), _ptr(out), _stream_ptr(x)), "fairy2i_block_decode")
+        return out
+
+
+# -------------------------------------------------------------- serving ---
+
+def add_rmsnorm_i8(x, gain, delta=None, eps=1e-5, h_out=None, out=None):
+    """h = x + delta and RMSNorm(h) as int8 activations in one pass
+    (fairy2i_add_rmsnorm_i8).
+
+    x, delta: complex64 [B, n] (delta may be None: h is x); gain: float32
+    [2n], the real parts' gains, then the imaginary parts'.  Returns (h,
+    q int8 [B, n, 2], x_scale float32 [B]); (q, x_scale) is what wl_matmul
+    takes.  h_out: where h goes (x and delta themselves are allowed; by
+    default a new tensor, and x as it is where there is no delta); out: a pair
+    (q, x_scale) to write."""
+    torch = _torch_module or _torch()
+    lib = _lib or load()
+    _require(x, torch.complex64, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [B, n]")
+    B, n = x.shape
+    dev = x.device
+    _require(gain, torch.float32, "gain", dev)
+    if gain.shape != (2 * n,):
+        raise ValueError(f"gain must have shape ({2 * n},), got {tuple(gain.shape)}")
+    if delta is not None:
+        _require(delta, torch.complex64, "delta", dev)
+        if delta.shape != x.shape:
+            raise ValueError("delta must have x's shape")
+        if h_out is None:
+            h_out = torch.empty_like(x)
+    if h_out is not None:
+        _require(h_out, torch.complex64, "h_out", dev)
+        if h_out.shape != x.shape:
+            raise ValueError("h_out must have x's shape")
+    if out is None:
+        q = torch.empty((B, n, 2), dtype=torch.int8, device=dev)
+        scale = torch.empty((B,), dtype=torch.float32, device=dev)
+    else:
+        q, scale = out
+        _require(q, torch.int8, "out[0]", dev)
+        _require(scale, torch.float32, "out[1]", dev)
+        if q.shape != (B, n, 2) or scale.shape != (B,):
+            raise ValueError("out must be (int8 [B, n, 2], float32 [B])")
+    _check(lib.fairy2i_add_rmsnorm_i8(x.data_ptr(), None if delta is None else delta.data_ptr(), gain.data_ptr(), eps,
+                                      B, n, None if h_out is None else h_out.data_ptr(), q.data_ptr(),
+                                      scale.data_ptr(), _raw_stream(x.get_device())), "fairy2i_add_rmsnorm_i8")
+    return x if h_out is None else h_out, q, scale
+
+
+def rope_table(n_pos, dc, base=10000.0, device="cuda"):
+    """float32 [n_pos, dc, 2]: (cos, sin) of p * base^(-j / dc) for position p
+    and entry j of a head (fairy2i_rope_table)."""
+    torch = _torch()
+    lib = load()
+    if n_pos < 1 or dc < 1:
+        raise ValueError("n_pos and dc must be positive")
+    out = torch.empty((n_pos, dc, 2), dtype=torch.float32, device=device)
+    _require(out, None, "device")
+    with torch.cuda.device(out.device):
+        _check(lib.fairy2i_rope_table(n_pos, dc, base, out.data_ptr(), _stream_ptr(out)), "fairy2i_rope_table")
+    return out
+
+
+class PagedKv:
+    """Paged cache of keys and values in microscaled 4-bit floating point, for
+    any number of sequences (fairy2i_kv_cache; the format and its layout are in
+    include/fairy2i.h).
+
+    n_pages pages of page_size positions (a multiple of 32), n_kv_heads heads
+    of dc complex entries (a multiple of 16, up to 128).  ``data``: a uint8
+    device tensor of PagedKv.bytes(...) bytes to use; a new one otherwise.
+
+    Every call takes the batch as three int32 device tensors: ``pages``
+    [n_seqs, max_pages] (the page of each run of page_size positions),
+    ``cu_new`` [n_seqs + 1] (sequence i's rows are cu_new[i] ..
+    cu_new[i + 1] - 1) and ``lens`` [n_seqs] (positions of the sequence, its
+    rows included).  They stay on the device: a captured graph follows what
+    they hold."""
+
+    def __init__(self, n_pages, page_size, n_kv_heads, dc, data=None, device="cuda"):
+        torch = _torch()
+        need = self.bytes(n_pages, page_size, n_kv_heads, dc)
+        if data is None:
+            data = torch.empty(need, dtype=torch.uint8, device=device)
+        _require(data, torch.uint8, "data")
+        if data.numel() < need:
+            raise ValueError(f"data must hold {need} bytes, got {data.numel()}")
+        self.data = data
+        self.n_pages, self.page_size, self.n_kv_heads, self.dc = n_pages, page_size, n_kv_heads, dc
+        self._desc = KvCacheDesc(data.data_ptr(), n_pages, page_size, n_kv_heads, dc, 0)
+        self._ref = ctypes.byref(self._desc)
+
+    @staticmethod
+    def bytes(n_pages, page_size, n_kv_heads, dc) -> int:
+        """Bytes of such a cache."""
+        need = int(load().fairy2i_kv_cache_bytes(n_pages, page_size, n_kv_heads, dc))
+        if need == 0:
+            raise ValueError("a cache has n_pages >= 1, page_size a multiple of 32 up to 2^20, n_kv_heads in "
+                             "[1, 65535] and dc a multiple of 16 up to 128")
+        return need
+
+    def _batch(self, pages, cu_new, lens, n_new):
+        torch = _torch_module
+        dev = self.data.device
+        for t, name in ((pages, "pages"), (cu_new, "cu_new"), (lens, "lens")):
+            _require(t, torch.int32, name, dev)
+        if pages.dim() != 2 or lens.shape != (pages.shape[0],) or cu_new.shape != (pages.shape[0] + 1,):
+            raise ValueError("pages must be [n_seqs, max_pages], cu_new [n_seqs + 1] and lens [n_seqs]")
+        return KvBatchDesc(pages.data_ptr(), cu_new.data_ptr(), lens.data_ptr(), n_new, *pages.shape)
+
+    def _rows(self, x, heads, name):
+        """(rows, heads, row stride) of complex64 [N, heads * dc] or [N, heads, dc] whose rows are whole."""
+        torch = _torch_module
+        if not isinstance(x, torch.Tensor):
+            raise TypeError(f"{name} must be a torch.Tensor")
+        if x.device != self.data.device:
+            raise ValueError(f"{name} is on {x.device}, expected {self.data.device}")
+        if x.dtype is not torch.complex64:
+            raise TypeError(f"{name} must be {torch.complex64}, got {x.dtype}")
+        if x.is_conj():
+            raise ValueError(f"{name} is a conjugated view: resolve_conj() it first")
+        dc, shape, stride = self.dc, x.shape, x.stride()
+        if len(shape) == 3:
+            whole = shape[2] == dc and stride[2] == 1 and (shape[1] == 1 or stride[1] == dc)
+            n = shape[1]
+        else:
+            whole = len(shape) == 2 and shape[1] % dc == 0 and stride[1] == 1
+            n = shape[1] // dc if whole else 0
+        if not whole or n == 0 or (heads is not None and n != heads):
+            raise ValueError(f"{name} must be [N, heads * {dc}] or [N, heads, {dc}]"
+                             + ("" if heads is None else f" with {heads} heads") + ", each row contiguous")
+        ld = stride[0] if shape[0] > 1 else n * dc
+        if ld < n * dc:
+            raise ValueError(f"{name}'s rows overlap")
+        return shape[0], n, ld
+
+    def append(self, k, v, pages, cu_new, lens, rope, q=None, q_out=None):
+        """Append the rows of k and v, k turned by its position, and turn q
+        alike (fairy2i_kv_append).
+
+        k, v: complex64 [N, n_kv_heads * dc]; q: complex64 [N, heads * dc] or
+        None (also [N, heads, dc]; rows may be columns of one wider product);
+        rope: float32 [positions, dc, 2] (rope_table).  Returns q in bf16,
+        [N, heads, dc, 2] (q_out: such a tensor to write), or None."""
+        torch = _torch_module or _torch()
+        lib = _lib or load()
+        N, _, k_ld = self._rows(k, self.n_kv_heads, "k")
+        Nv, _, v_ld = self._rows(v, self.n_kv_heads, "v")
+        heads = q_ld = 0
+        dev = self.data.device
+        if q is not None:
+            Nq, heads, q_ld = self._rows(q, None, "q")
+            if Nq != N:
+                raise ValueError("q, k and v must have as many rows")
+            if q_out is None:
+                q_out = torch.empty((N, heads, self.dc, 2), dtype=torch.bfloat16, device=dev)
+            else:
+                _require(q_out, torch.bfloat16, "q_out", dev)
+                if q_out.shape != (N, heads, self.dc, 2):
+                    raise ValueError(f"q_out must have shape {(N, heads, self.dc, 2)}")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if Nv != N:
+            raise ValueError("q, k and v must have as many rows")
+        _require(rope, torch.float32, "rope", dev)
+        if rope.dim() != 3 or rope.shape[1:] != (self.dc, 2):
+            raise ValueError(f"rope must be [positions, {self.dc}, 2]")
+        batch = self._batch(pages, cu_new, lens, N)
+        _check(lib.fairy2i_kv_append(self._ref, ctypes.byref(batch), None if q is None else q.data_ptr(), q_ld, heads,
+                                     k.data_ptr(), k_ld, v.data_ptr(), v_ld, rope.data_ptr(), rope.shape[0],
+                                     None if q is None else q_out.data_ptr(), _raw_stream(dev.index)),
+               "fairy2i_kv_append")
+        return q_out
+
+    def read(self, pages, cu_new, lens, n_new, out=None):
+        """(k, v) bf16 [n_new, n_kv_heads, dc, 2]: what the cache stands for
+        at the positions of the batch's n_new rows, exact (fairy2i_kv_read);
+        cu_new over whole sequences reads them all."""
+        torch = _torch_module or _torch()
+        lib = _lib or load()
+        dev = self.data.device
+        shape = (n_new, self.n_kv_heads, self.dc, 2)
+        if out is None:
+            out = (torch.empty(shape, dtype=torch.bfloat16, device=dev),
+                   torch.empty(shape, dtype=torch.bfloat16, device=dev))
+        for t in out:
+            _require(t, torch.bfloat16, "out", dev)
+            if t.shape != shape:
+                raise ValueError(f"out must be a pair of shape {shape}")
+        batch = self._batch(pages, cu_new, lens, n_new)
+        _check(lib.fairy2i_kv_read(self._ref, ctypes.byref(batch), out[0].data_ptr(), out[1].data_ptr(),
+                                   _raw_stream(dev.index)), "fairy2i_kv_read")
+        return tuple(out)
+
+    def attend_workspace_bytes(self, n_new, n_seqs, heads) -> int:
+        """Bytes of workspace that attend takes for such a batch."""
+        return int(load().fairy2i_kv_attend_workspace_bytes(self._ref, n_new, n_seqs, heads))
+
+    def attend(self, q, pages, cu_new, lens, scale=None, out=None, workspace=None):
+        """Causal Hermitian-score attention of the batch's rows over the cache
+        (fairy2i_kv_attend).
+
+        q: bf16 [N, heads, dc, 2], turned by its positions (append's result);
+        heads a multiple of n_kv_heads, neighbours sharing a key head; scale:
+        1 / sqrt(2 dc) by default.  Returns bf16 [N, heads, dc, 2] (out: such a
+        tensor to write); seen as [N, heads * dc, 2] it is what wl_matmul
+        takes."""
+        torch = _torch_module or _torch()
+        lib = _lib or load()
+        dev = self.data.device
+        _require(q, torch.bfloat16, "q", dev)
+        if q.dim() != 4 or q.shape[2:] != (self.dc, 2):
+            raise ValueError(f"q must be [N, heads, {self.dc}, 2]")
+        N, heads = q.shape[:2]
+        if heads == 0 or heads % self.n_kv_heads != 0:
+            raise ValueError(f"q's heads must be a multiple of {self.n_kv_heads}")
+        if out is None:
+            out = torch.empty_like(q)
+        else:
+            _require(out, torch.bfloat16, "out", dev)
+            if out.shape != q.shape:
+                raise ValueError("out must have q's shape")
+        batch = self._batch(pages, cu_new, lens, N)
+        if workspace is None:
+            need = lib.fairy2i_kv_attend_workspace_bytes(self._ref, N, pages.shape[0], heads)
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        else:  # its size is the library's to check
+            _require(workspace, torch.uint8, "workspace", dev)
+        _check(lib.fairy2i_kv_attend(self._ref, ctypes.byref(batch), q.data_ptr(), heads,
+                                     (2 * self.dc) ** -0.5 if scale is None else scale, out.data_ptr(),
+                                     workspace.data_ptr(), workspace.numel(), _raw_stream(dev.index)),
+               "fairy2i_kv_attend")
         return out

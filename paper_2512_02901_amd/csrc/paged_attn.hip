@@ -1,0 +1,537 @@
+// Hermitian-score attention over the paged 4-bit cache (fairy2i_kv_attend).
+//
+// Per key head the G query heads that share it and the sequence's new tokens
+// are rows (row = token * G + query head).  With one complex entry as two
+// reals, s = scale * Re(q^H k) is a real product, so everything is matrix
+// work: S^T = K Q^T and O^T = V^T P^T on v_mfma_f32_16x16x32_bf16, one block
+// of 32 reals (one scale) a product.  The 4-bit values become bf16 exactly
+// (a power of two times two bits) on their way into the operands, one
+// conversion for two values; the cache's layout is the operands' own, so a
+// lane's codes are its own 16-byte loads and S^T's accumulators are P^T's
+// operand as they stand.
+//
+// One pass with a running maximum and sum; positions are split over blocks
+// (chunks) and over a block's waves, joined through LDS and, where a row has
+// several chunks, by a second kernel.
+#include <math.h>
+
+#include "paged_kv.h"
+
+namespace fairy2i {
+
+namespace {
+
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kRows = 16;         // of a row tile
+constexpr int kMinChunk = 8;      // tiles: two a wave
+constexpr int kTargetItems = 1024;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct AttnArgs {
+  KvCache c;
+  KvBatch b;
+  const uint32_t* q;  // [n_new][heads][dc] bf16 pairs
+  uint32_t* out;      // the same
+  int32_t heads, group;
+  float scale;        // log2(e) times the score scale
+  float* part;        // [items][kRows][D] unnormalised sums
+  float2* ml;         // [items][kRows] running maximum and sum
+  int2* meta;         // [slots][kv_heads]: first item, chunks
+  int32_t items;
+};
+
+// Row tiles of a sequence: sequence i's start at slot row0 * G / 16 + i (its
+// ceil(n G / 16) tiles end before the next one's start).
+__device__ inline int row_slot(const AttnArgs& a, int i) {
+  return (int)((int64_t)kv_row(a.b, i) * a.group / kRows) + i;
+}
+int64_t row_slots(int64_t n_new, int64_t n_seqs, int group) { return n_new * group / kRows + n_seqs; }
+
+__device__ inline int row_tiles(const AttnArgs& a, const KvSeq& s) { return (int)(((int64_t)s.n * a.group + kRows - 1) / kRows); }
+__device__ inline int kv_tiles(int len) { return (len + kKvTile - 1) / kKvTile; }
+
+__device__ inline int64_t wave_sum(int64_t v) {
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+
+struct Item {
+  int seq, tile, head, chunk;  // row tile and chunk of the sequence, key head
+  int chunk_tiles;
+  KvSeq s;
+};
+
+// Chunks are as long as gives kTargetItems of them over all sequences, and
+// kMinChunk at least; every wave finds its block's item by itself.
+__device__ inline bool find_item(const AttnArgs& a, int id, Item& it) {
+  const int lane = threadIdx.x & 63;
+  int64_t work = 0;
+  for (int i = lane; i < a.b.n_seqs; i += 64) {
+    const KvSeq s = kv_seq(a.b, a.c, i);
+    work += (int64_t)kv_tiles(s.len) * row_tiles(a, s);
+  }
+  work = wave_sum(work) * a.c.kv_heads;
+  const int ct = max(kMinChunk, (int)((work + kTargetItems - 1) / kTargetItems));
+  int base = 0;  // items of the sequences before
+  for (int i0 = 0; i0 < a.b.n_seqs; i0 += 64) {
+    int items = 0;
+    if (i0 + lane < a.b.n_seqs) {
+      const KvSeq s = kv_seq(a.b, a.c, i0 + lane);
+      items = max(1, (kv_tiles(s.len) + ct - 1) / ct) * row_tiles(a, s) * a.c.kv_heads;
+    }
+    int upto = items;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int v = __shfl_up(upto, off);
+      if (lane >= off) upto += v;
+    }
+    const uint64_t past = __ballot(base + upto > id);
+    if (past != 0) {
+      const int w = __builtin_ctzll(past);
+      it.seq = __builtin_amdgcn_readfirstlane(i0 + w);
+      it.s = kv_seq(a.b, a.c, it.seq);
+      it.chunk_tiles = ct;
+      const int chunks = max(1, (kv_tiles(it.s.len) + ct - 1) / ct), rt = row_tiles(a, it.s);
+      const int local = id - base - __builtin_amdgcn_readfirstlane(__shfl(upto - items, w));
+      // heads next to each other, then chunks, then row tiles, the last (longest) first
+      const int hc = local / a.c.kv_heads, t = hc / chunks;
+      it.head = local - hc * a.c.kv_heads;
+      it.chunk = hc - t * chunks;
+      it.tile = rt - 1 - t;
+      return local >= 0 && it.tile >= 0;  // not so only for a cu_new that decreases
+    }
+    base += __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+  }
+  return false;
+}
+
+// A tile's codes and scales of one lane.
+template <int NB>
+struct TileRegs {
+  static constexpr KvTile T{NB};
+  uint32_t k[2 * NB], v[2 * NB];
+  uint32_t ks[2][(T.sb + 3) / 4], vs[2 * T.sb];
+
+  __device__ inline void load(const uint8_t* tile) {
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int u = 0; u < 2 * NB / T.unit; ++u) {
+      load_n<T.unit>(k + u * T.unit, tile + T.dword(u * T.unit, lane));
+      load_n<T.unit>(v + u * T.unit, tile + T.v_codes() + T.dword(u * T.unit, lane));
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint8_t* at = tile + T.k_scales() + (16 * s + r) * T.sb;
+      if constexpr (T.sb == 1) ks[s][0] = *at;
+      else if constexpr (T.sb == 2) ks[s][0] = *reinterpret_cast<const uint16_t*>(at);
+      else load_n<T.sb / 4>(ks[s], at);
+    }
+    load_n<2 * T.sb>(vs, tile + T.v_scales() + g * 8 * T.sb);
+  }
+
+  template <int N>
+  __device__ static inline void load_n(uint32_t* to, const uint8_t* at) {
+    if constexpr (N >= 4) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) {
+        const uint4 x = reinterpret_cast<const uint4*>(at)[i];
+        to[4 * i] = x.x;
+        to[4 * i + 1] = x.y;
+        to[4 * i + 2] = x.z;
+        to[4 * i + 3] = x.w;
+      }
+    } else if constexpr (N == 2) {
+      const uint2 x = *reinterpret_cast<const uint2*>(at);
+      to[0] = x.x;
+      to[1] = x.y;
+    } else {
+      to[0] = *reinterpret_cast<const uint32_t*>(at);
+    }
+  }
+
+  // Byte `i` of `words` as the scale operand: only its exponent field counts.
+  __device__ static inline float scale_at(const uint32_t* words, int i) {
+    const uint32_t w = words[i / 4];
+    const int b = i % 4;
+    return __uint_as_float(b == 3 ? w >> 1 : w << (23 - 8 * b));
+  }
+
+  // Keys of half `s` (16 positions), block b: the A operand of S^T.
+  __device__ inline bf16x8 key(int b, int s) const {
+    const float scale = scale_at(ks[s], b);
+    const uint32_t w = k[2 * b + s];
+    u32x4 o;
+    o[0] = pair<0>(w, scale);
+    o[1] = pair<1>(w, scale);
+    o[2] = pair<2>(w, scale);
+    o[3] = pair<3>(w, scale);
+    return __builtin_bit_cast(bf16x8, o);
+  }
+
+  // Values of block b: the A operands of O^T, real and imaginary parts.
+  __device__ inline void value(int b, bf16x8& re, bf16x8& im) const {
+    uint32_t c[8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t w = v[2 * b + h];
+      c[4 * h + 0] = pair<0>(w, scale_at(vs, (4 * h + 0) * T.sb + b));
+      c[4 * h + 1] = pair<1>(w, scale_at(vs, (4 * h + 1) * T.sb + b));
+      c[4 * h + 2] = pair<2>(w, scale_at(vs, (4 * h + 2) * T.sb + b));
+      c[4 * h + 3] = pair<3>(w, scale_at(vs, (4 * h + 3) * T.sb + b));
+    }
+    u32x4 lo, hi;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x05040100);
+      hi[i] = __builtin_amdgcn_perm(c[2 * i + 1], c[2 * i], 0x07060302);
+    }
+    re = __builtin_bit_cast(bf16x8, lo);
+    im = __builtin_bit_cast(bf16x8, hi);
+  }
+
+  template <int B>
+  __device__ static inline uint32_t pair(uint32_t w, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
+  }
+
+  // Scale bytes of the values from position `n` of the tile on, which nobody
+  // wrote: 2^0, so that their codes stay finite under a weight of zero.
+  __device__ inline void end_at(int n) {
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (16 * (j / 4) + 4 * g + j % 4 < n) continue;
+#pragma unroll
+      for (int b = 0; b < T.sb; ++b) {
+        const int i = j * T.sb + b;
+        vs[i / 4] = (vs[i / 4] & ~(0xFFu << (8 * (i % 4)))) | 127u << (8 * (i % 4));
+      }
+    }
+  }
+};
+
+// max over the four lanes that share a row
+__device__ inline float row_max(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const uint32_t x = __float_as_uint(v);
+  const auto c = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return fmaxf(__uint_as_float(c[0]), __uint_as_float(c[1]));
+}
+
+__device__ inline float row_sum(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const uint32_t x = __float_as_uint(v);
+  const auto c = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return __uint_as_float(c[0]) + __uint_as_float(c[1]);
+}
+
+__device__ inline uint32_t pack_bf16(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  bf16x2 p;
+  p[0] = (__bf16)lo;
+  p[1] = (__bf16)hi;
+  return __builtin_bit_cast(uint32_t, p);
+}
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Sixteen rows, a chunk of positions over four waves.
+template <int NB>
+__global__ __launch_bounds__(kThreads) void kv_attend_rows16_kernel(AttnArgs a) {
+  constexpr int D = 32 * NB, kStride = D + 4;
+  __shared__ float os[kWaves][kRows][kStride];
+  __shared__ float2 mls[kWaves][kRows];
+  Item it;
+  if (!find_item(a, blockIdx.x, it)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int r = lane & 15, g = lane >> 4;
+  const int rows = it.s.n * a.group, row = it.tile * kRows + r;
+  const int p0 = it.s.len - it.s.n;  // position of the first new token
+  const int token = row / a.group, hq = it.head * a.group + (row - token * a.group);
+  // what the row sees, and the least and most that any row of the tile sees
+  const int least = p0 + it.tile * kRows / a.group;
+  const int most = p0 + (min(it.tile * kRows + kRows, rows) - 1) / a.group;
+  const int last = min(p0 + token, most);  // rows past the end compute what nobody stores
+  const int tiles = kv_tiles(most + 1), chunks = max(1, (tiles + it.chunk_tiles - 1) / it.chunk_tiles);
+  if (it.chunk == 0 && threadIdx.x == 0)
+    a.meta[(int64_t)(row_slot(a, it.seq) + it.tile) * a.c.kv_heads + it.head] =
+        make_int2((int)blockIdx.x, chunks);
+  if (it.chunk >= chunks) return;
+  const int t_end = min(tiles, (it.chunk + 1) * it.chunk_tiles);
+
+  bf16x8 q[NB];
+  {
+    const uint32_t* at = a.q + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB) + 4 * g;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      u32x4 x = {0, 0, 0, 0};
+      if (row < rows) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = at[16 * b + k];
+      }
+      q[b] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  f32x4 o[2 * NB];
+#pragma unroll
+  for (int i = 0; i < 2 * NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.0f;  // the row's maximum (unscaled), the lane's share of its sum
+
+  auto tile_at = [&](int t) { return kv_tile(a.c, a.b, it.seq, t * kKvTile, it.head, KvTile(NB).bytes); };
+  TileRegs<NB> next;
+  int t = it.chunk * it.chunk_tiles + wave;
+  const uint8_t* at = t < t_end ? tile_at(t) : nullptr;
+  if (at) next.load(at);
+  for (; t < t_end; t += kWaves) {
+    TileRegs<NB> x = next;
+    const bool present = at != nullptr;
+    at = t + kWaves < t_end ? tile_at(t + kWaves) : nullptr;
+    if (at) next.load(at);
+    if (!present) continue;  // no such page: nothing to see there
+    f32x4 s[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.key(b, h), q[b], s[h], 0, 0, 0);
+    }
+    const int t0 = t * kKvTile;
+    if (t0 + kKvTile - 1 > least) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (t0 + 16 * h + 4 * g + i > last) s[h][i] = -INFINITY;
+      if (t0 + kKvTile > it.s.len) x.end_at(it.s.len - t0);
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i / 4][i % 4]);
+    top = fmaxf(m, row_max(top));
+    if (__any(top > m)) {
+      const float f = top == -INFINITY ? 1.0f : exp2_of((m - top) * a.scale);
+      m = top;
+      l *= f;
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) o[i] *= f;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m * a.scale;
+    u32x4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float p[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        p[e] = exp2_of(__builtin_fmaf(s[i / 2][2 * (i % 2) + e], a.scale, -ref));
+        l += p[e];
+      }
+      // the weight in two bf16 parts: what rounding it to one leaves is of the
+      // size of the output's own rounding
+      hi[i] = pack_bf16(p[0], p[1]);
+      lo[i] = pack_bf16(p[0] - __uint_as_float(hi[i] << 16), p[1] - __uint_as_float(hi[i] & 0xFFFF0000u));
+    }
+    const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      bf16x8 re, im;
+      x.value(b, re, im);
+      o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(re, ph, o[2 * b], 0, 0, 0);
+      o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(im, ph, o[2 * b + 1], 0, 0, 0);
+      o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(re, pl, o[2 * b], 0, 0, 0);
+      o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(im, pl, o[2 * b + 1], 0, 0, 0);
+    }
+  }
+  // join the waves
+  l = row_sum(l);
+  if (g == 0) mls[wave][r] = make_float2(m, l);
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)  // entry 16 b + 4 g + i
+      *reinterpret_cast<float2*>(&os[wave][r][32 * b + 8 * g + 2 * i]) = make_float2(o[2 * b][i], o[2 * b + 1][i]);
+  __syncthreads();
+  for (int e = threadIdx.x; e < kRows * (D / 2); e += kThreads) {
+    const int rr = e / (D / 2), c = e - rr * (D / 2), w = it.tile * kRows + rr;
+    if (w >= rows) continue;
+    float top = mls[0][rr].x;
+#pragma unroll
+    for (int i = 1; i < kWaves; ++i) top = fmaxf(top, mls[i][rr].x);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+    float2 y = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+      const float f = exp2_of((mls[i][rr].x - ref) * a.scale);
+      sum += f * mls[i][rr].y;
+      const float2 v = *reinterpret_cast<const float2*>(&os[i][rr][2 * c]);
+      y.x += f * v.x;
+      y.y += f * v.y;
+    }
+    if (chunks == 1) {
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      const int tk = w / a.group, hh = it.head * a.group + (w - tk * a.group);
+      a.out[((int64_t)(it.s.row0 + tk) * a.heads + hh) * (D / 2) + c] = pack_bf16(y.x * inv, y.y * inv);
+    } else {
+      const int64_t rec = (int64_t)blockIdx.x * kRows + rr;
+      *reinterpret_cast<float2*>(a.part + rec * D + 2 * c) = y;
+      if (c == 0) a.ml[rec] = make_float2(top, sum);
+    }
+  }
+}
+
+// Joins a row tile's chunks; blockIdx.y takes rows y, y + gridDim.y, ...
+template <int NB>
+__global__ __launch_bounds__(kThreads) void kv_attend_join_kernel(AttnArgs a) {
+  constexpr int D = 32 * NB, kPairs = D / 2, kLanes = kPairs <= 16 ? 16 : kPairs <= 32 ? 32 : kPairs <= 64 ? 64 : 128;
+  constexpr int kParts = kThreads / kLanes;
+  __shared__ float2 ys[kParts][kLanes];
+  __shared__ float sums[kParts];
+  const int slot = blockIdx.x / a.c.kv_heads, head = blockIdx.x - slot * a.c.kv_heads;
+  const int i = kv_find(a.b.n_seqs, slot, [&](int s) { return row_slot(a, s); });
+  if (i < 0) return;
+  const KvSeq s = kv_seq(a.b, a.c, i);
+  const int tile = slot - row_slot(a, i);
+  if (tile < 0 || tile >= row_tiles(a, s)) return;
+  const int2 meta = a.meta[(int64_t)slot * a.c.kv_heads + head];
+  const int chunks = meta.y;
+  if (chunks < 2) return;
+  // a chunk is kv_heads items after the one before; nothing else can stand
+  // there unless cu_new decreases somewhere and no item wrote it
+  if (meta.x < 0 || meta.x >= a.items || (int64_t)meta.x + (int64_t)(chunks - 1) * a.c.kv_heads >= a.items) return;
+  const int part = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
+  const int rows = s.n * a.group;
+  for (int rr = blockIdx.y; rr < kRows; rr += gridDim.y) {
+    const int w = tile * kRows + rr;
+    if (w >= rows) break;
+    float top = -INFINITY;
+    for (int k = threadIdx.x & 63; k < chunks; k += 64)
+      top = fmaxf(top, a.ml[((int64_t)meta.x + (int64_t)k * a.c.kv_heads) * kRows + rr].x);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+    float2 y = make_float2(0.0f, 0.0f);
+    for (int k = part; k < chunks; k += kParts) {
+      const int64_t rec = ((int64_t)meta.x + (int64_t)k * a.c.kv_heads) * kRows + rr;
+      const float2 ml = a.ml[rec];
+      const float f = exp2_of((ml.x - ref) * a.scale);
+      sum += f * ml.y;
+      if (c < kPairs) {
+        const float2 v = *reinterpret_cast<const float2*>(a.part + rec * D + 2 * c);
+        y.x += f * v.x;
+        y.y += f * v.y;
+      }
+    }
+    __syncthreads();  // the last row's readers
+    ys[part][c] = y;
+    if (c == 0) sums[part] = sum;
+    __syncthreads();
+    if (part == 0 && c < kPairs) {
+#pragma unroll
+      for (int k = 1; k < kParts; ++k) {
+        sum += sums[k];
+        y.x += ys[k][c].x;
+        y.y += ys[k][c].y;
+      }
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+      const int tk = w / a.group, hh = head * a.group + (w - tk * a.group);
+      a.out[((int64_t)(s.row0 + tk) * a.heads + hh) * kPairs + c] = pack_bf16(y.x * inv, y.y * inv);
+    }
+  }
+}
+
+struct Layout {
+  int64_t items, slots;
+  size_t part, ml, meta, bytes;
+};
+
+Layout layout_of(const fairy2i_kv_cache* c, int64_t n_new, int64_t n_seqs, int32_t n_heads) {
+  Layout l{};
+  const int64_t G = n_heads / c->n_kv_heads;
+  // a row tile more than its rows fill for each sequence that has any, and a
+  // chunk more than its work fills for each row tile
+  l.items = kTargetItems + c->n_kv_heads * (n_new * G / kRows + (n_seqs < n_new ? n_seqs : n_new));
+  l.slots = row_slots(n_new, n_seqs, (int)G);
+  auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+  l.part = up((size_t)l.items * kRows * 2 * c->dc * sizeof(float));
+  l.ml = up((size_t)l.items * kRows * sizeof(float2));
+  l.meta = up((size_t)l.slots * c->n_kv_heads * sizeof(int2));
+  l.bytes = l.part + l.ml + l.meta;
+  return l;
+}
+
+template <int NB>
+void launch(const AttnArgs& a, const Layout& l, bool one_chunk, hipStream_t s) {
+  hipLaunchKernelGGL(kv_attend_rows16_kernel<NB>, dim3((unsigned)l.items), dim3(kThreads), 0, s, a);
+  if (one_chunk) return;
+  const int64_t blocks = l.slots * a.c.kv_heads;
+  const unsigned split = blocks <= 512 ? kRows : blocks <= 2048 ? 4 : 1;
+  hipLaunchKernelGGL(kv_attend_join_kernel<NB>, dim3((unsigned)blocks, split), dim3(kThreads), 0, s, a);
+}
+
+bool valid_heads(const fairy2i_kv_cache* c, int32_t n_heads) {
+  return n_heads >= 1 && n_heads <= 65535 && n_heads % c->n_kv_heads == 0;
+}
+
+}  // namespace
+
+}  // namespace fairy2i
+
+using namespace fairy2i;
+
+extern "C" {
+
+size_t fairy2i_kv_attend_workspace_bytes(const fairy2i_kv_cache* cache, int64_t n_new, int64_t n_seqs,
+                                         int32_t n_heads) {
+  if (!cache || fairy2i_kv_cache_bytes(cache->n_pages, cache->page_size, cache->n_kv_heads, cache->dc) == 0 ||
+      !valid_heads(cache, n_heads) || n_new < 1 || n_new > (1 << 26) || n_seqs < 1 || n_seqs > (1 << 20))
+    return 0;
+  return layout_of(cache, n_new, n_seqs, n_heads).bytes;
+}
+
+fairy2i_status fairy2i_kv_attend(const fairy2i_kv_cache* cache, const fairy2i_kv_batch* batch, const void* q,
+                                 int32_t n_heads, float scale, void* out, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  if (const fairy2i_status s = kv_check(cache, batch)) return s;
+  if (!q || !out) return FAIRY2I_ERR_NULL;
+  if (!valid_heads(cache, n_heads) || !(scale > 0.0f) || !(scale <= 1e30f)) return FAIRY2I_ERR_SHAPE;
+  const Layout l = layout_of(cache, batch->n_new, batch->n_seqs, n_heads);
+  if (!workspace || workspace_bytes < l.bytes || (reinterpret_cast<uintptr_t>(workspace) & 15) != 0)
+    return FAIRY2I_ERR_WORKSPACE;
+  if (l.items > INT32_MAX / 256 || l.slots * cache->n_kv_heads > INT32_MAX / 256) return FAIRY2I_ERR_UNSUPPORTED;
+  AttnArgs a{};
+  a.c = kv_cache_of(cache);
+  a.b = kv_batch_of(batch);
+  a.q = static_cast<const uint32_t*>(q);
+  a.out = static_cast<uint32_t*>(out);
+  a.heads = n_heads;
+  a.group = n_heads / cache->n_kv_heads;
+  a.scale = scale * 1.44269504088896341f;
+  a.items = (int32_t)l.items;
+  char* ws = static_cast<char*>(workspace);
+  a.part = reinterpret_cast<float*>(ws);
+  a.ml = reinterpret_cast<float2*>(ws + l.part);
+  a.meta = reinterpret_cast<int2*>(ws + l.part + l.ml);
+  const bool one_chunk = (int64_t)batch->max_pages * cache->page_size <= kMinChunk * kKvTile;
+  auto s = static_cast<hipStream_t>(stream);
+  switch (cache->dc / 16) {
+    case 1: launch<1>(a, l, one_chunk, s); break;
+    case 2: launch<2>(a, l, one_chunk, s); break;
+    case 3: launch<3>(a, l, one_chunk, s); break;
+    case 4: launch<4>(a, l, one_chunk, s); break;
+    case 5: launch<5>(a, l, one_chunk, s); break;
+    case 6: launch<6>(a, l, one_chunk, s); break;
+    case 7: launch<7>(a, l, one_chunk, s); break;
+    default: launch<8>(a, l, one_chunk, s); break;
+  }
+  return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,353 @@
+// Append to and read from the paged 4-bit cache.
+//
+// A wave owns four neighbouring positions (4 g .. 4 g + 3) of a head, a lane
+// one or two complex entries of them.  Four positions are what a dword of
+// either code array holds: a value dword is four positions of an entry, a key
+// dword four entries of a position, so both go out whole (the keys' bytes
+// transposed within four lanes), and no two waves share a byte.
+#include <math.h>
+
+#include "paged_kv.h"
+
+namespace fairy2i {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// Groups of four positions: sequence i's start at slot cu_new[i] / 4 + 2 i, so
+// a slot's sequence is found without adding up anything.  (n positions touch
+// at most (n + 2) / 4 + 1 <= n / 4 + 2 groups.)
+__device__ inline int slot_of(const KvBatch& b, int i) { return (kv_row(b, i) >> 2) + 2 * i; }
+inline int64_t slots(int64_t n_new, int64_t n_seqs) { return n_new / 4 + 2 * n_seqs; }
+
+// 4 x 4 bytes transposed over four lanes: byte j of lane i's result is byte i
+// of lane j's argument.
+__device__ inline uint32_t transpose4(uint32_t x) {
+  const int sh = 8 * (threadIdx.x & 3);
+  uint32_t r = ((uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x00, 0xF, 0xF, true) >> sh & 0xFF);
+  r |= ((uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x55, 0xF, 0xF, true) >> sh & 0xFF) << 8;
+  r |= ((uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xAA, 0xF, 0xF, true) >> sh & 0xFF) << 16;
+  r |= ((uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xFF, 0xF, 0xF, true) >> sh & 0xFF) << 24;
+  return r;
+}
+
+// (re + i im)(c + i s), each product and sum rounded once.
+__device__ inline float2 turn(float2 v, float2 cs) {
+#pragma clang fp contract(off)
+  return make_float2(v.x * cs.x - v.y * cs.y, v.x * cs.y + v.y * cs.x);
+}
+
+__device__ inline uint32_t bf16_of(float v) {  // nearest even; a NaN stays one
+  const uint32_t u = __float_as_uint(v);
+  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (u >> 16) | 0x40u;
+  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+}
+
+__device__ inline uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Biased exponent of the scale for a block whose largest magnitude has the
+// bits `top`: the smallest e with top <= 7 2^e, so that what saturates at 6 is
+// off by at most the half step of [4, 6]; from 2^-125 (0.5 2^e stays normal)
+// to 2^125 (6 2^e stays finite).
+__device__ inline uint32_t scale_of(uint32_t top) {
+  const int e = (int)(top >> 23) - 2 + ((top & 0x7FFFFFu) > 0x600000u);
+  return (uint32_t)min(max(e, 2), 252);
+}
+
+// v / 2^e to the nearest of 0 .5 1 1.5 2 3 4 6 (ties to the even code).
+__device__ inline uint32_t e2m1(float v, uint32_t scale) {
+  const float u = v * __uint_as_float((254u - scale) << 23), a = fabsf(u);
+  const uint32_t c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.0f);
+  return c | (__float_as_uint(v) >> 28 & 8u);
+}
+
+struct AppendArgs {
+  KvCache c;
+  KvBatch b;
+  const float2 *q, *k, *v;
+  int64_t q_ld, k_ld, v_ld;
+  const float2* rope;  // [rope_len][dc]
+  int64_t rope_len;
+  uint32_t* q_out;     // [n_new][heads][dc] bf16 pairs, or null
+  int32_t heads;
+  int32_t head_groups; // of keys and values: waves that a slot takes
+  int32_t kv_blocks, q_chunks;
+};
+
+// EPL: entries a lane (2 for dc > 64).  Heads of up to 32 entries share a wave.
+template <int EPL>
+__device__ void append_kv(const AppendArgs& a) {
+  const int lane = threadIdx.x & 63, dc = a.c.dc;
+  const int job = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)));
+  const int slot = job / a.head_groups, hg = job - slot * a.head_groups;
+  const int i = kv_find(a.b.n_seqs, slot, [&](int s) { return slot_of(a.b, s); });
+  if (i < 0) return;
+  const KvSeq s = kv_seq(a.b, a.c, i);
+  const int p0 = s.len - s.n, group = (max(p0, 0) >> 2) + slot - slot_of(a.b, i), u0 = 4 * group % kKvTile;
+  if (s.n == 0 || group < 0 || 4 * (int64_t)group >= s.len) return;
+  const int hpw = dc <= 32 ? 64 / dc : 1;  // heads a wave
+  const int sub = hpw > 1 ? lane / dc : 0, h = hg * hpw + sub;
+  const KvTile t(dc / 16);
+  const bool head = h < a.c.kv_heads;
+  uint8_t* tile = kv_tile(a.c, a.b, i, 4 * group, head ? h : 0, t.bytes);
+  if (!tile) return;
+  uint32_t valid = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int p = 4 * group + j;
+    if (p >= p0 && p < s.len && p < a.rope_len) valid |= 1u << j;
+  }
+  float2 kx[EPL][4], vx[EPL][4];
+#pragma unroll
+  for (int x = 0; x < EPL; ++x) {
+    const int e = lane - sub * dc + 64 * x;
+    const bool mine = head && e < dc;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool load = mine && (valid >> j & 1);
+      const int64_t row = s.row0 + (4 * group + j - p0);
+      const float2 zero = make_float2(0.0f, 0.0f);
+      const float2 cs = load ? a.rope[(int64_t)(4 * group + j) * dc + e] : zero;
+      const float2 k = load ? a.k[row * a.k_ld + (int64_t)h * dc + e] : zero;
+      kx[x][j] = turn(k, cs);
+      vx[x][j] = load ? a.v[row * a.v_ld + (int64_t)h * dc + e] : zero;
+    }
+  }
+  // whole-wave work from here on: every lane takes part in the exchanges
+  uint32_t bad = 0;  // positions of the lane's head that hold a value that is not finite
+  const uint64_t of_head = hpw > 1 ? ((1ull << dc) - 1) << (sub * dc) : ~0ull;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int x = 0; x < EPL; ++x)
+      top = max(top, max(max(abs_bits(kx[x][j].x), abs_bits(kx[x][j].y)), max(abs_bits(vx[x][j].x), abs_bits(vx[x][j].y))));
+    if (__ballot(top >= 0x7F800000u) & of_head) bad |= 1u << j;
+  }
+#pragma unroll
+  for (int x = 0; x < EPL; ++x) {
+    const int e = lane - sub * dc + 64 * x, b = e / 16, r = e % 16;
+    const bool mine = head && e < dc;
+    uint32_t kc = 0, vc = 0, my_ks = 0, my_vs = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t kt = max(abs_bits(kx[x][j].x), abs_bits(kx[x][j].y));
+      uint32_t vt = max(abs_bits(vx[x][j].x), abs_bits(vx[x][j].y));
+#pragma unroll
+      for (int off = 8; off > 0; off >>= 1) {
+        kt = max(kt, (uint32_t)__shfl_xor((int)kt, off));
+        vt = max(vt, (uint32_t)__shfl_xor((int)vt, off));
+      }
+      // a value block that is not finite is stored as zeros: its position's
+      // keys carry the NaN, so whoever attends to it sees one, nobody else
+      const bool void_v = vt >= 0x7F800000u;
+      if (void_v) vt = 0;
+      const uint32_t ks = scale_of(kt), vs = scale_of(vt);
+      kc |= (e2m1(kx[x][j].x, ks) | e2m1(kx[x][j].y, ks) << 4) << (8 * j);
+      if (!void_v) vc |= (e2m1(vx[x][j].x, vs) | e2m1(vx[x][j].y, vs) << 4) << (8 * j);
+      if (r == j) {
+        my_ks = bad >> j & 1 ? 255u : ks;
+        my_vs = vs;
+      }
+    }
+    const uint32_t kd = transpose4(kc);
+    if (mine) {
+      const int w = 2 * b + u0 / 16, g = u0 % 16 / 4, j = lane & 3;
+      if (valid >> j & 1) *reinterpret_cast<uint32_t*>(tile + t.dword(w, r / 4 * 16 + u0 % 16 + j)) = kd;
+      uint8_t* at = tile + t.v_codes() + t.dword(w, g * 16 + r);
+      if (valid == 15) {
+        *reinterpret_cast<uint32_t*>(at) = vc;
+      } else {
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          if (valid >> m & 1) at[m] = (uint8_t)(vc >> (8 * m));
+      }
+      if (r < 4 && (valid >> r & 1)) {
+        tile[t.k_scales() + (u0 + r) * t.sb + b] = (uint8_t)my_ks;
+        tile[t.v_scales() + (g * 8 + u0 / 16 * 4 + r) * t.sb + b] = (uint8_t)my_vs;
+      }
+    }
+  }
+}
+
+// 1024 entries of a token's q.
+__device__ void rotate_q(const AppendArgs& a) {
+  const int id = (int)blockIdx.x - a.kv_blocks, row = id / a.q_chunks, e0 = (id - row * a.q_chunks) * 1024;
+  const int i = kv_find(a.b.n_seqs, row, [&](int s) { return kv_row(a.b, s); });
+  int64_t p = -1;
+  if (i >= 0) {
+    const KvSeq s = kv_seq(a.b, a.c, i);
+    if (row < s.row0 + s.n) p = s.len - s.n + (row - s.row0);
+  }
+  const int n = a.heads * a.c.dc;
+  float2 x[4], cs[4];
+  const bool known = p >= 0 && p < a.rope_len;
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    const int e = e0 + m * kThreads + threadIdx.x;
+    x[m] = cs[m] = make_float2(__builtin_nanf(""), __builtin_nanf(""));
+    if (known && e < n) {
+      x[m] = a.q[(int64_t)row * a.q_ld + e];
+      cs[m] = a.rope[p * a.c.dc + e % a.c.dc];
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    const int e = e0 + m * kThreads + threadIdx.x;
+    const float2 y = turn(x[m], cs[m]);
+    if (e < n) a.q_out[(int64_t)row * n + e] = bf16_of(y.x) | bf16_of(y.y) << 16;
+  }
+}
+
+template <int EPL>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
+  if ((int)blockIdx.x < a.kv_blocks) append_kv<EPL>(a);
+  else rotate_q(a);
+}
+
+struct ReadArgs {
+  KvCache c;
+  KvBatch b;
+  uint32_t *k, *v;  // [n_new][kv_heads][dc] bf16 pairs
+  int32_t head_groups;
+};
+
+template <int EPL>
+__global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
+  const int lane = threadIdx.x & 63, dc = a.c.dc;
+  const int job = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)));
+  const int slot = job / a.head_groups, hg = job - slot * a.head_groups;
+  const int i = kv_find(a.b.n_seqs, slot, [&](int s) { return slot_of(a.b, s); });
+  if (i < 0) return;
+  const KvSeq s = kv_seq(a.b, a.c, i);
+  const int p0 = s.len - s.n, group = (max(p0, 0) >> 2) + slot - slot_of(a.b, i), u0 = 4 * group % kKvTile;
+  if (s.n == 0 || group < 0 || 4 * (int64_t)group >= s.len) return;
+  const int hpw = dc <= 32 ? 64 / dc : 1;
+  const int sub = hpw > 1 ? lane / dc : 0, h = hg * hpw + sub;
+  const KvTile t(dc / 16);
+  const bool head = h < a.c.kv_heads;
+  const uint8_t* tile = kv_tile(a.c, a.b, i, 4 * group, head ? h : 0, t.bytes);
+#pragma unroll
+  for (int x = 0; x < EPL; ++x) {
+    const int e = lane - sub * dc + 64 * x, b = e / 16, r = e % 16;
+    const bool mine = head && e < dc;
+    const int w = 2 * b + u0 / 16, g = u0 % 16 / 4;
+    uint32_t kd = 0, vd = 0, ks[4] = {255, 255, 255, 255}, vs[4] = {255, 255, 255, 255};  // no page: NaN
+    if (mine && tile) {
+      kd = *reinterpret_cast<const uint32_t*>(tile + t.dword(w, r / 4 * 16 + u0 % 16 + (lane & 3)));
+      vd = *reinterpret_cast<const uint32_t*>(tile + t.v_codes() + t.dword(w, g * 16 + r));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        ks[j] = tile[t.k_scales() + (u0 + j) * t.sb + b];
+        vs[j] = tile[t.v_scales() + (g * 8 + u0 / 16 * 4 + j) * t.sb + b];
+      }
+    }
+    kd = transpose4(kd);
+    auto pair = [](uint32_t codes, uint32_t scale) {  // a power of two times a value of two bits: exact in bf16
+      return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, __uint_as_float(scale << 23), 0));
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int p = 4 * group + j;
+      if (mine && p >= p0 && p < s.len) {
+        const int64_t at = ((int64_t)(s.row0 + (p - p0)) * a.c.kv_heads + h) * dc + e;
+        a.k[at] = pair(kd >> (8 * j), ks[j]);
+        a.v[at] = pair(vd >> (8 * j), vs[j]);
+      }
+    }
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void rope_table_kernel(int64_t n, int dc, double base, float2* __restrict__ out) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= n) return;
+  const int64_t p = i / dc;
+  double sn, cs;
+  sincos((double)p * pow(base, -(double)(i - p * dc) / dc), &sn, &cs);
+  out[i] = make_float2((float)cs, (float)sn);
+}
+
+int head_groups(int kv_heads, int dc) {
+  const int hpw = dc <= 32 ? 64 / dc : 1;
+  return (kv_heads + hpw - 1) / hpw;
+}
+
+}  // namespace
+
+}  // namespace fairy2i
+
+using namespace fairy2i;
+
+extern "C" {
+
+size_t fairy2i_kv_cache_bytes(int64_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t dc) {
+  if (n_pages < 1 || n_pages > INT32_MAX || page_size < kKvTile || page_size > (1 << 20) || page_size % kKvTile != 0 ||
+      n_kv_heads < 1 || n_kv_heads > 65535 || dc < 16 || dc > kKvMaxDc || dc % 16 != 0)
+    return 0;
+  const double bytes = (double)n_pages * n_kv_heads * (page_size / kKvTile) * KvTile(dc / 16).bytes;
+  if (bytes > 9e18) return 0;
+  return (size_t)n_pages * (size_t)n_kv_heads * (size_t)(page_size / kKvTile) * (size_t)KvTile(dc / 16).bytes;
+}
+
+fairy2i_status fairy2i_rope_table(int64_t n_pos, int32_t dc, double base, float* out, void* stream) {
+  if (!out) return FAIRY2I_ERR_NULL;
+  if (n_pos < 1 || n_pos > ((int64_t)1 << 30) || dc < 1 || dc > 4096 || !(base > 0.0) || !(base <= 1e300))
+    return FAIRY2I_ERR_SHAPE;
+  const int64_t n = n_pos * dc, blocks = (n + kThreads - 1) / kThreads;
+  if (blocks > INT32_MAX) return FAIRY2I_ERR_SHAPE;
+  hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream), n,
+                     (int)dc, base, reinterpret_cast<float2*>(out));
+  return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
+}
+
+fairy2i_status fairy2i_kv_append(const fairy2i_kv_cache* cache, const fairy2i_kv_batch* batch, const float* q,
+                                 int64_t q_ld, int32_t n_heads, const float* k, int64_t k_ld, const float* v,
+                                 int64_t v_ld, const float* rope, int64_t rope_len, void* q_out, void* stream) {
+  if (const fairy2i_status s = kv_check(cache, batch)) return s;
+  if (!k || !v || !rope || (q && !q_out) || (!q && q_out)) return FAIRY2I_ERR_NULL;
+  const int64_t nkv = (int64_t)cache->n_kv_heads * cache->dc, nq = q ? (int64_t)n_heads * cache->dc : 0;
+  if (rope_len < 1 || k_ld < nkv || v_ld < nkv || (q && (n_heads < 1 || n_heads > 65535 || q_ld < nq)))
+    return FAIRY2I_ERR_SHAPE;
+  AppendArgs a{};
+  a.c = kv_cache_of(cache);
+  a.b = kv_batch_of(batch);
+  a.q = reinterpret_cast<const float2*>(q);
+  a.k = reinterpret_cast<const float2*>(k);
+  a.v = reinterpret_cast<const float2*>(v);
+  a.q_ld = q_ld;
+  a.k_ld = k_ld;
+  a.v_ld = v_ld;
+  a.rope = reinterpret_cast<const float2*>(rope);
+  a.rope_len = rope_len;
+  a.q_out = static_cast<uint32_t*>(q_out);
+  a.heads = n_heads;
+  a.head_groups = head_groups(cache->n_kv_heads, cache->dc);
+  const int64_t waves = slots(batch->n_new, batch->n_seqs) * a.head_groups, kv_blocks = (waves + 3) / 4;
+  const int64_t chunks = (nq + 1023) / 1024, blocks = kv_blocks + chunks * batch->n_new;
+  if (waves > INT32_MAX - 4 || blocks > INT32_MAX) return FAIRY2I_ERR_UNSUPPORTED;
+  a.kv_blocks = (int32_t)kv_blocks;
+  a.q_chunks = (int32_t)chunks;
+  auto kernel = cache->dc <= 64 ? kv_append_kernel<1> : kv_append_kernel<2>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+  return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
+}
+
+fairy2i_status fairy2i_kv_read(const fairy2i_kv_cache* cache, const fairy2i_kv_batch* batch, void* k_out, void* v_out,
+                               void* stream) {
+  if (const fairy2i_status s = kv_check(cache, batch)) return s;
+  if (!k_out || !v_out) return FAIRY2I_ERR_NULL;
+  ReadArgs a{};
+  a.c = kv_cache_of(cache);
+  a.b = kv_batch_of(batch);
+  a.k = static_cast<uint32_t*>(k_out);
+  a.v = static_cast<uint32_t*>(v_out);
+  a.head_groups = head_groups(cache->n_kv_heads, cache->dc);
+  const int64_t waves = slots(batch->n_new, batch->n_seqs) * a.head_groups;
+  if (waves > INT32_MAX - 4) return FAIRY2I_ERR_UNSUPPORTED;
+  auto kernel = cache->dc <= 64 ? kv_read_kernel<1> : kv_read_kernel<2>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + 3) / 4)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+  return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
+}
+
+}  // extern "C"

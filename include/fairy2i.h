@@ -784,8 +784,8 @@ typedef struct fairy2i_kv_batch {
 } fairy2i_kv_batch;
 
 /* Bytes of a cache; 0 for sizes that are not supported (n_pages < 1,
- * page_size not a multiple of 32 in [32, 2^20], n_kv_heads outside [1, 65535],
- * dc not a multiple of 16 in [16, 128]). */
+ * page_size not a multiple of 32 in [32, 65536], n_kv_heads outside [1, 65535],
+ * dc not a multiple of 16 in [16, 128], 2^31 tiles or more). */
 size_t fairy2i_kv_cache_bytes(int64_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t dc);
 
 /*
@@ -837,13 +837,13 @@ fairy2i_status fairy2i_kv_read(const fairy2i_kv_cache* cache, const fairy2i_kv_b
  * only positions without a page) is zero.  The rows' own keys and values have
  * to be in the cache.
  * Scores, maximum, sum and the weighted sums are float32; the weights enter
- * the matrix cores as bf16 (as two bf16 parts where few rows share a pass).
+ * the matrix cores as two bf16 parts (2^-16 relative).
  * The result of a call does not depend on the order in which its blocks run.
  * workspace: fairy2i_kv_attend_workspace_bytes(cache, n_new, n_seqs, n_heads)
  * bytes, 16-byte aligned, contents ignored (cache->data is not looked at; 0
  * for sizes that are not supported).
  * Errors: as fairy2i_kv_append; FAIRY2I_ERR_SHAPE for n_heads that is not a
- * multiple of n_kv_heads or a scale outside (0, 1e30];
+ * multiple of n_kv_heads or a scale outside [1e-30, 1e30];
  * FAIRY2I_ERR_WORKSPACE.
  */
 size_t fairy2i_kv_attend_workspace_bytes(const fairy2i_kv_cache* cache, int64_t n_new, int64_t n_seqs,

@@ -1019,7 +1019,7 @@ class PagedKv:
         """Bytes of such a cache."""
         need = int(load().fairy2i_kv_cache_bytes(n_pages, page_size, n_kv_heads, dc))
         if need == 0:
-            raise ValueError("a cache has n_pages >= 1, page_size a multiple of 32 up to 2^20, n_kv_heads in "
+            raise ValueError("a cache has n_pages >= 1, page_size a multiple of 32 up to 65536, n_kv_heads in "
                              "[1, 65535] and dc a multiple of 16 up to 128")
         return need
 

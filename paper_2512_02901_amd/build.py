@@ -37,6 +37,7 @@ EXTRA = {
     "decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "decode_f4_split.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "block.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "paged_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     # and leave the cooperative kernel's one-lane claim atomics as written (the
     # atomic optimizer would read each result back at once, waiting for every
     # load in flight)

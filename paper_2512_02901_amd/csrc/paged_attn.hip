@@ -21,10 +21,20 @@ namespace fairy2i {
 
 namespace {
 
+constexpr int kRows = 16;         // that a matrix product takes
+constexpr int kCus = 256;
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kRows = 16;         // of a row tile
+// Blocks of 16 rows in a row tile: one where no sequence can have more, else
+// as many as share a conversion.
+constexpr int wide_rb(int nb) { return nb <= 4 ? 2 : 1; }
+// What a call is cut into, where its rows alone are fewer.
+constexpr int kItems = 1024;
 constexpr int kMinChunk = 8;      // tiles: two a wave
-constexpr int kTargetItems = 1024;
+
+// The running reference of a row's weights is raised once a score is 2^8 past
+// it: raising it at every new maximum scales 64 sums a lane in nearly every
+// tile of a prompt, and weights of up to 2^8 lose nothing in float32 or bf16.
+constexpr float kRaise = 8.0f;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -37,20 +47,23 @@ struct AttnArgs {
   uint32_t* out;      // the same
   int32_t heads, group;
   float scale;        // log2(e) times the score scale
-  float* part;        // [items][kRows][D] unnormalised sums
-  float2* ml;         // [items][kRows] running maximum and sum
-  int2* meta;         // [slots][kv_heads]: first item, chunks
-  int32_t items;
+  float* part;        // [items][rows of a tile][D] unnormalised sums
+  float2* ml;         // [items][rows of a tile] running maximum and sum
+  int2* meta;         // [slots][kv_heads]: first of a row block's records, chunks
+  int32_t items, tile_rows;
 };
 
-// Row tiles of a sequence: sequence i's start at slot row0 * G / 16 + i (its
-// ceil(n G / 16) tiles end before the next one's start).
+// Row blocks of a sequence: sequence i's start at slot row0 * G / 16 + i (its
+// ceil(n G / 16) blocks end before the next one's start).
 __device__ inline int row_slot(const AttnArgs& a, int i) {
   return (int)((int64_t)kv_row(a.b, i) * a.group / kRows) + i;
 }
 int64_t row_slots(int64_t n_new, int64_t n_seqs, int group) { return n_new * group / kRows + n_seqs; }
 
-__device__ inline int row_tiles(const AttnArgs& a, const KvSeq& s) { return (int)(((int64_t)s.n * a.group + kRows - 1) / kRows); }
+__device__ inline int row_blocks(const AttnArgs& a, const KvSeq& s) { return (int)(((int64_t)s.n * a.group + kRows - 1) / kRows); }
+// Tiles of `RB` blocks; a sequence with one block has a tile of one.
+template <int RB>
+__device__ inline int row_tiles(const AttnArgs& a, const KvSeq& s) { return (row_blocks(a, s) + RB - 1) / RB; }
 __device__ inline int kv_tiles(int len) { return (len + kKvTile - 1) / kKvTile; }
 
 __device__ inline int64_t wave_sum(int64_t v) {
@@ -61,27 +74,30 @@ __device__ inline int64_t wave_sum(int64_t v) {
 struct Item {
   int seq, tile, head, chunk;  // row tile and chunk of the sequence, key head
   int chunk_tiles;
+  int id;  // in the order of chunks
   KvSeq s;
 };
 
-// Chunks are as long as gives kTargetItems of them over all sequences, and
-// kMinChunk at least; every wave finds its block's item by itself.
+// Chunks are as long as gives kItems of them over all sequences, and
+// kMinChunk tiles at least; found by one wave.
+template <int RB>
 __device__ inline bool find_item(const AttnArgs& a, int id, Item& it) {
   const int lane = threadIdx.x & 63;
   int64_t work = 0;
   for (int i = lane; i < a.b.n_seqs; i += 64) {
     const KvSeq s = kv_seq(a.b, a.c, i);
-    work += (int64_t)kv_tiles(s.len) * row_tiles(a, s);
+    work += (int64_t)kv_tiles(s.len) * row_tiles<RB>(a, s);
   }
   work = wave_sum(work) * a.c.kv_heads;
-  const int ct = max(kMinChunk, (int)((work + kTargetItems - 1) / kTargetItems));
+  int ct = __builtin_amdgcn_readfirstlane(max(kMinChunk, (int)((work + kItems - 1) / kItems)));
+  auto items_of = [&](int i) {
+    if (i >= a.b.n_seqs) return 0;
+    const KvSeq s = kv_seq(a.b, a.c, i);
+    return max(1, (kv_tiles(s.len) + ct - 1) / ct) * row_tiles<RB>(a, s) * a.c.kv_heads;
+  };
   int base = 0;  // items of the sequences before
   for (int i0 = 0; i0 < a.b.n_seqs; i0 += 64) {
-    int items = 0;
-    if (i0 + lane < a.b.n_seqs) {
-      const KvSeq s = kv_seq(a.b, a.c, i0 + lane);
-      items = max(1, (kv_tiles(s.len) + ct - 1) / ct) * row_tiles(a, s) * a.c.kv_heads;
-    }
+    const int items = items_of(i0 + lane);
     int upto = items;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -92,15 +108,16 @@ __device__ inline bool find_item(const AttnArgs& a, int id, Item& it) {
     if (past != 0) {
       const int w = __builtin_ctzll(past);
       it.seq = __builtin_amdgcn_readfirstlane(i0 + w);
+      it.id = id;
       it.s = kv_seq(a.b, a.c, it.seq);
-      it.chunk_tiles = ct;
-      const int chunks = max(1, (kv_tiles(it.s.len) + ct - 1) / ct), rt = row_tiles(a, it.s);
+      const int chunks = max(1, (kv_tiles(it.s.len) + ct - 1) / ct), rt = row_tiles<RB>(a, it.s);
       const int local = id - base - __builtin_amdgcn_readfirstlane(__shfl(upto - items, w));
       // heads next to each other, then chunks, then row tiles, the last (longest) first
       const int hc = local / a.c.kv_heads, t = hc / chunks;
-      it.head = local - hc * a.c.kv_heads;
-      it.chunk = hc - t * chunks;
-      it.tile = rt - 1 - t;
+      it.head = __builtin_amdgcn_readfirstlane(local - hc * a.c.kv_heads);
+      it.chunk = __builtin_amdgcn_readfirstlane(hc - t * chunks);
+      it.tile = __builtin_amdgcn_readfirstlane(rt - 1 - t);
+      it.chunk_tiles = ct;
       return local >= 0 && it.tile >= 0;  // not so only for a cu_new that decreases
     }
     base += __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
@@ -242,155 +259,324 @@ __device__ inline uint32_t pack_bf16(float lo, float hi) {
 
 __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Sixteen rows, a chunk of positions over four waves.
+// Sums of the waves that hand theirs over: all for one row block, else two.
+template <int NB, int RB>
+constexpr int kLds = (RB > 1 ? 2 : kWaves) * 16 * RB * ((32 * NB + 4) * 4 + 8);
+
+// The queries of rows row0 .. row0 + 15 of a tile: operand B of S^T.
 template <int NB>
-__global__ __launch_bounds__(kThreads) void kv_attend_rows16_kernel(AttnArgs a) {
-  constexpr int D = 32 * NB, kStride = D + 4;
-  __shared__ float os[kWaves][kRows][kStride];
-  __shared__ float2 mls[kWaves][kRows];
-  Item it;
-  if (!find_item(a, blockIdx.x, it)) return;
+__device__ inline void load_q(const AttnArgs& a, const Item& it, int row0, bf16x8 (&q)[NB]) {
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  const int row = row0 + r, token = row / a.group, hq = it.head * a.group + (row - token * a.group);
+  const u32x4* at = reinterpret_cast<const u32x4*>(a.q + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
+  const bool real = row < it.s.n * a.group;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) q[b] = __builtin_bit_cast(bf16x8, real ? at[4 * b] : u32x4{0, 0, 0, 0});
+}
+
+// Scores past what the lane's row sees, in tiles from position t0 on.
+template <int H>
+__device__ inline void mask(f32x4 (&s)[H], int t0, int last) {
+  int from = t0 + 4 * ((threadIdx.x & 63) >> 4);
+  asm volatile("" : "+v"(from));  // keeps the comparisons out of the tiles that need none
+#pragma unroll
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (from + 16 * h + i > last) s[h][i] = -INFINITY;
+}
+
+// A row block's running softmax: what its weights are relative to (times the
+// scale, and as a score; -infinity until a finite score is seen), and the lane's
+// share of their sum.
+struct Softmax {
+  float ref = 0.0f, m = -INFINITY, l = 0.0f;
+};
+
+// Over the scores of H times 16 positions: raises the reference where they ask
+// for it (scaling l and o), adds to l and leaves the weights in p.
+template <int NB, int H>
+__device__ inline void weigh(const f32x4 (&s)[H], float scale, Softmax& x, f32x4 (&o)[2 * NB], float (&p)[4 * H]) {
+  float top = s[0][0];
+#pragma unroll
+  for (int i = 1; i < 4 * H; ++i) top = fmaxf(top, s[i / 4][i % 4]);
+  if (__any(top > x.m + kRaise / scale)) {
+    asm volatile("");
+    top = fmaxf(x.m, row_max(top));  // the row's own, in all of its lanes
+    const float f = top == -INFINITY ? 1.0f : exp2_of((x.m - top) * scale);
+    x.m = top;
+    x.ref = top == -INFINITY ? 0.0f : top * scale;
+    x.l *= f;
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) o[i] *= f;
+  }
+#pragma unroll
+  for (int i = 0; i < 4 * H; ++i) {
+    p[i] = exp2_of(__builtin_fmaf(s[i / 4][i % 4], scale, -x.ref));
+    x.l += p[i];
+  }
+}
+
+// p as the sum of two bf16 numbers each (2^-17 relative).
+__device__ inline void split_bf16(const float* p, bf16x8& ph, bf16x8& pl) {
+  u32x4 hi, lo;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    hi[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+    asm("" : "+v"(hi[i]));  // one conversion, its halves taken apart
+    lo[i] = pack_bf16(p[2 * i] - __uint_as_float(hi[i] << 16), p[2 * i + 1] - __uint_as_float(hi[i] & 0xFFFF0000u));
+  }
+  ph = __builtin_bit_cast(bf16x8, hi);
+  pl = __builtin_bit_cast(bf16x8, lo);
+}
+
+// A tile of 16 RB rows, a chunk of positions over four waves: each streams tiles
+// of its own.  A tile is converted once for its RB row blocks; the weights go
+// in as two bf16 parts, since what rounding them to one would leave is of the
+// size of the output's own rounding.
+template <int NB, int RB>
+__device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds) {
+  constexpr int D = 32 * NB, kStride = D + 4, kTileRows = kRows * RB;
+  auto os = reinterpret_cast<float(*)[kTileRows][kStride]>(lds);
+  auto mls = reinterpret_cast<float2(*)[kTileRows]>(lds + sizeof(float) * (RB > 1 ? 2 : kWaves) * kTileRows * kStride);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int r = lane & 15, g = lane >> 4;
-  const int rows = it.s.n * a.group, row = it.tile * kRows + r;
+  const int rows = it.s.n * a.group, row0 = it.tile * kTileRows;
   const int p0 = it.s.len - it.s.n;  // position of the first new token
-  const int token = row / a.group, hq = it.head * a.group + (row - token * a.group);
-  // what the row sees, and the least and most that any row of the tile sees
-  const int least = p0 + it.tile * kRows / a.group;
-  const int most = p0 + (min(it.tile * kRows + kRows, rows) - 1) / a.group;
-  const int last = min(p0 + token, most);  // rows past the end compute what nobody stores
+  // the least and the most that any row of the tile sees
+  const int least = p0 + row0 / a.group;
+  const int most = p0 + (min(row0 + kTileRows, rows) - 1) / a.group;
   const int tiles = kv_tiles(most + 1), chunks = max(1, (tiles + it.chunk_tiles - 1) / it.chunk_tiles);
-  if (it.chunk == 0 && threadIdx.x == 0)
-    a.meta[(int64_t)(row_slot(a, it.seq) + it.tile) * a.c.kv_heads + it.head] =
-        make_int2((int)blockIdx.x, chunks);
+  if (it.chunk == 0 && threadIdx.x < RB && row0 + kRows * (int)threadIdx.x < rows)
+    a.meta[(int64_t)(row_slot(a, it.seq) + it.tile * RB + threadIdx.x) * a.c.kv_heads + it.head] =
+        make_int2(it.id * kTileRows + kRows * (int)threadIdx.x, chunks);
   if (it.chunk >= chunks) return;
   const int t_end = min(tiles, (it.chunk + 1) * it.chunk_tiles);
-
-  bf16x8 q[NB];
-  {
-    const uint32_t* at = a.q + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB) + 4 * g;
+  int last[RB];  // what the lane's rows see; rows past the end compute what nobody stores
+  bf16x8 q[RB][NB];
+  f32x4 o[RB][2 * NB];
+  Softmax sm[RB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      u32x4 x = {0, 0, 0, 0};
-      if (row < rows) {
+  for (int y = 0; y < RB; ++y) {
+    last[y] = min(p0 + (row0 + kRows * y + r) / a.group, most);
+    load_q<NB>(a, it, row0 + kRows * y, q[y]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] = at[16 * b + k];
-      }
-      q[b] = __builtin_bit_cast(bf16x8, x);
-    }
+    for (int i = 0; i < 2 * NB; ++i) o[y][i] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  f32x4 o[2 * NB];
-#pragma unroll
-  for (int i = 0; i < 2 * NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.0f;  // the row's maximum (unscaled), the lane's share of its sum
 
-  auto tile_at = [&](int t) { return kv_tile(a.c, a.b, it.seq, t * kKvTile, it.head, KvTile(NB).bytes); };
-  TileRegs<NB> next;
-  int t = it.chunk * it.chunk_tiles + wave;
-  const uint8_t* at = t < t_end ? tile_at(t) : nullptr;
-  if (at) next.load(at);
-  for (; t < t_end; t += kWaves) {
-    TileRegs<NB> x = next;
-    const bool present = at != nullptr;
-    at = t + kWaves < t_end ? tile_at(t + kWaves) : nullptr;
-    if (at) next.load(at);
-    if (!present) continue;  // no such page: nothing to see there
-    f32x4 s[2];
+  // the wave's k-th tile: the pages of 64 at a time, one a lane
+  const int t_first = it.chunk * it.chunk_tiles + wave;
+  int ids = 0;
+  auto tile_at = [&](int k) -> const uint8_t* {
+    if (k % 64 == 0) {
+      const int t = t_first + kWaves * (k + lane);
+      ids = t < t_end ? kv_tile_index(a.c, a.b, it.seq, t, it.head) : -1;
+    }
+    const int id = __builtin_amdgcn_readlane(ids, k % 64);
+    return id < 0 ? nullptr : a.c.data + (int64_t)id * KvTile(NB).bytes;
+  };
+  auto step = [&](int t, TileRegs<NB>& x) {
+    f32x4 s[RB][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int b = 0; b < NB; ++b) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.key(b, h), q[b], s[h], 0, 0, 0);
-    }
-    const int t0 = t * kKvTile;
-    if (t0 + kKvTile - 1 > least) {
+      for (int y = 0; y < RB; ++y) s[y][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int b = 0; b < NB; ++b) {
+        const bf16x8 k = x.key(b, h);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (t0 + 16 * h + 4 * g + i > last) s[h][i] = -INFINITY;
-      if (t0 + kKvTile > it.s.len) x.end_at(it.s.len - t0);
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) top = fmaxf(top, s[i / 4][i % 4]);
-    top = fmaxf(m, row_max(top));
-    if (__any(top > m)) {
-      const float f = top == -INFINITY ? 1.0f : exp2_of((m - top) * a.scale);
-      m = top;
-      l *= f;
-#pragma unroll
-      for (int i = 0; i < 2 * NB; ++i) o[i] *= f;
-    }
-    const float ref = m == -INFINITY ? 0.0f : m * a.scale;
-    u32x4 hi, lo;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float p[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        p[e] = exp2_of(__builtin_fmaf(s[i / 2][2 * (i % 2) + e], a.scale, -ref));
-        l += p[e];
+        for (int y = 0; y < RB; ++y) s[y][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[y][b], s[y][h], 0, 0, 0);
       }
-      // the weight in two bf16 parts: what rounding it to one leaves is of the
-      // size of the output's own rounding
-      hi[i] = pack_bf16(p[0], p[1]);
-      lo[i] = pack_bf16(p[0] - __uint_as_float(hi[i] << 16), p[1] - __uint_as_float(hi[i] & 0xFFFF0000u));
     }
-    const bf16x8 ph = __builtin_bit_cast(bf16x8, hi), pl = __builtin_bit_cast(bf16x8, lo);
+    if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);  // the values' conversions would take registers from here on
+    const int t0 = t * kKvTile;
+    const bool edge = t0 + kKvTile - 1 > least;
+    if (edge && t0 + kKvTile > it.s.len) x.end_at(it.s.len - t0);
+    bf16x8 ph[RB], pl[RB];
+#pragma unroll
+    for (int y = 0; y < RB; ++y) {
+      if (edge) mask<2>(s[y], t0, last[y]);
+      float p[8];
+      weigh<NB, 2>(s[y], a.scale, sm[y], o[y], p);
+      split_bf16(p, ph[y], pl[y]);
+    }
+    if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       bf16x8 re, im;
       x.value(b, re, im);
-      o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(re, ph, o[2 * b], 0, 0, 0);
-      o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(im, ph, o[2 * b + 1], 0, 0, 0);
-      o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(re, pl, o[2 * b], 0, 0, 0);
-      o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(im, pl, o[2 * b + 1], 0, 0, 0);
+#pragma unroll
+      for (int y = 0; y < RB; ++y) {
+        o[y][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(re, ph[y], o[y][2 * b], 0, 0, 0);
+        o[y][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(im, ph[y], o[y][2 * b + 1], 0, 0, 0);
+      }
+#pragma unroll
+      for (int y = 0; y < RB; ++y) {
+        o[y][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(re, pl[y], o[y][2 * b], 0, 0, 0);
+        o[y][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(im, pl[y], o[y][2 * b + 1], 0, 0, 0);
+      }
+    }
+  };
+  {
+    // two sets of registers, one loaded while the other is used
+    TileRegs<NB> xa, xb;
+    int k = 0, t = t_first;
+    const uint8_t* at = tile_at(0);
+    if (at) xa.load(at);
+    while (t < t_end) {
+      const uint8_t* next = tile_at(k + 1);
+      if (next) xb.load(next);
+      if (at) step(t, xa);
+      t += kWaves;
+      if (t >= t_end) break;
+      at = tile_at(k + 2);
+      if (at) xa.load(at);
+      if (next) step(t, xb);
+      t += kWaves;
+      k += 2;
     }
   }
-  // join the waves
-  l = row_sum(l);
-  if (g == 0) mls[wave][r] = make_float2(m, l);
+  // Join the waves: one row block's through LDS by all threads, more by the
+  // upper two waves handing over to the lower two, and those to one.
 #pragma unroll
-  for (int b = 0; b < NB; ++b)
+  for (int y = 0; y < RB; ++y) sm[y].l = row_sum(sm[y].l);
+  auto put = [&](int w) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)  // entry 16 b + 4 g + i
-      *reinterpret_cast<float2*>(&os[wave][r][32 * b + 8 * g + 2 * i]) = make_float2(o[2 * b][i], o[2 * b + 1][i]);
-  __syncthreads();
-  for (int e = threadIdx.x; e < kRows * (D / 2); e += kThreads) {
-    const int rr = e / (D / 2), c = e - rr * (D / 2), w = it.tile * kRows + rr;
-    if (w >= rows) continue;
-    float top = mls[0][rr].x;
+    for (int y = 0; y < RB; ++y) {
+      if (g == 0) mls[w][kRows * y + r] = make_float2(sm[y].m, sm[y].l);
 #pragma unroll
-    for (int i = 1; i < kWaves; ++i) top = fmaxf(top, mls[i][rr].x);
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
-    float2 y = make_float2(0.0f, 0.0f);
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-      const float f = exp2_of((mls[i][rr].x - ref) * a.scale);
-      sum += f * mls[i][rr].y;
-      const float2 v = *reinterpret_cast<const float2*>(&os[i][rr][2 * c]);
-      y.x += f * v.x;
-      y.y += f * v.y;
+        for (int i = 0; i < 4; i += 2)  // entries 16 b + 4 g + i, + 1
+          *reinterpret_cast<float4*>(&os[w][kRows * y + r][32 * b + 8 * g + 2 * i]) =
+              make_float4(o[y][2 * b][i], o[y][2 * b + 1][i], o[y][2 * b][i + 1], o[y][2 * b + 1][i + 1]);
     }
-    if (chunks == 1) {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      const int tk = w / a.group, hh = it.head * a.group + (w - tk * a.group);
-      a.out[((int64_t)(it.s.row0 + tk) * a.heads + hh) * (D / 2) + c] = pack_bf16(y.x * inv, y.y * inv);
-    } else {
-      const int64_t rec = (int64_t)blockIdx.x * kRows + rr;
-      *reinterpret_cast<float2*>(a.part + rec * D + 2 * c) = y;
-      if (c == 0) a.ml[rec] = make_float2(top, sum);
+  };
+  if constexpr (RB > 1) {
+    auto add = [&](int w) {
+#pragma unroll
+      for (int y = 0; y < RB; ++y) {
+        const float2 ml = mls[w][kRows * y + r];
+        const float top = fmaxf(sm[y].m, ml.x), ref = top == -INFINITY ? 0.0f : top;
+        const float f = exp2_of((sm[y].m - ref) * a.scale), h = exp2_of((ml.x - ref) * a.scale);
+        sm[y].m = top;
+        sm[y].l = f * sm[y].l + h * ml.y;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const float4 v = *reinterpret_cast<const float4*>(&os[w][kRows * y + r][32 * b + 8 * g + 2 * i]);
+            o[y][2 * b][i] = f * o[y][2 * b][i] + h * v.x;
+            o[y][2 * b + 1][i] = f * o[y][2 * b + 1][i] + h * v.y;
+            o[y][2 * b][i + 1] = f * o[y][2 * b][i + 1] + h * v.z;
+            o[y][2 * b + 1][i + 1] = f * o[y][2 * b + 1][i + 1] + h * v.w;
+          }
+      }
+    };
+    if (wave >= 2) put(wave - 2);
+    __syncthreads();
+    if (wave < 2) add(wave);
+    __syncthreads();
+    if (wave == 1) put(0);
+    __syncthreads();
+    if (wave != 0) return;
+    add(0);
+#pragma unroll
+    for (int y = 0; y < RB; ++y) {
+      const int row = row0 + kRows * y + r, token = row / a.group, hq = it.head * a.group + (row - token * a.group);
+      if (row >= rows) continue;
+      if (chunks == 1) {
+        const float inv = sm[y].l == 0.0f ? 0.0f : 1.0f / sm[y].l;
+        u32x4* to = reinterpret_cast<u32x4*>(a.out + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          u32x4 v;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = pack_bf16(o[y][2 * b][i] * inv, o[y][2 * b + 1][i] * inv);
+          to[4 * b] = v;
+        }
+      } else {
+        const int64_t rec = (int64_t)it.id * kTileRows + (row - row0);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; i += 2)
+            *reinterpret_cast<float4*>(a.part + rec * D + 32 * b + 8 * g + 2 * i) =
+                make_float4(o[y][2 * b][i], o[y][2 * b + 1][i], o[y][2 * b][i + 1], o[y][2 * b + 1][i + 1]);
+        if (g == 0) a.ml[rec] = make_float2(sm[y].m, sm[y].l);
+      }
+    }
+  } else {
+    put(wave);
+    __syncthreads();
+    for (int e = threadIdx.x; e < kRows * (D / 2); e += kThreads) {
+      const int rr = e / (D / 2), c = e - rr * (D / 2), w = row0 + rr;
+      if (w >= rows) continue;
+      float top = mls[0][rr].x;
+#pragma unroll
+      for (int i = 1; i < kWaves; ++i) top = fmaxf(top, mls[i][rr].x);
+      const float ref = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f;
+      float2 y = make_float2(0.0f, 0.0f);
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        const float f = exp2_of((mls[i][rr].x - ref) * a.scale);
+        sum += f * mls[i][rr].y;
+        const float2 v = *reinterpret_cast<const float2*>(&os[i][rr][2 * c]);
+        y.x += f * v.x;
+        y.y += f * v.y;
+      }
+      if (chunks == 1) {
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const int tk = w / a.group, hh = it.head * a.group + (w - tk * a.group);
+        a.out[((int64_t)(it.s.row0 + tk) * a.heads + hh) * (D / 2) + c] = pack_bf16(y.x * inv, y.y * inv);
+      } else {
+        const int64_t rec = (int64_t)it.id * kTileRows + rr;
+        *reinterpret_cast<float2*>(a.part + rec * D + 2 * c) = y;
+        if (c == 0) a.ml[rec] = make_float2(top, sum);
+      }
     }
   }
 }
 
+template <int NB, int RB>
+__global__ __launch_bounds__(kThreads, RB > 1 ? 2 : 1) void kv_attend_kernel(AttnArgs a) {
+  __shared__ __align__(16) char lds[kLds<NB, RB>];
+  // one wave looks the item up for all
+  Item it;
+  int* found = reinterpret_cast<int*>(lds);
+  if (threadIdx.x < 64) {
+    const bool is = find_item<RB>(a, blockIdx.x, it);
+    if (threadIdx.x == 0) {
+      found[0] = is;
+      found[1] = it.seq;
+      found[2] = it.tile;
+      found[3] = it.head;
+      found[4] = it.chunk;
+      found[5] = it.chunk_tiles;
+    }
+  }
+  __syncthreads();
+  auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
+  if (!get(0)) return;
+  it.seq = get(1);
+  it.tile = get(2);
+  it.head = get(3);
+  it.chunk = get(4);
+  it.chunk_tiles = get(5);
+  it.id = blockIdx.x;
+  it.s = kv_seq(a.b, a.c, it.seq);
+  __syncthreads();  // the sums go where the item stands
+  attend_tile<NB, RB>(a, it, lds);
+}
+
+constexpr int kJoinThreads = 256;
+
 // Joins a row tile's chunks; blockIdx.y takes rows y, y + gridDim.y, ...
 template <int NB>
-__global__ __launch_bounds__(kThreads) void kv_attend_join_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a) {
   constexpr int D = 32 * NB, kPairs = D / 2, kLanes = kPairs <= 16 ? 16 : kPairs <= 32 ? 32 : kPairs <= 64 ? 64 : 128;
-  constexpr int kParts = kThreads / kLanes;
+  constexpr int kParts = kJoinThreads / kLanes;
   __shared__ float2 ys[kParts][kLanes];
   __shared__ float sums[kParts];
   const int slot = blockIdx.x / a.c.kv_heads, head = blockIdx.x - slot * a.c.kv_heads;
@@ -398,13 +584,14 @@ __global__ __launch_bounds__(kThreads) void kv_attend_join_kernel(AttnArgs a) {
   if (i < 0) return;
   const KvSeq s = kv_seq(a.b, a.c, i);
   const int tile = slot - row_slot(a, i);
-  if (tile < 0 || tile >= row_tiles(a, s)) return;
+  if (tile < 0 || tile >= row_blocks(a, s)) return;
   const int2 meta = a.meta[(int64_t)slot * a.c.kv_heads + head];
   const int chunks = meta.y;
   if (chunks < 2) return;
   // a chunk is kv_heads items after the one before; nothing else can stand
   // there unless cu_new decreases somewhere and no item wrote it
-  if (meta.x < 0 || meta.x >= a.items || (int64_t)meta.x + (int64_t)(chunks - 1) * a.c.kv_heads >= a.items) return;
+  const int64_t stride = (int64_t)a.c.kv_heads * a.tile_rows, records = (int64_t)a.items * a.tile_rows;
+  if (meta.x < 0 || meta.x + (int64_t)(chunks - 1) * stride + kRows > records) return;
   const int part = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
   const int rows = s.n * a.group;
   for (int rr = blockIdx.y; rr < kRows; rr += gridDim.y) {
@@ -412,14 +599,14 @@ __global__ __launch_bounds__(kThreads) void kv_attend_join_kernel(AttnArgs a) {
     if (w >= rows) break;
     float top = -INFINITY;
     for (int k = threadIdx.x & 63; k < chunks; k += 64)
-      top = fmaxf(top, a.ml[((int64_t)meta.x + (int64_t)k * a.c.kv_heads) * kRows + rr].x);
+      top = fmaxf(top, a.ml[meta.x + (int64_t)k * stride + rr].x);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
     const float ref = top == -INFINITY ? 0.0f : top;
     float sum = 0.0f;
     float2 y = make_float2(0.0f, 0.0f);
     for (int k = part; k < chunks; k += kParts) {
-      const int64_t rec = ((int64_t)meta.x + (int64_t)k * a.c.kv_heads) * kRows + rr;
+      const int64_t rec = meta.x + (int64_t)k * stride + rr;
       const float2 ml = a.ml[rec];
       const float f = exp2_of((ml.x - ref) * a.scale);
       sum += f * ml.y;
@@ -448,20 +635,24 @@ __global__ __launch_bounds__(kThreads) void kv_attend_join_kernel(AttnArgs a) {
 }
 
 struct Layout {
-  int64_t items, slots;
+  bool wide;
+  int64_t items, slots, tile_rows;
   size_t part, ml, meta, bytes;
 };
 
 Layout layout_of(const fairy2i_kv_cache* c, int64_t n_new, int64_t n_seqs, int32_t n_heads) {
   Layout l{};
   const int64_t G = n_heads / c->n_kv_heads;
+  // some sequence has more than a block of rows
+  l.wide = n_new * G > kRows * n_seqs;
+  l.tile_rows = l.wide ? kRows * wide_rb(c->dc / 16) : kRows;
   // a row tile more than its rows fill for each sequence that has any, and a
   // chunk more than its work fills for each row tile
-  l.items = kTargetItems + c->n_kv_heads * (n_new * G / kRows + (n_seqs < n_new ? n_seqs : n_new));
+  l.items = kItems + c->n_kv_heads * (n_new * G / l.tile_rows + (n_seqs < n_new ? n_seqs : n_new));
   l.slots = row_slots(n_new, n_seqs, (int)G);
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-  l.part = up((size_t)l.items * kRows * 2 * c->dc * sizeof(float));
-  l.ml = up((size_t)l.items * kRows * sizeof(float2));
+  l.part = up((size_t)l.items * l.tile_rows * 2 * c->dc * sizeof(float));
+  l.ml = up((size_t)l.items * l.tile_rows * sizeof(float2));
   l.meta = up((size_t)l.slots * c->n_kv_heads * sizeof(int2));
   l.bytes = l.part + l.ml + l.meta;
   return l;
@@ -469,11 +660,12 @@ Layout layout_of(const fairy2i_kv_cache* c, int64_t n_new, int64_t n_seqs, int32
 
 template <int NB>
 void launch(const AttnArgs& a, const Layout& l, bool one_chunk, hipStream_t s) {
-  hipLaunchKernelGGL(kv_attend_rows16_kernel<NB>, dim3((unsigned)l.items), dim3(kThreads), 0, s, a);
+  auto kernel = l.wide ? kv_attend_kernel<NB, wide_rb(NB)> : kv_attend_kernel<NB, 1>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)l.items), dim3(kThreads), 0, s, a);
   if (one_chunk) return;
   const int64_t blocks = l.slots * a.c.kv_heads;
   const unsigned split = blocks <= 512 ? kRows : blocks <= 2048 ? 4 : 1;
-  hipLaunchKernelGGL(kv_attend_join_kernel<NB>, dim3((unsigned)blocks, split), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(kv_attend_join_kernel<NB>, dim3((unsigned)blocks, split), dim3(kJoinThreads), 0, s, a);
 }
 
 bool valid_heads(const fairy2i_kv_cache* c, int32_t n_heads) {
@@ -501,11 +693,12 @@ fairy2i_status fairy2i_kv_attend(const fairy2i_kv_cache* cache, const fairy2i_kv
                                  void* stream) {
   if (const fairy2i_status s = kv_check(cache, batch)) return s;
   if (!q || !out) return FAIRY2I_ERR_NULL;
-  if (!valid_heads(cache, n_heads) || !(scale > 0.0f) || !(scale <= 1e30f)) return FAIRY2I_ERR_SHAPE;
+  if (!valid_heads(cache, n_heads) || !(scale >= 1e-30f) || !(scale <= 1e30f)) return FAIRY2I_ERR_SHAPE;
   const Layout l = layout_of(cache, batch->n_new, batch->n_seqs, n_heads);
   if (!workspace || workspace_bytes < l.bytes || (reinterpret_cast<uintptr_t>(workspace) & 15) != 0)
     return FAIRY2I_ERR_WORKSPACE;
-  if (l.items > INT32_MAX / 256 || l.slots * cache->n_kv_heads > INT32_MAX / 256) return FAIRY2I_ERR_UNSUPPORTED;
+  if (l.items > INT32_MAX / kThreads || l.items * l.tile_rows > INT32_MAX || l.slots * cache->n_kv_heads > INT32_MAX / kThreads)
+    return FAIRY2I_ERR_UNSUPPORTED;
   AttnArgs a{};
   a.c = kv_cache_of(cache);
   a.b = kv_batch_of(batch);
@@ -515,6 +708,7 @@ fairy2i_status fairy2i_kv_attend(const fairy2i_kv_cache* cache, const fairy2i_kv
   a.group = n_heads / cache->n_kv_heads;
   a.scale = scale * 1.44269504088896341f;
   a.items = (int32_t)l.items;
+  a.tile_rows = (int32_t)l.tile_rows;
   char* ws = static_cast<char*>(workspace);
   a.part = reinterpret_cast<float*>(ws);
   a.ml = reinterpret_cast<float2*>(ws + l.part);

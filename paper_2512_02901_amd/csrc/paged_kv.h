@@ -76,13 +76,18 @@ __device__ inline int kv_find(int n_seqs, int at, F start) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
+// Number of tile t (of a sequence's positions) of head h in the cache; -1 where
+// the table names no page.
+__device__ inline int kv_tile_index(const KvCache& c, const KvBatch& b, int i, int t, int h) {
+  const int tiles = c.page_size / kKvTile, page = t / tiles;
+  const int id = b.pages[(int64_t)i * b.max_pages + page];
+  return (uint32_t)id < (uint64_t)c.n_pages ? (id * c.kv_heads + h) * tiles + (t - page * tiles) : -1;
+}
+
 // Tile of position p of sequence i and head h; null where the table names no page.
 __device__ inline uint8_t* kv_tile(const KvCache& c, const KvBatch& b, int i, int p, int h, int bytes) {
-  const int page = p / c.page_size;
-  const int id = b.pages[(int64_t)i * b.max_pages + page];
-  if ((uint32_t)id >= (uint64_t)c.n_pages) return nullptr;
-  const int tiles = c.page_size / kKvTile;
-  return c.data + (((int64_t)id * c.kv_heads + h) * tiles + (p - page * c.page_size) / kKvTile) * bytes;
+  const int id = kv_tile_index(c, b, i, p / kKvTile, h);
+  return id < 0 ? nullptr : c.data + (int64_t)id * bytes;
 }
 
 #endif

@@ -282,11 +282,10 @@ using namespace fairy2i;
 extern "C" {
 
 size_t fairy2i_kv_cache_bytes(int64_t n_pages, int32_t page_size, int32_t n_kv_heads, int32_t dc) {
-  if (n_pages < 1 || n_pages > INT32_MAX || page_size < kKvTile || page_size > (1 << 20) || page_size % kKvTile != 0 ||
+  if (n_pages < 1 || n_pages > INT32_MAX || page_size < kKvTile || page_size > 65536 || page_size % kKvTile != 0 ||
       n_kv_heads < 1 || n_kv_heads > 65535 || dc < 16 || dc > kKvMaxDc || dc % 16 != 0)
     return 0;
-  const double bytes = (double)n_pages * n_kv_heads * (page_size / kKvTile) * KvTile(dc / 16).bytes;
-  if (bytes > 9e18) return 0;
+  if ((double)n_pages * n_kv_heads * (page_size / kKvTile) > INT32_MAX) return 0;  // tiles are numbered in 32 bits
   return (size_t)n_pages * (size_t)n_kv_heads * (size_t)(page_size / kKvTile) * (size_t)KvTile(dc / 16).bytes;
 }
 

@@ -15,6 +15,8 @@
 // several chunks, by a second kernel.
 #include <math.h>
 
+#include <type_traits>
+
 #include "paged_kv.h"
 
 namespace fairy2i {
@@ -27,8 +29,13 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 // Blocks of 16 rows in a row tile: one where no sequence can have more, else
 // as many as share a conversion.
 constexpr int wide_rb(int nb) { return nb <= 4 ? 2 : 1; }
-// What a call is cut into, where its rows alone are fewer.
-constexpr int kItems = 1024;
+// Blocks that are resident at once, which a call is cut into where its rows
+// alone are fewer: by the kernels' registers.  More items than that, and the
+// last ones run beside empty CUs: one token over 262144 positions, 32 heads on
+// 8 of dc = 64 (768 resident), us: 512 64, 768 64, 1024 72, 1536 74, 3072 94;
+// dc = 128 (512), 8 sequences up to 16384: 28, 35, 35, 36, 40.
+constexpr int resident(int nb, bool wide) { return kCus * (wide ? (nb <= 2 ? 3 : 2) : nb <= 2 ? 4 : nb <= 4 ? 3 : 2); }
+constexpr int kMaxItems = 4 * kCus;
 constexpr int kMinChunk = 8;      // tiles: two a wave
 
 // The running reference of a row's weights is raised once a score is 2^8 past
@@ -66,61 +73,90 @@ template <int RB>
 __device__ inline int row_tiles(const AttnArgs& a, const KvSeq& s) { return (row_blocks(a, s) + RB - 1) / RB; }
 __device__ inline int kv_tiles(int len) { return (len + kKvTile - 1) / kKvTile; }
 
-__device__ inline int64_t wave_sum(int64_t v) {
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+// Sum over the lanes below and this one, without a trip through LDS.
+template <typename T>
+__device__ inline T up_to(T v) {
+  auto add = [&](auto shift) {
+    constexpr int ctrl = decltype(shift)::value, rows = ctrl == 0x142 ? 0xA : ctrl == 0x143 ? 0xC : 0xF;
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xF, false);
+    if constexpr (sizeof(T) == 8) {
+      const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), ctrl, rows, 0xF, false);
+      v += (T)((uint64_t)hi << 32 | lo);
+    } else {
+      v += (T)lo;
+    }
+  };
+  add(std::integral_constant<int, 0x111>{});  // one lane up in rows of 16, two, four, eight
+  add(std::integral_constant<int, 0x112>{});
+  add(std::integral_constant<int, 0x114>{});
+  add(std::integral_constant<int, 0x118>{});
+  add(std::integral_constant<int, 0x142>{});  // row 0's last to row 1, 2's to 3
+  add(std::integral_constant<int, 0x143>{});  // row 1's last to rows 2 and 3
   return v;
+}
+
+__device__ inline int of_lane(int v, int i) { return __builtin_amdgcn_readlane(v, i); }
+__device__ inline int64_t of_lane(int64_t v, int i) {
+  const uint32_t lo = of_lane((int)v, i), hi = of_lane((int)(v >> 32), i);
+  return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
 struct Item {
   int seq, tile, head, chunk;  // row tile and chunk of the sequence, key head
   int chunk_tiles;
-  int id;  // in the order of chunks
+  int id;  // where its sums go, if the chunk is one of several
   KvSeq s;
 };
 
-// Chunks are as long as gives kItems of them over all sequences, and
-// kMinChunk tiles at least; found by one wave.
+// Chunks are as long as makes `target` of them over all sequences, and
+// kMinChunk tiles at least.  Whole chunks go first, what is left of the
+// sequences after them, so that the short ones fill the gaps; of a sequence's,
+// the last row tiles (which see most) go first and heads are neighbours.
 template <int RB>
-__device__ inline bool find_item(const AttnArgs& a, int id, Item& it) {
-  const int lane = threadIdx.x & 63;
-  int64_t work = 0;
-  for (int i = lane; i < a.b.n_seqs; i += 64) {
-    const KvSeq s = kv_seq(a.b, a.c, i);
+__device__ inline bool find_item(const AttnArgs& a, int at, int target, Item& it) {
+  const int lane = threadIdx.x & 63, n = a.b.n_seqs, kv = a.c.kv_heads;
+  auto seq = [&](int i) { return i < n ? kv_seq(a.b, a.c, i) : KvSeq{0, 0, 0}; };
+  const KvSeq first = seq(lane);
+  int64_t work = (int64_t)kv_tiles(first.len) * row_tiles<RB>(a, first);
+  for (int i = 64 + lane; i < n; i += 64) {
+    const KvSeq s = seq(i);
     work += (int64_t)kv_tiles(s.len) * row_tiles<RB>(a, s);
   }
-  work = wave_sum(work) * a.c.kv_heads;
-  int ct = __builtin_amdgcn_readfirstlane(max(kMinChunk, (int)((work + kItems - 1) / kItems)));
-  auto items_of = [&](int i) {
-    if (i >= a.b.n_seqs) return 0;
-    const KvSeq s = kv_seq(a.b, a.c, i);
-    return max(1, (kv_tiles(s.len) + ct - 1) / ct) * row_tiles<RB>(a, s) * a.c.kv_heads;
-  };
-  int base = 0;  // items of the sequences before
-  for (int i0 = 0; i0 < a.b.n_seqs; i0 += 64) {
-    const int items = items_of(i0 + lane);
-    int upto = items;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int v = __shfl_up(upto, off);
-      if (lane >= off) upto += v;
-    }
-    const uint64_t past = __ballot(base + upto > id);
+  // of one sequence, its lane's number; of more, the last lane's sum
+  auto total = [&](auto v) { return n > 1 ? of_lane(up_to(v), 63) : of_lane(v, 0); };
+  work = total(work);
+  const int ct = max(kMinChunk, (int)((work * kv + target - 1) / target));
+  // items of a sequence's whole chunks, and all of them (one, if it is empty)
+  auto whole_of = [&](const KvSeq& s) { return kv_tiles(s.len) / ct * row_tiles<RB>(a, s) * kv; };
+  auto all_of = [&](const KvSeq& s) { return max(1, (kv_tiles(s.len) + ct - 1) / ct) * row_tiles<RB>(a, s) * kv; };
+  int whole = whole_of(first);
+  for (int i = 64 + lane; i < n; i += 64) whole += whole_of(seq(i));
+  whole = total(whole);
+  const bool rest = at >= whole;
+  if (rest) at -= whole;
+  int before = 0, ids = 0;  // items of the sequences before: of this kind, and all
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const KvSeq s = i0 == 0 ? first : seq(i0 + lane);
+    const int all = all_of(s), mine = rest ? all - whole_of(s) : whole_of(s);
+    const int upto = n > 1 ? up_to(mine) : mine, ids_upto = n > 1 ? up_to(all) : all;
+    const uint64_t past = __ballot(before + upto > at);
     if (past != 0) {
       const int w = __builtin_ctzll(past);
-      it.seq = __builtin_amdgcn_readfirstlane(i0 + w);
-      it.id = id;
-      it.s = kv_seq(a.b, a.c, it.seq);
-      const int chunks = max(1, (kv_tiles(it.s.len) + ct - 1) / ct), rt = row_tiles<RB>(a, it.s);
-      const int local = id - base - __builtin_amdgcn_readfirstlane(__shfl(upto - items, w));
-      // heads next to each other, then chunks, then row tiles, the last (longest) first
-      const int hc = local / a.c.kv_heads, t = hc / chunks;
-      it.head = __builtin_amdgcn_readfirstlane(local - hc * a.c.kv_heads);
-      it.chunk = __builtin_amdgcn_readfirstlane(hc - t * chunks);
-      it.tile = __builtin_amdgcn_readfirstlane(rt - 1 - t);
+      auto of = [&](int v) { return of_lane(v, w); };
+      const int local = at - before - of(upto - mine), rt = of(row_tiles<RB>(a, s)), chunks = of(kv_tiles(s.len)) / ct;
+      const int per = rest ? 1 : chunks;  // chunks of this kind that a row tile has
+      const int hc = local / kv, t = hc / max(per, 1);
+      it.seq = i0 + w;
+      it.s = {of(s.row0), of(s.n), of(s.len)};
+      it.head = local - hc * kv;
+      it.chunk = rest ? chunks : hc - t * per;
+      it.tile = rt - 1 - t;
       it.chunk_tiles = ct;
-      return local >= 0 && it.tile >= 0;  // not so only for a cu_new that decreases
+      it.id = ids + of(ids_upto - all) + (t * (of(all) / max(rt * kv, 1)) + it.chunk) * kv + it.head;
+      return local >= 0 && it.tile >= 0 && it.id < a.items;  // not so only for a cu_new that decreases
     }
-    base += __builtin_amdgcn_readfirstlane(__shfl(upto, 63));
+    before += __builtin_amdgcn_readlane(upto, 63);
+    ids += __builtin_amdgcn_readlane(ids_upto, 63);
   }
   return false;
 }
@@ -542,94 +578,154 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
 template <int NB, int RB>
 __global__ __launch_bounds__(kThreads, RB > 1 ? 2 : 1) void kv_attend_kernel(AttnArgs a) {
   __shared__ __align__(16) char lds[kLds<NB, RB>];
+  static_assert(sizeof(Item) <= kLds<NB, RB>);
   // one wave looks the item up for all
-  Item it;
-  int* found = reinterpret_cast<int*>(lds);
+  Item it{};
+  Item* found = reinterpret_cast<Item*>(lds);
   if (threadIdx.x < 64) {
-    const bool is = find_item<RB>(a, blockIdx.x, it);
-    if (threadIdx.x == 0) {
-      found[0] = is;
-      found[1] = it.seq;
-      found[2] = it.tile;
-      found[3] = it.head;
-      found[4] = it.chunk;
-      found[5] = it.chunk_tiles;
-    }
+    if (!find_item<RB>(a, blockIdx.x, resident(NB, RB > 1), it)) it.seq = -1;
+    if (threadIdx.x == 0) *found = it;
   }
   __syncthreads();
-  auto get = [&](int i) { return __builtin_amdgcn_readfirstlane(found[i]); };
-  if (!get(0)) return;
-  it.seq = get(1);
-  it.tile = get(2);
-  it.head = get(3);
-  it.chunk = get(4);
-  it.chunk_tiles = get(5);
-  it.id = blockIdx.x;
-  it.s = kv_seq(a.b, a.c, it.seq);
+  it = *found;
+  int* word = reinterpret_cast<int*>(&it);
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(Item) / 4); ++i) word[i] = __builtin_amdgcn_readfirstlane(word[i]);
+  if (it.seq < 0) return;
   __syncthreads();  // the sums go where the item stands
   attend_tile<NB, RB>(a, it, lds);
 }
 
 constexpr int kJoinThreads = 256;
 
-// Joins a row tile's chunks; blockIdx.y takes rows y, y + gridDim.y, ...
+// Joins a row block's chunks.  What bounds it is a chain of loads (of the
+// sequences, of the chunks' maxima and sums), so the first sums are asked for
+// before their weights are known, eight a lane at a time.  Up to 64 chunks: a
+// wave a row; more: a block a row.  blockIdx.y: which rows, of 16.
 template <int NB>
 __global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a) {
-  constexpr int D = 32 * NB, kPairs = D / 2, kLanes = kPairs <= 16 ? 16 : kPairs <= 32 ? 32 : kPairs <= 64 ? 64 : 128;
-  constexpr int kParts = kJoinThreads / kLanes;
-  __shared__ float2 ys[kParts][kLanes];
-  __shared__ float sums[kParts];
+  constexpr int D = 32 * NB, kQuads = D / 4, kLanes = kQuads <= 8 ? 8 : kQuads <= 16 ? 16 : kQuads <= 32 ? 32 : 64;
+  constexpr int kAhead = 8, kWavesJ = kJoinThreads / 64;
+  __shared__ float weight[kMaxItems + 1];
+  __shared__ float4 ys[kJoinThreads];
+  __shared__ float tops[kWavesJ], sums[kWavesJ];
   const int slot = blockIdx.x / a.c.kv_heads, head = blockIdx.x - slot * a.c.kv_heads;
+  const int2 meta = a.meta[(int64_t)slot * a.c.kv_heads + head];
   const int i = kv_find(a.b.n_seqs, slot, [&](int s) { return row_slot(a, s); });
   if (i < 0) return;
-  const KvSeq s = kv_seq(a.b, a.c, i);
-  const int tile = slot - row_slot(a, i);
-  if (tile < 0 || tile >= row_blocks(a, s)) return;
-  const int2 meta = a.meta[(int64_t)slot * a.c.kv_heads + head];
+  const int row0 = kv_row(a.b, i), rows = max(kv_row(a.b, i + 1) - row0, 0) * a.group;
+  const int block = slot - row_slot(a, i);
+  if (block < 0 || block * kRows >= rows) return;
   const int chunks = meta.y;
   if (chunks < 2) return;
   // a chunk is kv_heads items after the one before; nothing else can stand
   // there unless cu_new decreases somewhere and no item wrote it
   const int64_t stride = (int64_t)a.c.kv_heads * a.tile_rows, records = (int64_t)a.items * a.tile_rows;
-  if (meta.x < 0 || meta.x + (int64_t)(chunks - 1) * stride + kRows > records) return;
-  const int part = threadIdx.x / kLanes, c = threadIdx.x % kLanes;
-  const int rows = s.n * a.group;
-  for (int rr = blockIdx.y; rr < kRows; rr += gridDim.y) {
-    const int w = tile * kRows + rr;
+  if (chunks > kMaxItems + 1 || meta.x < 0 || meta.x + (int64_t)(chunks - 1) * stride + kRows > records) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  // threads of a row: of a wave, or of the block
+  const bool few = chunks <= 64;
+  const int mine = few ? lane : tid, parts = (few ? 64 : kJoinThreads) / kLanes, part = mine / kLanes, c = mine % kLanes;
+  const int step = gridDim.y * (few ? kWavesJ : 1);
+  for (int rr = few ? blockIdx.y * kWavesJ + wave : blockIdx.y; rr < kRows; rr += step) {
+    const int w = block * kRows + rr;
     if (w >= rows) break;
-    float top = -INFINITY;
-    for (int k = threadIdx.x & 63; k < chunks; k += 64)
-      top = fmaxf(top, a.ml[meta.x + (int64_t)k * stride + rr].x);
+    auto record = [&](int k) { return meta.x + (int64_t)k * stride + rr; };
+    float4 v[kAhead];
+    auto ask = [&](int k0) {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
-    float2 y = make_float2(0.0f, 0.0f);
-    for (int k = part; k < chunks; k += kParts) {
-      const int64_t rec = meta.x + (int64_t)k * stride + rr;
-      const float2 ml = a.ml[rec];
-      const float f = exp2_of((ml.x - ref) * a.scale);
-      sum += f * ml.y;
-      if (c < kPairs) {
-        const float2 v = *reinterpret_cast<const float2*>(a.part + rec * D + 2 * c);
-        y.x += f * v.x;
-        y.y += f * v.y;
+      for (int j = 0; j < kAhead; ++j) {
+        const int k = k0 + j * parts;
+        v[j] = k < chunks && c < kQuads ? *reinterpret_cast<const float4*>(a.part + record(k) * D + 4 * c)
+                                        : make_float4(0.f, 0.f, 0.f, 0.f);
       }
+    };
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](int j, float f) {
+      y.x += f * v[j].x;
+      y.y += f * v[j].y;
+      y.z += f * v[j].z;
+      y.w += f * v[j].w;
+    };
+    float top = -INFINITY, sum = 0.0f;
+    ask(part);
+    if (few) {
+      const float2 ml = lane < chunks ? a.ml[record(lane)] : make_float2(-INFINITY, 0.0f);
+      top = ml.x;
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+      const float f = exp2_of((ml.x - (top == -INFINITY ? 0.0f : top)) * a.scale);
+      sum = f * ml.y;
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+      for (int k0 = part; k0 - part < chunks; k0 += kAhead * parts) {
+        if (k0 != part) ask(k0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int k = k0 + j * parts;
+          const float g = __shfl(f, k & 63);
+          add(j, k < chunks ? g : 0.0f);
+        }
+      }
+#pragma unroll
+      for (int off = kLanes; off < 64; off <<= 1) {
+        y.x += __shfl_xor(y.x, off);
+        y.y += __shfl_xor(y.y, off);
+        y.z += __shfl_xor(y.z, off);
+        y.w += __shfl_xor(y.w, off);
+      }
+    } else {
+      for (int k = tid; k < chunks; k += kJoinThreads) {
+        const float m = a.ml[record(k)].x;
+        weight[k] = m;
+        top = fmaxf(top, m);
+      }
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
+      if (lane == 0) tops[wave] = top;
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kWavesJ; ++j) top = fmaxf(top, tops[j]);
+      const float ref = top == -INFINITY ? 0.0f : top;
+      for (int k = tid; k < chunks; k += kJoinThreads) {
+        const float f = exp2_of((weight[k] - ref) * a.scale);
+        weight[k] = f;
+        sum += f * a.ml[record(k)].y;
+      }
+#pragma unroll
+      for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+      if (lane == 0) sums[wave] = sum;
+      __syncthreads();
+      for (int k0 = part; k0 < chunks; k0 += kAhead * parts) {
+        if (k0 != part) ask(k0);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+          const int k = k0 + j * parts;
+          add(j, k < chunks ? weight[k] : 0.0f);
+        }
+      }
+      ys[tid] = y;
+      __syncthreads();
+      if (part == 0) {
+#pragma unroll
+        for (int k = 1; k < kJoinThreads / kLanes; ++k) {
+          const float4 u = ys[k * kLanes + c];
+          y.x += u.x;
+          y.y += u.y;
+          y.z += u.z;
+          y.w += u.w;
+        }
+        sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kWavesJ; ++j) sum += sums[j];
+      }
+      __syncthreads();  // the next row's writers
     }
-    __syncthreads();  // the last row's readers
-    ys[part][c] = y;
-    if (c == 0) sums[part] = sum;
-    __syncthreads();
-    if (part == 0 && c < kPairs) {
-#pragma unroll
-      for (int k = 1; k < kParts; ++k) {
-        sum += sums[k];
-        y.x += ys[k][c].x;
-        y.y += ys[k][c].y;
-      }
+    if (part == 0 && c < kQuads) {
       const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
       const int tk = w / a.group, hh = head * a.group + (w - tk * a.group);
-      a.out[((int64_t)(s.row0 + tk) * a.heads + hh) * kPairs + c] = pack_bf16(y.x * inv, y.y * inv);
+      *reinterpret_cast<uint2*>(a.out + ((int64_t)(row0 + tk) * a.heads + hh) * (D / 2) + 2 * c) =
+          make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
     }
   }
 }
@@ -648,7 +744,7 @@ Layout layout_of(const fairy2i_kv_cache* c, int64_t n_new, int64_t n_seqs, int32
   l.tile_rows = l.wide ? kRows * wide_rb(c->dc / 16) : kRows;
   // a row tile more than its rows fill for each sequence that has any, and a
   // chunk more than its work fills for each row tile
-  l.items = kItems + c->n_kv_heads * (n_new * G / l.tile_rows + (n_seqs < n_new ? n_seqs : n_new));
+  l.items = resident((int)c->dc / 16, l.tile_rows > kRows) + c->n_kv_heads * (n_new * G / l.tile_rows + (n_seqs < n_new ? n_seqs : n_new));
   l.slots = row_slots(n_new, n_seqs, (int)G);
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
   l.part = up((size_t)l.items * l.tile_rows * 2 * c->dc * sizeof(float));

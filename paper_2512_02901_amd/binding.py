@@ -938,37 +938,55 @@ def add_rmsnorm_i8(x, gain, delta=None, eps=1e-5, h_out=None, out=None):
     (q, x_scale) to write."""
     torch = _torch_module or _torch()
     lib = _lib or load()
-    _require(x, torch.complex64, "x")
-    if x.dim() != 2:
-        raise ValueError("x must be [B, n]")
-    B, n = x.shape
-    dev = x.device
-    _require(gain, torch.float32, "gain", dev)
-    if gain.shape != (2 * n,):
-        raise ValueError(f"gain must have shape ({2 * n},), got {tuple(gain.shape)}")
-    if delta is not None:
-        _require(delta, torch.complex64, "delta", dev)
-        if delta.shape != x.shape:
-            raise ValueError("delta must have x's shape")
-        if h_out is None:
-            h_out = torch.empty_like(x)
+    # launch latency counts: everything is looked over in one expression, _check_norm names what is wrong
+    try:
+        index = x.get_device()
+        ok = (index >= 0 and x.dtype is torch.complex64 and x.is_contiguous() and not x.is_conj()
+              and gain.dtype is torch.float32 and gain.get_device() == index and gain.is_contiguous()
+              and (delta is None or (delta.dtype is torch.complex64 and delta.get_device() == index
+                                     and delta.is_contiguous() and not delta.is_conj() and delta.shape == x.shape)))
+        B, n = x.shape
+        ok = ok and gain.shape == (2 * n,)
+    except (AttributeError, TypeError, ValueError):
+        ok = False
+    if not ok:
+        _check_norm(x, gain, delta)
     if h_out is not None:
-        _require(h_out, torch.complex64, "h_out", dev)
-        if h_out.shape != x.shape:
-            raise ValueError("h_out must have x's shape")
+        _require(h_out, torch.complex64, "h_out", x.device)
+        if h_out.shape != x.shape or h_out.is_conj():
+            raise ValueError("h_out must have x's shape, and not be a conjugated view")
+    elif delta is not None:
+        h_out = torch.empty_like(x)
     if out is None:
-        q = torch.empty((B, n, 2), dtype=torch.int8, device=dev)
-        scale = torch.empty((B,), dtype=torch.float32, device=dev)
+        q = torch.empty((B, n, 2), dtype=torch.int8, device=x.device)
+        scale = torch.empty(B, dtype=torch.float32, device=x.device)
     else:
         q, scale = out
-        _require(q, torch.int8, "out[0]", dev)
-        _require(scale, torch.float32, "out[1]", dev)
+        _require(q, torch.int8, "out[0]", x.device)
+        _require(scale, torch.float32, "out[1]", x.device)
         if q.shape != (B, n, 2) or scale.shape != (B,):
             raise ValueError("out must be (int8 [B, n, 2], float32 [B])")
     _check(lib.fairy2i_add_rmsnorm_i8(x.data_ptr(), None if delta is None else delta.data_ptr(), gain.data_ptr(), eps,
                                       B, n, None if h_out is None else h_out.data_ptr(), q.data_ptr(),
-                                      scale.data_ptr(), _raw_stream(x.get_device())), "fairy2i_add_rmsnorm_i8")
+                                      scale.data_ptr(), _raw_stream(index)), "fairy2i_add_rmsnorm_i8")
     return x if h_out is None else h_out, q, scale
+
+
+def _check_norm(x, gain, delta):
+    torch = _torch()
+    _require(x, torch.complex64, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [B, n]")
+    _require(gain, torch.float32, "gain", x.device)
+    if gain.shape != (2 * x.shape[1],):
+        raise ValueError(f"gain must have shape ({2 * x.shape[1]},), got {tuple(gain.shape)}")
+    if delta is not None:
+        _require(delta, torch.complex64, "delta", x.device)
+        if delta.shape != x.shape:
+            raise ValueError("delta must have x's shape")
+    for t, name in ((x, "x"), (delta, "delta")):
+        if t is not None and t.is_conj():
+            raise ValueError(f"{name} is a conjugated view: resolve_conj() it first")
 
 
 def rope_table(n_pos, dc, base=10000.0, device="cuda"):
@@ -1010,6 +1028,7 @@ class PagedKv:
         if data.numel() < need:
             raise ValueError(f"data must hold {need} bytes, got {data.numel()}")
         self.data = data
+        self._index = data.get_device()
         self.n_pages, self.page_size, self.n_kv_heads, self.dc = n_pages, page_size, n_kv_heads, dc
         self._desc = KvCacheDesc(data.data_ptr(), n_pages, page_size, n_kv_heads, dc, 0)
         self._ref = ctypes.byref(self._desc)
@@ -1025,19 +1044,27 @@ class PagedKv:
 
     def _batch(self, pages, cu_new, lens, n_new):
         torch = _torch_module
-        dev = self.data.device
+        index = self._index
+        int32 = torch.int32
+        try:
+            n_seqs, max_pages = pages.shape
+            if (pages.dtype is int32 and pages.get_device() == index and pages.is_contiguous()
+                    and cu_new.dtype is int32 and cu_new.get_device() == index and cu_new.is_contiguous()
+                    and lens.dtype is int32 and lens.get_device() == index and lens.is_contiguous()
+                    and lens.shape == (n_seqs,) and cu_new.shape == (n_seqs + 1,)):
+                return KvBatchDesc(pages.data_ptr(), cu_new.data_ptr(), lens.data_ptr(), n_new, n_seqs, max_pages)
+        except (AttributeError, TypeError, ValueError):
+            pass
         for t, name in ((pages, "pages"), (cu_new, "cu_new"), (lens, "lens")):
-            _require(t, torch.int32, name, dev)
-        if pages.dim() != 2 or lens.shape != (pages.shape[0],) or cu_new.shape != (pages.shape[0] + 1,):
-            raise ValueError("pages must be [n_seqs, max_pages], cu_new [n_seqs + 1] and lens [n_seqs]")
-        return KvBatchDesc(pages.data_ptr(), cu_new.data_ptr(), lens.data_ptr(), n_new, *pages.shape)
+            _require(t, int32, name, self.data.device)
+        raise ValueError("pages must be [n_seqs, max_pages], cu_new [n_seqs + 1] and lens [n_seqs]")
 
     def _rows(self, x, heads, name):
         """(rows, heads, row stride) of complex64 [N, heads * dc] or [N, heads, dc] whose rows are whole."""
         torch = _torch_module
         if not isinstance(x, torch.Tensor):
             raise TypeError(f"{name} must be a torch.Tensor")
-        if x.device != self.data.device:
+        if x.get_device() != self._index:
             raise ValueError(f"{name} is on {x.device}, expected {self.data.device}")
         if x.dtype is not torch.complex64:
             raise TypeError(f"{name} must be {torch.complex64}, got {x.dtype}")
@@ -1045,8 +1072,8 @@ class PagedKv:
             raise ValueError(f"{name} is a conjugated view: resolve_conj() it first")
         dc, shape, stride = self.dc, x.shape, x.stride()
         if len(shape) == 3:
-            whole = shape[2] == dc and stride[2] == 1 and (shape[1] == 1 or stride[1] == dc)
             n = shape[1]
+            whole = shape[2] == dc and stride[2] == 1 and (n == 1 or stride[1] == dc)
         else:
             whole = len(shape) == 2 and shape[1] % dc == 0 and stride[1] == 1
             n = shape[1] // dc if whole else 0
@@ -1071,28 +1098,27 @@ class PagedKv:
         N, _, k_ld = self._rows(k, self.n_kv_heads, "k")
         Nv, _, v_ld = self._rows(v, self.n_kv_heads, "v")
         heads = q_ld = 0
-        dev = self.data.device
         if q is not None:
             Nq, heads, q_ld = self._rows(q, None, "q")
             if Nq != N:
                 raise ValueError("q, k and v must have as many rows")
             if q_out is None:
-                q_out = torch.empty((N, heads, self.dc, 2), dtype=torch.bfloat16, device=dev)
+                q_out = torch.empty((N, heads, self.dc, 2), dtype=torch.bfloat16, device=k.device)
             else:
-                _require(q_out, torch.bfloat16, "q_out", dev)
+                _require(q_out, torch.bfloat16, "q_out", k.device)
                 if q_out.shape != (N, heads, self.dc, 2):
                     raise ValueError(f"q_out must have shape {(N, heads, self.dc, 2)}")
         elif q_out is not None:
             raise ValueError("q_out without q")
         if Nv != N:
             raise ValueError("q, k and v must have as many rows")
-        _require(rope, torch.float32, "rope", dev)
+        _require(rope, torch.float32, "rope", k.device)
         if rope.dim() != 3 or rope.shape[1:] != (self.dc, 2):
             raise ValueError(f"rope must be [positions, {self.dc}, 2]")
         batch = self._batch(pages, cu_new, lens, N)
         _check(lib.fairy2i_kv_append(self._ref, ctypes.byref(batch), None if q is None else q.data_ptr(), q_ld, heads,
                                      k.data_ptr(), k_ld, v.data_ptr(), v_ld, rope.data_ptr(), rope.shape[0],
-                                     None if q is None else q_out.data_ptr(), _raw_stream(dev.index)),
+                                     None if q is None else q_out.data_ptr(), _raw_stream(self._index)),
                "fairy2i_kv_append")
         return q_out
 
@@ -1107,13 +1133,14 @@ class PagedKv:
         if out is None:
             out = (torch.empty(shape, dtype=torch.bfloat16, device=dev),
                    torch.empty(shape, dtype=torch.bfloat16, device=dev))
-        for t in out:
-            _require(t, torch.bfloat16, "out", dev)
-            if t.shape != shape:
-                raise ValueError(f"out must be a pair of shape {shape}")
+        else:
+            for t in out:
+                _require(t, torch.bfloat16, "out", dev)
+                if t.shape != shape:
+                    raise ValueError(f"out must be a pair of shape {shape}")
         batch = self._batch(pages, cu_new, lens, n_new)
         _check(lib.fairy2i_kv_read(self._ref, ctypes.byref(batch), out[0].data_ptr(), out[1].data_ptr(),
-                                   _raw_stream(dev.index)), "fairy2i_kv_read")
+                                   _raw_stream(self._index)), "fairy2i_kv_read")
         return tuple(out)
 
     def attend_workspace_bytes(self, n_new, n_seqs, heads) -> int:
@@ -1131,27 +1158,32 @@ class PagedKv:
         takes."""
         torch = _torch_module or _torch()
         lib = _lib or load()
-        dev = self.data.device
-        _require(q, torch.bfloat16, "q", dev)
-        if q.dim() != 4 or q.shape[2:] != (self.dc, 2):
+        index = self._index
+        try:
+            ok = q.dtype is torch.bfloat16 and q.get_device() == index and q.is_contiguous()
+            N, heads, dc, two = q.shape
+            ok = ok and dc == self.dc and two == 2
+        except (AttributeError, ValueError):
+            ok = False
+        if not ok:
+            _require(q, torch.bfloat16, "q", self.data.device)
             raise ValueError(f"q must be [N, heads, {self.dc}, 2]")
-        N, heads = q.shape[:2]
         if heads == 0 or heads % self.n_kv_heads != 0:
             raise ValueError(f"q's heads must be a multiple of {self.n_kv_heads}")
         if out is None:
             out = torch.empty_like(q)
         else:
-            _require(out, torch.bfloat16, "out", dev)
+            _require(out, torch.bfloat16, "out", q.device)
             if out.shape != q.shape:
                 raise ValueError("out must have q's shape")
         batch = self._batch(pages, cu_new, lens, N)
         if workspace is None:
             need = lib.fairy2i_kv_attend_workspace_bytes(self._ref, N, pages.shape[0], heads)
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
         else:  # its size is the library's to check
-            _require(workspace, torch.uint8, "workspace", dev)
+            _require(workspace, torch.uint8, "workspace", q.device)
         _check(lib.fairy2i_kv_attend(self._ref, ctypes.byref(batch), q.data_ptr(), heads,
                                      (2 * self.dc) ** -0.5 if scale is None else scale, out.data_ptr(),
-                                     workspace.data_ptr(), workspace.numel(), _raw_stream(dev.index)),
+                                     workspace.data_ptr(), workspace.numel(), _raw_stream(index)),
                "fairy2i_kv_attend")
         return out

@@ -7,6 +7,8 @@
 // transposed within four lanes), and no two waves share a byte.
 #include <math.h>
 
+#include <type_traits>
+
 #include "paged_kv.h"
 
 namespace fairy2i {
@@ -38,10 +40,12 @@ __device__ inline float2 turn(float2 v, float2 cs) {
   return make_float2(v.x * cs.x - v.y * cs.y, v.x * cs.y + v.y * cs.x);
 }
 
-__device__ inline uint32_t bf16_of(float v) {  // nearest even; a NaN stays one
-  const uint32_t u = __float_as_uint(v);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (u >> 16) | 0x40u;
-  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
+__device__ inline uint32_t bf16_pair(float2 v) {  // nearest even
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  bf16x2 p;
+  p[0] = (__bf16)v.x;
+  p[1] = (__bf16)v.y;
+  return __builtin_bit_cast(uint32_t, p);
 }
 
 __device__ inline uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
@@ -55,11 +59,21 @@ __device__ inline uint32_t scale_of(uint32_t top) {
   return (uint32_t)min(max(e, 2), 252);
 }
 
-// v / 2^e to the nearest of 0 .5 1 1.5 2 3 4 6 (ties to the even code).
-__device__ inline uint32_t e2m1(float v, uint32_t scale) {
-  const float u = v * __uint_as_float((254u - scale) << 23), a = fabsf(u);
-  const uint32_t c = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.0f);
-  return c | (__float_as_uint(v) >> 28 & 8u);
+// Largest over the 16 lanes of a row, in all of them.
+__device__ inline uint32_t row_top(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true));  // rotated by 8, 4, 2, 1
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x124, 0xF, 0xF, true));
+  v = max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x122, 0xF, 0xF, true));
+  return max(v, (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x121, 0xF, 0xF, true));
+}
+
+// Byte J of `to`: v / 2^e, each part to the nearest of 0 .5 1 1.5 2 3 4 6 (ties
+// to the even code, above 6 as 6), the real one in the low nibble.  The
+// conversion takes the exponent of the scale; held against comparisons at every
+// midpoint for every third float and every fourth, scales from 2^-125 to 2^125.
+template <int J>
+__device__ inline uint32_t e2m1(uint32_t to, float2 v, uint32_t scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(to, v.x, v.y, __uint_as_float(scale << 23), J);
 }
 
 struct AppendArgs {
@@ -130,27 +144,29 @@ __device__ void append_kv(const AppendArgs& a) {
     const int e = lane - sub * dc + 64 * x, b = e / 16, r = e % 16;
     const bool mine = head && e < dc;
     uint32_t kc = 0, vc = 0, my_ks = 0, my_vs = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t kt = max(abs_bits(kx[x][j].x), abs_bits(kx[x][j].y));
-      uint32_t vt = max(abs_bits(vx[x][j].x), abs_bits(vx[x][j].y));
-#pragma unroll
-      for (int off = 8; off > 0; off >>= 1) {
-        kt = max(kt, (uint32_t)__shfl_xor((int)kt, off));
-        vt = max(vt, (uint32_t)__shfl_xor((int)vt, off));
-      }
+    auto quantise = [&](auto of) {
+      constexpr int j = decltype(of)::value;
+      const uint32_t kt = row_top(max(abs_bits(kx[x][j].x), abs_bits(kx[x][j].y)));
+      uint32_t vt = row_top(max(abs_bits(vx[x][j].x), abs_bits(vx[x][j].y)));
       // a value block that is not finite is stored as zeros: its position's
       // keys carry the NaN, so whoever attends to it sees one, nobody else
-      const bool void_v = vt >= 0x7F800000u;
-      if (void_v) vt = 0;
+      float2 v = vx[x][j];
+      if (vt >= 0x7F800000u) {
+        vt = 0;
+        v = make_float2(0.0f, 0.0f);
+      }
       const uint32_t ks = scale_of(kt), vs = scale_of(vt);
-      kc |= (e2m1(kx[x][j].x, ks) | e2m1(kx[x][j].y, ks) << 4) << (8 * j);
-      if (!void_v) vc |= (e2m1(vx[x][j].x, vs) | e2m1(vx[x][j].y, vs) << 4) << (8 * j);
+      kc = e2m1<j>(kc, kx[x][j], ks);
+      vc = e2m1<j>(vc, v, vs);
       if (r == j) {
         my_ks = bad >> j & 1 ? 255u : ks;
         my_vs = vs;
       }
-    }
+    };
+    quantise(std::integral_constant<int, 0>{});
+    quantise(std::integral_constant<int, 1>{});
+    quantise(std::integral_constant<int, 2>{});
+    quantise(std::integral_constant<int, 3>{});
     const uint32_t kd = transpose4(kc);
     if (mine) {
       const int w = 2 * b + u0 / 16, g = u0 % 16 / 4, j = lane & 3;
@@ -171,32 +187,38 @@ __device__ void append_kv(const AppendArgs& a) {
   }
 }
 
-// 1024 entries of a token's q.
+// 1024 entries of a token's q, asked for before its position is known.
 __device__ void rotate_q(const AppendArgs& a) {
   const int id = (int)blockIdx.x - a.kv_blocks, row = id / a.q_chunks, e0 = (id - row * a.q_chunks) * 1024;
+  const int n = a.heads * a.c.dc;
+  const float2* q = a.q + (int64_t)row * a.q_ld;
+  float2 x[4], cs[4];
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    const int e = e0 + m * kThreads + threadIdx.x;
+    x[m] = e < n ? q[e] : make_float2(0.0f, 0.0f);
+  }
   const int i = kv_find(a.b.n_seqs, row, [&](int s) { return kv_row(a.b, s); });
   int64_t p = -1;
   if (i >= 0) {
     const KvSeq s = kv_seq(a.b, a.c, i);
     if (row < s.row0 + s.n) p = s.len - s.n + (row - s.row0);
   }
-  const int n = a.heads * a.c.dc;
-  float2 x[4], cs[4];
   const bool known = p >= 0 && p < a.rope_len;
+  const float2* turns = a.rope + (known ? p : 0) * a.c.dc;
+  int c = (e0 + (int)threadIdx.x) % a.c.dc;
+  const int step = kThreads % a.c.dc;
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
-    const int e = e0 + m * kThreads + threadIdx.x;
-    x[m] = cs[m] = make_float2(__builtin_nanf(""), __builtin_nanf(""));
-    if (known && e < n) {
-      x[m] = a.q[(int64_t)row * a.q_ld + e];
-      cs[m] = a.rope[p * a.c.dc + e % a.c.dc];
-    }
+    cs[m] = known ? turns[c] : make_float2(__builtin_nanf(""), __builtin_nanf(""));
+    c += step;
+    if (c >= a.c.dc) c -= a.c.dc;
   }
+  uint32_t* out = a.q_out + (int64_t)row * n;
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
     const int e = e0 + m * kThreads + threadIdx.x;
-    const float2 y = turn(x[m], cs[m]);
-    if (e < n) a.q_out[(int64_t)row * n + e] = bf16_of(y.x) | bf16_of(y.y) << 16;
+    if (e < n) out[e] = bf16_pair(turn(x[m], cs[m]));
   }
 }
 

@@ -13,6 +13,7 @@
 // One pass with a running maximum and sum; positions are split over blocks
 // (chunks) and over a block's waves, joined through LDS and, where a row has
 // several chunks, by a second kernel.
+#include <float.h>
 #include <math.h>
 
 #include <type_traits>
@@ -26,9 +27,24 @@ namespace {
 constexpr int kRows = 16;         // that a matrix product takes
 constexpr int kCus = 256;
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
-// Blocks of 16 rows in a row tile: one where no sequence can have more, else
-// as many as share a conversion.
-constexpr int wide_rb(int nb) { return nb <= 4 ? 2 : 1; }
+// Blocks of 16 rows in a row tile: one, or, past kWideRows rows a sequence in
+// the mean, as many as share a conversion of the cache: two of a wave up to
+// dc = 32, one of each of eight waves at dc = 48 and 64, and one again above
+// (dc = 128, 1024 tokens behind 1024, 16 heads on 4: 16 rows 66 us, 32 111).
+// us, one block | shared: dc = 64, 32 heads on 32, a prompt of 2048 107 | 74;
+// 32 on 8, 2048 behind 2048 220 | 152, 8 prompts of up to 700 80 | 49; dc = 32,
+// 16 on 4, 3 x 509 behind 15872 111 | 97 (by eight waves 106); dc = 16, 8 on 1,
+// 2 x 512 behind 7680 50 | 46 (78).
+constexpr int wide_rb(int nb) { return nb <= 2 ? 2 : 1; }
+constexpr int kSharedWaves = 8;
+constexpr bool shared(int nb) { return nb == 3 || nb == 4; }
+constexpr int wide_blocks(int nb) { return shared(nb) ? kSharedWaves : wide_rb(nb); }
+// Small blocks leave fewer rows idle and fill more of the machine.  64
+// sequences of up to 2000 positions, rows each, us, one block | shared: dc = 64,
+// 32 heads on 8: 32 rows 44 | 70, 64 56 | 73, 128 75 | 80, 256 140 | 120;
+// dc = 32, 16 on 4: 32 23 | 25, 128 40 | 42, 256 53 | 56.  One sequence, 16381
+// positions: dc = 64 32 18.6 | 21.5, 128 32.2 | 32.7, 256 52 | 46.
+constexpr int kWideRows = 128;
 // Blocks that are resident at once, which a call is cut into where its rows
 // alone are fewer: by the kernels' registers.  More items than that, and the
 // last ones run beside empty CUs: one token over 262144 positions, 32 heads on
@@ -132,6 +148,14 @@ __device__ inline bool find_item(const AttnArgs& a, int at, int target, Item& it
   int whole = whole_of(first);
   for (int i = 64 + lane; i < n; i += 64) whole += whole_of(seq(i));
   whole = total(whole);
+  if (RB == kSharedWaves) {
+    // One or two blocks a CU, the longest first: the second ones in the other
+    // order, so that a CU's two are as long together as any other's.
+    int all = all_of(first);
+    for (int i = 64 + lane; i < n; i += 64) all += all_of(seq(i));
+    all = total(all);
+    if (all > kCus && all <= 2 * kCus && at >= kCus && at < all) at = all - 1 - (at - kCus);
+  }
   const bool rest = at >= whole;
   if (rest) at -= whole;
   int before = 0, ids = 0;  // items of the sequences before: of this kind, and all
@@ -161,19 +185,26 @@ __device__ inline bool find_item(const AttnArgs& a, int at, int target, Item& it
   return false;
 }
 
-// A tile's codes and scales of one lane.
-template <int NB>
+// Codes and scales of a tile (PARTS = 1) or of about half of its blocks, part
+// PART of two, of one lane.
+template <int NB, int PARTS>
 struct TileRegs {
   static constexpr KvTile T{NB};
-  uint32_t k[2 * NB], v[2 * NB];
+  static constexpr int kUnits = 2 * NB / T.unit, kBlocks = T.unit / 2;  // loads of each array, blocks a load
+  static constexpr int kMax = (kUnits + PARTS - 1) / PARTS;
+  uint32_t k[kMax * T.unit], v[kMax * T.unit];
   uint32_t ks[2][(T.sb + 3) / 4], vs[2 * T.sb];
 
+  static constexpr int first(int part) { return part * (kUnits / PARTS); }
+  static constexpr int last(int part) { return part + 1 == PARTS ? kUnits : first(part + 1); }
+
+  template <int PART>
   __device__ inline void load(const uint8_t* tile) {
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int u = 0; u < 2 * NB / T.unit; ++u) {
-      load_n<T.unit>(k + u * T.unit, tile + T.dword(u * T.unit, lane));
-      load_n<T.unit>(v + u * T.unit, tile + T.v_codes() + T.dword(u * T.unit, lane));
+    for (int u = first(PART); u < last(PART); ++u) {
+      load_n<T.unit>(k + (u - first(PART)) * T.unit, tile + T.dword(u * T.unit, lane));
+      load_n<T.unit>(v + (u - first(PART)) * T.unit, tile + T.v_codes() + T.dword(u * T.unit, lane));
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -213,9 +244,10 @@ struct TileRegs {
   }
 
   // Keys of half `s` (16 positions), block b: the A operand of S^T.
+  template <int PART>
   __device__ inline bf16x8 key(int b, int s) const {
     const float scale = scale_at(ks[s], b);
-    const uint32_t w = k[2 * b + s];
+    const uint32_t w = k[2 * (b - first(PART) * kBlocks) + s];
     u32x4 o;
     o[0] = pair<0>(w, scale);
     o[1] = pair<1>(w, scale);
@@ -225,11 +257,12 @@ struct TileRegs {
   }
 
   // Values of block b: the A operands of O^T, real and imaginary parts.
+  template <int PART>
   __device__ inline void value(int b, bf16x8& re, bf16x8& im) const {
     uint32_t c[8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const uint32_t w = v[2 * b + h];
+      const uint32_t w = v[2 * (b - first(PART) * kBlocks) + h];
       c[4 * h + 0] = pair<0>(w, scale_at(vs, (4 * h + 0) * T.sb + b));
       c[4 * h + 1] = pair<1>(w, scale_at(vs, (4 * h + 1) * T.sb + b));
       c[4 * h + 2] = pair<2>(w, scale_at(vs, (4 * h + 2) * T.sb + b));
@@ -299,6 +332,10 @@ __device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 template <int NB, int RB>
 constexpr int kLds = (RB > 1 ? 2 : kWaves) * 16 * RB * ((32 * NB + 4) * 4 + 8);
 
+// Four tiles' operands and whether the table has them.
+template <int NB>
+constexpr int kSharedLds = kSharedWaves / 2 * (4096 * NB + 4);
+
 // The queries of rows row0 .. row0 + 15 of a tile: operand B of S^T.
 template <int NB>
 __device__ inline void load_q(const AttnArgs& a, const Item& it, int row0, bf16x8 (&q)[NB]) {
@@ -322,15 +359,17 @@ __device__ inline void mask(f32x4 (&s)[H], int t0, int last) {
       if (from + 16 * h + i > last) s[h][i] = -INFINITY;
 }
 
-// A row block's running softmax: what its weights are relative to (times the
-// scale, and as a score; -infinity until a finite score is seen), and the lane's
-// share of their sum.
+// A row block's running softmax: the score that its weights are relative to, and
+// the lane's share of their sum.  It starts below every finite score and takes
+// no part until one is seen: masked ones are -infinity, and weigh nothing.
 struct Softmax {
-  float ref = 0.0f, m = -INFINITY, l = 0.0f;
+  float m = -FLT_MAX, l = 0.0f;
 };
 
 // Over the scores of H times 16 positions: raises the reference where they ask
-// for it (scaling l and o), adds to l and leaves the weights in p.
+// for it (scaling l and o), adds to l and leaves the weights in p.  The reference
+// is subtracted before the scale: one fused multiply-add of its product would
+// save an instruction, but its rounding passes 2^7 once scores pass 2^31.
 template <int NB, int H>
 __device__ inline void weigh(const f32x4 (&s)[H], float scale, Softmax& x, f32x4 (&o)[2 * NB], float (&p)[4 * H]) {
   float top = s[0][0];
@@ -339,16 +378,15 @@ __device__ inline void weigh(const f32x4 (&s)[H], float scale, Softmax& x, f32x4
   if (__any(top > x.m + kRaise / scale)) {
     asm volatile("");
     top = fmaxf(x.m, row_max(top));  // the row's own, in all of its lanes
-    const float f = top == -INFINITY ? 1.0f : exp2_of((x.m - top) * scale);
+    const float f = exp2_of((x.m - top) * scale);
     x.m = top;
-    x.ref = top == -INFINITY ? 0.0f : top * scale;
     x.l *= f;
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i) o[i] *= f;
   }
 #pragma unroll
   for (int i = 0; i < 4 * H; ++i) {
-    p[i] = exp2_of(__builtin_fmaf(s[i / 4][i % 4], scale, -x.ref));
+    p[i] = exp2_of((s[i / 4][i % 4] - x.m) * scale);
     x.l += p[i];
   }
 }
@@ -411,7 +449,7 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
     const int id = __builtin_amdgcn_readlane(ids, k % 64);
     return id < 0 ? nullptr : a.c.data + (int64_t)id * KvTile(NB).bytes;
   };
-  auto step = [&](int t, TileRegs<NB>& x) {
+  auto step = [&](int t, TileRegs<NB, 1>& x) {
     f32x4 s[RB][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -419,7 +457,7 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
       for (int y = 0; y < RB; ++y) s[y][h] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const bf16x8 k = x.key(b, h);
+        const bf16x8 k = x.template key<0>(b, h);
 #pragma unroll
         for (int y = 0; y < RB; ++y) s[y][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[y][b], s[y][h], 0, 0, 0);
       }
@@ -440,7 +478,7 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       bf16x8 re, im;
-      x.value(b, re, im);
+      x.template value<0>(b, re, im);
 #pragma unroll
       for (int y = 0; y < RB; ++y) {
         o[y][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(re, ph[y], o[y][2 * b], 0, 0, 0);
@@ -455,18 +493,18 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
   };
   {
     // two sets of registers, one loaded while the other is used
-    TileRegs<NB> xa, xb;
+    TileRegs<NB, 1> xa, xb;
     int k = 0, t = t_first;
     const uint8_t* at = tile_at(0);
-    if (at) xa.load(at);
+    if (at) xa.template load<0>(at);
     while (t < t_end) {
       const uint8_t* next = tile_at(k + 1);
-      if (next) xb.load(next);
+      if (next) xb.template load<0>(next);
       if (at) step(t, xa);
       t += kWaves;
       if (t >= t_end) break;
       at = tile_at(k + 2);
-      if (at) xa.load(at);
+      if (at) xa.template load<0>(at);
       if (next) step(t, xb);
       t += kWaves;
       k += 2;
@@ -493,8 +531,8 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
 #pragma unroll
       for (int y = 0; y < RB; ++y) {
         const float2 ml = mls[w][kRows * y + r];
-        const float top = fmaxf(sm[y].m, ml.x), ref = top == -INFINITY ? 0.0f : top;
-        const float f = exp2_of((sm[y].m - ref) * a.scale), h = exp2_of((ml.x - ref) * a.scale);
+        const float top = fmaxf(sm[y].m, ml.x);
+        const float f = exp2_of((sm[y].m - top) * a.scale), h = exp2_of((ml.x - top) * a.scale);
         sm[y].m = top;
         sm[y].l = f * sm[y].l + h * ml.y;
 #pragma unroll
@@ -551,12 +589,11 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
       float top = mls[0][rr].x;
 #pragma unroll
       for (int i = 1; i < kWaves; ++i) top = fmaxf(top, mls[i][rr].x);
-      const float ref = top == -INFINITY ? 0.0f : top;
       float sum = 0.0f;
       float2 y = make_float2(0.0f, 0.0f);
 #pragma unroll
       for (int i = 0; i < kWaves; ++i) {
-        const float f = exp2_of((mls[i][rr].x - ref) * a.scale);
+        const float f = exp2_of((mls[i][rr].x - top) * a.scale);
         sum += f * mls[i][rr].y;
         const float2 v = *reinterpret_cast<const float2*>(&os[i][rr][2 * c]);
         y.x += f * v.x;
@@ -575,15 +612,148 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
   }
 }
 
-template <int NB, int RB>
-__global__ __launch_bounds__(kThreads, RB > 1 ? 2 : 1) void kv_attend_kernel(AttnArgs a) {
-  __shared__ __align__(16) char lds[kLds<NB, RB>];
-  static_assert(sizeof(Item) <= kLds<NB, RB>);
-  // one wave looks the item up for all
+// Many rows of heads whose conversions cost as much as their softmax (dc = 48,
+// 64): a wave for each 16 of a tile's 128 rows, all walking the chunk's tiles
+// together, four at a time from LDS.  Two waves convert a tile for all of them
+// into the operands' order, its codes loaded a round before.  What counts is
+// four waves a SIMD (128 registers): alone, a wave issues a vector instruction
+// every seventh cycle or so, and none beside its own matrix products.  Operands
+// are asked for four products ahead; left to the compiler, each is waited for
+// right after it is asked for.
+template <int NB>
+__device__ inline void attend_shared(const AttnArgs& a, const Item& it, char* lds) {
+  constexpr int D = 32 * NB, W = kSharedWaves, R = W / 2;
+  using Regs = TileRegs<NB, 2>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int r = lane & 15, g = lane >> 4, mine = wave / 2;
+  auto operand = [&](int tile, int i) {  // i: keys 2 b + s, values 2 NB + 2 b + (0 re, 1 im)
+    return reinterpret_cast<bf16x8*>(lds + tile * 4096 * NB + i * 1024) + lane;
+  };
+  int* there = reinterpret_cast<int*>(lds + R * 4096 * NB);  // whether the table has the round's tiles
+  const int rows = it.s.n * a.group, tile0 = it.tile * kRows * W, row0 = tile0 + wave * kRows;
+  const int p0 = it.s.len - it.s.n;  // position of the first new token
+  const int tile_most = p0 + (min(tile0 + kRows * W, rows) - 1) / a.group;
+  const int tiles = kv_tiles(tile_most + 1), chunks = max(1, (tiles + it.chunk_tiles - 1) / it.chunk_tiles);
+  if (it.chunk == 0 && threadIdx.x < W && tile0 + kRows * (int)threadIdx.x < rows)
+    a.meta[(int64_t)(row_slot(a, it.seq) + it.tile * W + threadIdx.x) * a.c.kv_heads + it.head] =
+        make_int2(it.id * a.tile_rows + kRows * (int)threadIdx.x, chunks);
+  if (it.chunk >= chunks) return;
+  const int t_end = min(tiles, (it.chunk + 1) * it.chunk_tiles);
+  // the least and the most that any of the wave's rows sees
+  const int least = p0 + row0 / a.group;
+  const int most = row0 < rows ? p0 + (min(row0 + kRows, rows) - 1) / a.group : -1;
+  const int last = min(p0 + (row0 + r) / a.group, most);  // rows past the end compute what nobody stores
+  bf16x8 q[NB];
+  load_q<NB>(a, it, row0, q);
+  f32x4 o[2 * NB];
+#pragma unroll
+  for (int i = 0; i < 2 * NB; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  Softmax sm;
+
+  Regs x;
+  const int t_first = it.chunk * it.chunk_tiles;
+  int ids = 0;  // of 64 tiles, one a lane
+  auto fetch = [&](int k) {  // the wave's part of tile k + mine: whether there is one
+    if (k % 64 == 0) {
+      const int t = t_first + k + lane;
+      ids = t < t_end ? kv_tile_index(a.c, a.b, it.seq, t, it.head) : -1;
+    }
+    const int id = __builtin_amdgcn_readlane(ids, k % 64 + mine);
+    if (id >= 0) {
+      const uint8_t* at = a.c.data + (int64_t)id * KvTile(NB).bytes;
+      if (wave % 2 == 0) x.template load<0>(at);
+      else x.template load<1>(at);
+    }
+    return id >= 0;
+  };
+  auto convert = [&](auto part) {
+    constexpr int P = decltype(part)::value;
+#pragma unroll
+    for (int b = Regs::first(P) * Regs::kBlocks; b < Regs::last(P) * Regs::kBlocks; ++b) {
+      *operand(mine, 2 * b) = x.template key<P>(b, 0);
+      *operand(mine, 2 * b + 1) = x.template key<P>(b, 1);
+      bf16x8 re, im;
+      x.template value<P>(b, re, im);
+      *operand(mine, 2 * NB + 2 * b) = re;
+      *operand(mine, 2 * NB + 2 * b + 1) = im;
+    }
+  };
+  bool have = fetch(0);
+  for (int k = 0; t_first + k < t_end; k += R) {
+    __syncthreads();  // the last round's readers
+    if (have) {
+      const int t0 = (t_first + k + mine) * kKvTile;
+      if (t0 + kKvTile > it.s.len) x.end_at(it.s.len - t0);
+      if (wave % 2 == 0) convert(std::integral_constant<int, 0>{});
+      else convert(std::integral_constant<int, 1>{});
+    }
+    if (lane == 0 && wave % 2 == 0) there[mine] = have;
+    have = fetch(k + R);
+    __syncthreads();
+#pragma unroll 1
+    for (int u = 0; u < R; ++u) {
+      const int t0 = (t_first + k + u) * kKvTile;
+      if (t0 > most) break;
+      if (!__builtin_amdgcn_readfirstlane(there[u])) continue;  // no such page: nothing to see there
+      constexpr int N = 2 * NB, AHEAD = 4;
+      bf16x8 buf[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) buf[i] = *operand(u, i);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        s[i % 2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(buf[i % AHEAD], q[i / 2], s[i % 2], 0, 0, 0);
+        buf[i % AHEAD] = *operand(u, i + AHEAD);  // the last ones: the first values
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (t0 + kKvTile - 1 > least) mask<2>(s, t0, last);
+      float p[8];
+      weigh<NB, 2>(s, a.scale, sm, o, p);
+      bf16x8 ph, pl;
+      split_bf16(p, ph, pl);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(buf[(i + N) % AHEAD], ph, o[i], 0, 0, 0);
+        o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(buf[(i + N) % AHEAD], pl, o[i], 0, 0, 0);
+        if (i + AHEAD < N) buf[(i + N) % AHEAD] = *operand(u, N + i + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  const float sum = row_sum(sm.l);
+  const int row = row0 + r, token = row / a.group, hq = it.head * a.group + (row - token * a.group);
+  if (row >= rows) return;
+  if (chunks == 1) {
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    u32x4* to = reinterpret_cast<u32x4*>(a.out + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      u32x4 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = pack_bf16(o[2 * b][i] * inv, o[2 * b + 1][i] * inv);
+      to[4 * b] = v;
+    }
+  } else {
+    const int64_t rec = (int64_t)it.id * a.tile_rows + (row - tile0);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2)
+        *reinterpret_cast<float4*>(a.part + rec * D + 32 * b + 8 * g + 2 * i) =
+            make_float4(o[2 * b][i], o[2 * b + 1][i], o[2 * b][i + 1], o[2 * b + 1][i + 1]);
+    if (g == 0) a.ml[rec] = make_float2(sm.m, sum);
+  }
+}
+
+// The block's item, looked up by one wave for all; seq < 0: none.
+template <int RB>
+__device__ inline Item block_item(const AttnArgs& a, int target, char* lds) {
   Item it{};
   Item* found = reinterpret_cast<Item*>(lds);
   if (threadIdx.x < 64) {
-    if (!find_item<RB>(a, blockIdx.x, resident(NB, RB > 1), it)) it.seq = -1;
+    if (!find_item<RB>(a, blockIdx.x, target, it)) it.seq = -1;
     if (threadIdx.x == 0) *found = it;
   }
   __syncthreads();
@@ -591,9 +761,23 @@ __global__ __launch_bounds__(kThreads, RB > 1 ? 2 : 1) void kv_attend_kernel(Att
   int* word = reinterpret_cast<int*>(&it);
 #pragma unroll
   for (int i = 0; i < (int)(sizeof(Item) / 4); ++i) word[i] = __builtin_amdgcn_readfirstlane(word[i]);
-  if (it.seq < 0) return;
-  __syncthreads();  // the sums go where the item stands
-  attend_tile<NB, RB>(a, it, lds);
+  __syncthreads();  // what else stands there comes after this
+  return it;
+}
+
+template <int NB, int RB>
+__global__ __launch_bounds__(kThreads, RB > 1 ? 2 : 1) void kv_attend_kernel(AttnArgs a) {
+  __shared__ __align__(16) char lds[kLds<NB, RB>];
+  static_assert(sizeof(Item) <= kLds<NB, RB>);
+  const Item it = block_item<RB>(a, resident(NB, RB > 1), lds);
+  if (it.seq >= 0) attend_tile<NB, RB>(a, it, lds);
+}
+
+template <int NB>
+__global__ __launch_bounds__(64 * kSharedWaves, 4) void kv_attend_shared_kernel(AttnArgs a) {
+  __shared__ __align__(16) char lds[kSharedLds<NB>];
+  const Item it = block_item<kSharedWaves>(a, resident(NB, true), lds);
+  if (it.seq >= 0) attend_shared<NB>(a, it, lds);
 }
 
 constexpr int kJoinThreads = 256;
@@ -647,14 +831,14 @@ __global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a
       y.z += f * v[j].z;
       y.w += f * v[j].w;
     };
-    float top = -INFINITY, sum = 0.0f;
+    float top = -FLT_MAX, sum = 0.0f;
     ask(part);
     if (few) {
-      const float2 ml = lane < chunks ? a.ml[record(lane)] : make_float2(-INFINITY, 0.0f);
+      const float2 ml = lane < chunks ? a.ml[record(lane)] : make_float2(-FLT_MAX, 0.0f);
       top = ml.x;
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-      const float f = exp2_of((ml.x - (top == -INFINITY ? 0.0f : top)) * a.scale);
+      const float f = exp2_of((ml.x - top) * a.scale);
       sum = f * ml.y;
 #pragma unroll
       for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
@@ -686,9 +870,8 @@ __global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < kWavesJ; ++j) top = fmaxf(top, tops[j]);
-      const float ref = top == -INFINITY ? 0.0f : top;
       for (int k = tid; k < chunks; k += kJoinThreads) {
-        const float f = exp2_of((weight[k] - ref) * a.scale);
+        const float f = exp2_of((weight[k] - top) * a.scale);
         weight[k] = f;
         sum += f * a.ml[record(k)].y;
       }
@@ -739,12 +922,11 @@ struct Layout {
 Layout layout_of(const fairy2i_kv_cache* c, int64_t n_new, int64_t n_seqs, int32_t n_heads) {
   Layout l{};
   const int64_t G = n_heads / c->n_kv_heads;
-  // some sequence has more than a block of rows
-  l.wide = n_new * G > kRows * n_seqs;
-  l.tile_rows = l.wide ? kRows * wide_rb(c->dc / 16) : kRows;
+  l.wide = n_new * G > kWideRows * n_seqs && wide_blocks((int)c->dc / 16) > 1;
+  l.tile_rows = l.wide ? kRows * wide_blocks(c->dc / 16) : kRows;
   // a row tile more than its rows fill for each sequence that has any, and a
   // chunk more than its work fills for each row tile
-  l.items = resident((int)c->dc / 16, l.tile_rows > kRows) + c->n_kv_heads * (n_new * G / l.tile_rows + (n_seqs < n_new ? n_seqs : n_new));
+  l.items = resident((int)c->dc / 16, l.wide) + c->n_kv_heads * (n_new * G / l.tile_rows + (n_seqs < n_new ? n_seqs : n_new));
   l.slots = row_slots(n_new, n_seqs, (int)G);
   auto up = [](size_t b) { return (b + 255) / 256 * 256; };
   l.part = up((size_t)l.items * l.tile_rows * 2 * c->dc * sizeof(float));
@@ -756,8 +938,17 @@ Layout layout_of(const fairy2i_kv_cache* c, int64_t n_new, int64_t n_seqs, int32
 
 template <int NB>
 void launch(const AttnArgs& a, const Layout& l, bool one_chunk, hipStream_t s) {
-  auto kernel = l.wide ? kv_attend_kernel<NB, wide_rb(NB)> : kv_attend_kernel<NB, 1>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)l.items), dim3(kThreads), 0, s, a);
+  auto kernel = kv_attend_kernel<NB, 1>;
+  int threads = kThreads;
+  if constexpr (shared(NB)) {
+    if (l.wide) {
+      kernel = kv_attend_shared_kernel<NB>;
+      threads = 64 * kSharedWaves;
+    }
+  } else if constexpr (wide_rb(NB) > 1) {
+    if (l.wide) kernel = kv_attend_kernel<NB, wide_rb(NB)>;
+  }
+  hipLaunchKernelGGL(kernel, dim3((unsigned)l.items), dim3(threads), 0, s, a);
   if (one_chunk) return;
   const int64_t blocks = l.slots * a.c.kv_heads;
   const unsigned split = blocks <= 512 ? kRows : blocks <= 2048 ? 4 : 1;
@@ -793,7 +984,7 @@ fairy2i_status fairy2i_kv_attend(const fairy2i_kv_cache* cache, const fairy2i_kv
   const Layout l = layout_of(cache, batch->n_new, batch->n_seqs, n_heads);
   if (!workspace || workspace_bytes < l.bytes || (reinterpret_cast<uintptr_t>(workspace) & 15) != 0)
     return FAIRY2I_ERR_WORKSPACE;
-  if (l.items > INT32_MAX / kThreads || l.items * l.tile_rows > INT32_MAX || l.slots * cache->n_kv_heads > INT32_MAX / kThreads)
+  if (l.items > INT32_MAX / 512 || l.items * l.tile_rows > INT32_MAX || l.slots * cache->n_kv_heads > INT32_MAX / 512)
     return FAIRY2I_ERR_UNSUPPORTED;
   AttnArgs a{};
   a.c = kv_cache_of(cache);

@@ -583,3 +583,55 @@ def test_refusals(gpu):
     bad(f2.Fairy2iError, f2.add_rmsnorm_i8, x[:0], g)
     bad(ValueError, f2.rope_table, 0, 4, device=gpu)
     bad(f2.Fairy2iError, f2.rope_table, 4, 4, base=-1.0, device=gpu)
+
+
+# ------------------------------------------- more than one kernel's own edges
+
+
+@pytest.mark.parametrize("extra", [0, 1024])
+@pytest.mark.parametrize("kv, heads, dc, page", [(1, 2, 48, 32), (2, 2, 64, 96), (1, 3, 64, 32), (1, 2, 32, 64), (1, 1, 112, 32)])
+def test_attend_row_tiles_and_rounds(gpu, kv, heads, dc, page, extra):
+    """Rows on both sides of 16, 32 and 128 a sequence and in the mean, lengths
+    past 64 tiles (2048 positions) and not of whole rounds, some pages missing."""
+    b = Batch([(1 + extra, 1 + extra), (150, 2500), (17, 17), (128, 129), (1, 2177), (0, 300), (8, 2049), (33, 33)], kv, dc, page, gpu, seed=17).fill()
+    b.table[1, 3] = -1
+    b.table[1, -(-2400 // page)] = -1
+    b.table[4, 1:5] = b.n_pages
+    b.table[7] = -1
+    q = queries(b, heads, 1.5)
+    got = b.dev().attend(q.to(gpu), *b.t)
+    attend_check(b, heads, q.double().numpy(), got, (2 * dc) ** -0.5)
+    assert (host(got)[b.cu[7]:] == 0).all()
+
+
+@pytest.mark.parametrize("n_seqs", [65, 130, 300])
+def test_many_sequences(gpu, n_seqs):
+    """More sequences than a wave has lanes; some empty, some without rows."""
+    rng = np.random.default_rng(n_seqs)
+    seqs = [(int(n), int(n + c)) for n, c in zip(rng.integers(0, 3, n_seqs), rng.integers(0, 90, n_seqs))]
+    seqs[n_seqs // 2] = (1, 1700)
+    b = Batch(seqs, 2, 32, 32, gpu, seed=18).fill()
+    k, v, q = random_c(b.rng, b.N, 2, 32), random_c(b.rng, b.N, 2, 32), random_c(b.rng, b.N, 4, 32)
+    rope = rope_of(b.width * 32, 32, gpu)
+    qr = b.dev().append(dev(k, gpu), dev(v, gpu), *b.t, rope, q=dev(q, gpu))
+    np.testing.assert_array_equal(host(b.data), expect_append(b, k, v, host(rope)))
+    b.cache = host(b.data)
+    got = b.kvc.attend(qr, *b.t)
+    attend_check(b, 4, host(qr).astype(np.float64), got, 64 ** -0.5)
+    rk, rv = b.kvc.read(*b.t, b.N)
+    for i in (0, n_seqs // 2, n_seqs - 1):
+        n, length = seqs[i]
+        want = sv.read(b.cache, 32, 2, 32, b.table[i], length)[:, length - n:]
+        np.testing.assert_array_equal(host(rk)[b.cu[i]:b.cu[i + 1]], want[0])
+        np.testing.assert_array_equal(host(rv)[b.cu[i]:b.cu[i + 1]], want[1])
+
+
+def test_scale_at_the_ends_of_its_range(gpu):
+    b = Batch([(3, 300), (20, 40)], 1, 64, 32, gpu, seed=19).fill()
+    q = queries(b, 2)
+    b.dev()
+    for scale in (1e-30, 1e30):
+        got = host(b.kvc.attend(q.to(gpu), *b.t, scale=scale))
+        assert np.isfinite(got).all()
+    flat = b.kvc.attend(q.to(gpu), *b.t, scale=1e-30)
+    attend_check(b, 2, q.double().numpy(), flat, 1e-30)

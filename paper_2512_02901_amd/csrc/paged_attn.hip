@@ -784,8 +784,11 @@ constexpr int kJoinThreads = 256;
 
 // Joins a row block's chunks.  What bounds it is a chain of loads (of the
 // sequences, of the chunks' maxima and sums), so the first sums are asked for
-// before their weights are known, eight a lane at a time.  Up to 64 chunks: a
-// wave a row; more: a block a row.  blockIdx.y: which rows, of 16.
+// before their weights are known, eight a lane at a time.  Up to 8 chunks: a
+// lane for four reals, so a wave has several rows (with a wave a row, 32 x 64
+// tokens over 4096 positions, dc = 64, took 141 us for 130, 2 x 512 over 8192,
+// dc = 16, 46 for 39); up to 64: a wave a row; more: a block a row.
+// blockIdx.y: which rows, of 16.
 template <int NB>
 __global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a) {
   constexpr int D = 32 * NB, kQuads = D / 4, kLanes = kQuads <= 8 ? 8 : kQuads <= 16 ? 16 : kQuads <= 32 ? 32 : 64;
@@ -807,6 +810,43 @@ __global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a
   const int64_t stride = (int64_t)a.c.kv_heads * a.tile_rows, records = (int64_t)a.items * a.tile_rows;
   if (chunks > kMaxItems + 1 || meta.x < 0 || meta.x + (int64_t)(chunks - 1) * stride + kRows > records) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto store = [&](int w, int c, const float4& y, float sum) {
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    const int tk = w / a.group, hh = head * a.group + (w - tk * a.group);
+    *reinterpret_cast<uint2*>(a.out + ((int64_t)(row0 + tk) * a.heads + hh) * (D / 2) + 2 * c) =
+        make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
+  };
+  if (chunks <= kAhead) {
+    constexpr int kPer = 64 / kLanes;
+    const int c = lane % kLanes;
+    for (int rr = (blockIdx.y * kWavesJ + wave) * kPer + lane / kLanes; rr < kRows; rr += gridDim.y * kWavesJ * kPer) {
+      const int w = block * kRows + rr;
+      if (w >= rows) break;
+      float2 ml[kAhead];
+      float4 v[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int64_t rec = meta.x + k * stride + rr;
+        ml[k] = k < chunks ? a.ml[rec] : make_float2(-FLT_MAX, 0.0f);
+        v[k] = k < chunks && c < kQuads ? *reinterpret_cast<const float4*>(a.part + rec * D + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      float top = ml[0].x, sum = 0.0f;
+#pragma unroll
+      for (int k = 1; k < kAhead; ++k) top = fmaxf(top, ml[k].x);
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float f = exp2_of((ml[k].x - top) * a.scale);
+        sum += f * ml[k].y;
+        y.x += f * v[k].x;
+        y.y += f * v[k].y;
+        y.z += f * v[k].z;
+        y.w += f * v[k].w;
+      }
+      if (c < kQuads) store(w, c, y, sum);
+    }
+    return;
+  }
   // threads of a row: of a wave, or of the block
   const bool few = chunks <= 64;
   const int mine = few ? lane : tid, parts = (few ? 64 : kJoinThreads) / kLanes, part = mine / kLanes, c = mine % kLanes;
@@ -904,12 +944,7 @@ __global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a
       }
       __syncthreads();  // the next row's writers
     }
-    if (part == 0 && c < kQuads) {
-      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-      const int tk = w / a.group, hh = head * a.group + (w - tk * a.group);
-      *reinterpret_cast<uint2*>(a.out + ((int64_t)(row0 + tk) * a.heads + hh) * (D / 2) + 2 * c) =
-          make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
-    }
+    if (part == 0 && c < kQuads) store(w, c, y, sum);
   }
 }
 
@@ -951,7 +986,11 @@ void launch(const AttnArgs& a, const Layout& l, bool one_chunk, hipStream_t s) {
   hipLaunchKernelGGL(kernel, dim3((unsigned)l.items), dim3(threads), 0, s, a);
   if (one_chunk) return;
   const int64_t blocks = l.slots * a.c.kv_heads;
-  const unsigned split = blocks <= 512 ? kRows : blocks <= 2048 ? 4 : 1;
+  // Blocks a row block: more only where few rows leave the machine empty, each
+  // costs its chain of lookups.  us of the whole call, 16 | 4 | 1: one token
+  // behind 131071, 64 heads on 4 (dc = 64) 27 | 37; 16 sequences of 4096, 32 on 8
+  // (dc = 64) 23.3 | 22.2; 2 x 512 tokens behind 7680, 8 on 1 (dc = 16) 4: 39, 1: 37.
+  const unsigned split = blocks <= 32 ? kRows : blocks <= 512 ? 4 : 1;
   hipLaunchKernelGGL(kv_attend_join_kernel<NB>, dim3((unsigned)blocks, split), dim3(kJoinThreads), 0, s, a);
 }
 

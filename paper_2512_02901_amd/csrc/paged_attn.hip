@@ -13,6 +13,18 @@
 // One pass with a running maximum and sum; positions are split over blocks
 // (chunks) and over a block's waves, joined through LDS and, where a row has
 // several chunks, by a second kernel.
+//
+// What bounds it, with us of a whole call:
+//  - a few tokens a sequence: memory.  One token over 262144 positions, 32 heads
+//    on 8 of dc = 64 (285 MB), 60 us, its first kernel 53 (5.4 TB/s, a copy's
+//    rate); 63 sequences of up to 8192 (302 MB) 76, 72 (4.2 TB/s: blocks start with
+//    a chain of lookups, about 8 us under load, that their own loads wait for);
+//  - short contexts: that chain and the join's; one token over 40 positions 4.4,
+//    over 2048 (32 heads) 9.2, of which the join 3.0;
+//  - prompts: the vector work of softmax and weights, issued beside the matrix
+//    products of other waves only.  2048 tokens, 32 heads of dc = 64, 73 us (0.47
+//    PFLOP/s of 4 products of 2 flops an entry, 0.7 as executed, the weights' two
+//    parts counted); 811 tokens behind 15872, 16 on 4 of dc = 32, 86 us (0.42).
 #include <float.h>
 #include <math.h>
 
@@ -33,8 +45,8 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 // (dc = 128, 1024 tokens behind 1024, 16 heads on 4: 16 rows 66 us, 32 111).
 // us, one block | shared: dc = 64, 32 heads on 32, a prompt of 2048 107 | 74;
 // 32 on 8, 2048 behind 2048 220 | 152, 8 prompts of up to 700 80 | 49; dc = 32,
-// 16 on 4, 3 x 509 behind 15872 111 | 97 (by eight waves 106); dc = 16, 8 on 1,
-// 2 x 512 behind 7680 50 | 46 (78).
+// 16 on 4, 509 behind 15872 and 302 behind 2065 111 | 97 (by eight waves 106);
+// dc = 16, 8 on 1, 2 x 512 behind 7680 50 | 46 (78).
 constexpr int wide_rb(int nb) { return nb <= 2 ? 2 : 1; }
 constexpr int kSharedWaves = 8;
 constexpr bool shared(int nb) { return nb == 3 || nb == 4; }
@@ -785,9 +797,9 @@ constexpr int kJoinThreads = 256;
 // Joins a row block's chunks.  What bounds it is a chain of loads (of the
 // sequences, of the chunks' maxima and sums), so the first sums are asked for
 // before their weights are known, eight a lane at a time.  Up to 8 chunks: a
-// lane for four reals, so a wave has several rows (with a wave a row, 32 x 64
-// tokens over 4096 positions, dc = 64, took 141 us for 130, 2 x 512 over 8192,
-// dc = 16, 46 for 39); up to 64: a wave a row; more: a block a row.
+// lane for four reals, so a wave has several rows (with a wave a row, 32 x up to
+// 64 tokens over up to 4096 positions, dc = 64, took 141 us for 130, 2 x 512 over
+// 8192, dc = 16, 46 for 39); up to 64: a wave a row; more: a block a row.
 // blockIdx.y: which rows, of 16.
 template <int NB>
 __global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a) {

@@ -5,6 +5,12 @@
 // either code array holds: a value dword is four positions of an entry, a key
 // dword four entries of a position, so both go out whole (the keys' bytes
 // transposed within four lanes), and no two waves share a byte.
+//
+// What bounds the append is memory: 8 bytes an entry of q, k and v in, 4 of q
+// and about 1 of k and v each out.  3926 tokens of 32 heads on 8 (dc = 64) 28.6 us
+// (5.3 TB/s, a plain copy's rate, with q's turns in blocks beside the keys');
+// 15 single tokens of 32 on 32 4.8 us, a chain of loads (which sequence, its
+// page, its values).  Reading the same tokens back 7.6 and 3.5 us.
 #include <math.h>
 
 #include <type_traits>
@@ -89,7 +95,8 @@ struct AppendArgs {
   int32_t kv_blocks, q_chunks;
 };
 
-// EPL: entries a lane (2 for dc > 64).  Heads of up to 32 entries share a wave.
+// EPL: entries a lane (2 for dc > 64, since a head's values meet in one wave to
+// be found finite).  Heads of up to 32 entries share a wave.
 template <int EPL>
 __device__ void append_kv(const AppendArgs& a) {
   const int lane = threadIdx.x & 63, dc = a.c.dc;

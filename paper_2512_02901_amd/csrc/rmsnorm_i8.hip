@@ -6,6 +6,10 @@
 // float32 as well (rounding is monotonic): the sum and the maximum come out
 // of one reduction, and a token's t stay in registers from the load to q.
 // The squares are summed in double: no finite token overflows.
+//
+// What bounds it is memory, 26 bytes an entry with delta and h (8 + 8 + 8 + 2):
+// 2048 tokens of 2048 entries 20.2 us (5.4 TB/s, a plain copy's rate); 77 of 1500
+// 4.1 us and one of 2048 3.0 us, an empty launch and two trips to memory.
 #include <float.h>
 
 #include "common.h"
@@ -193,6 +197,15 @@ extern "C" fairy2i_status fairy2i_add_rmsnorm_i8(const float* x, const float* de
   if (B <= 0 || n <= 0 || B > INT32_MAX || n > ((int64_t)1 << 24) || !(eps > 0.0f) || eps > FLT_MAX) return FAIRY2I_ERR_SHAPE;
   auto s = static_cast<hipStream_t>(stream);
   auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
+  // As many threads as take a token at a group each, up to 512, then up to four
+  // groups each.  us for 1 | 2048 tokens (a launch in a graph is about 2 of them):
+  //   n = 256   64 x 1 3.3 | 5.0    256 x 1 3.3 | 6.2     512 x 1 3.5 | 8.9
+  //   n = 1024 256 x 1 3.5 | 11.9    64 x 4 4.6 | 12.0    512 x 1 3.5 | 13.7
+  //   n = 2048 512 x 1 3.9 | 20.8   256 x 2 4.1 | 20.1   1024 x 1 4.2 | 22.9
+  //   n = 4096 512 x 2 4.6 | 36.6   512 x 4 4.8 | 38.1   1024 x 1 5.0 | 37.4
+  //   n = 8192 512 x 4 6.2 | 91.1  1024 x 2 6.6 | 90.4
+  // The form for any size reads a token twice: 4.8 | 14.7 at n = 1024, 18.5 | 108
+  // at n = 8192.
   if (n % 4 != 0 || n > 8192 || ((at(x) | at(delta) | at(gain) | at(h)) & 15) != 0 || (at(q) & 7) != 0)
     hipLaunchKernelGGL(add_rmsnorm_i8_any_kernel, dim3((unsigned)B), dim3(256), 0, s,
                        reinterpret_cast<const float2*>(x), reinterpret_cast<const float2*>(delta), gain, eps, n,
@@ -203,6 +216,8 @@ extern "C" fairy2i_status fairy2i_add_rmsnorm_i8(const float* x, const float* de
     launch_vec<256, 1>(x, delta, gain, eps, B, n, h, q, x_scale, s);
   else if (n <= 2048)
     launch_vec<512, 1>(x, delta, gain, eps, B, n, h, q, x_scale, s);
+  else if (n <= 4096)
+    launch_vec<512, 2>(x, delta, gain, eps, B, n, h, q, x_scale, s);
   else
     launch_vec<512, 4>(x, delta, gain, eps, B, n, h, q, x_scale, s);
   return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;

@@ -65,6 +65,8 @@ constexpr int kWideRows = 128;
 constexpr int resident(int nb, bool wide) { return kCus * (wide ? (nb <= 2 ? 3 : 2) : nb <= 2 ? 4 : nb <= 4 ? 3 : 2); }
 constexpr int kMaxItems = 4 * kCus;
 constexpr int kMinChunk = 8;      // tiles: two a wave
+constexpr int kMostTiles = 1 << 25;  // 2^30 positions
+constexpr int kClasses = 9;
 
 // The running reference of a row's weights is raised once a score is 2^8 past
 // it: raising it at every new maximum scales 64 sums a lane in nearly every
@@ -136,13 +138,22 @@ struct Item {
   KvSeq s;
 };
 
-// Chunks are as long as makes `target` of them over all sequences, and
-// kMinChunk tiles at least.  Whole chunks go first, what is left of the
-// sequences after them, so that the short ones fill the gaps; of a sequence's,
-// the last row tiles (which see most) go first and heads are neighbours.
+// One or two blocks of eight waves a CU, the longest first: the second ones in
+// the other order, so that a CU's two are as long together as any other's.
 template <int RB>
-__device__ inline bool find_item(const AttnArgs& a, int at, int target, Item& it) {
+__device__ inline int in_turn(int at, int items) {
+  return RB == kSharedWaves && items > kCus && items <= 2 * kCus && at >= kCus && at < items ? items - 1 - (at - kCus) : at;
+}
+
+// Chunks are as long as makes `target` of them over all sequences, and
+// kMinChunk tiles at least.  Whole chunks go first, then what is left of the
+// sequences in kClasses - 1 classes of its length, the longest first, so that the
+// short ones fill the gaps; of a sequence's, the last row tiles (which see most)
+// go first and heads are neighbours.  `hist`: kClasses words of LDS for the wave.
+template <int RB>
+__device__ inline bool find_item(const AttnArgs& a, int at, int target, int* hist, Item& it) {
   const int lane = threadIdx.x & 63, n = a.b.n_seqs, kv = a.c.kv_heads;
+  if (n > 1 && lane < kClasses) hist[lane] = 0;
   auto seq = [&](int i) { return i < n ? kv_seq(a.b, a.c, i) : KvSeq{0, 0, 0}; };
   const KvSeq first = seq(lane);
   int64_t work = (int64_t)kv_tiles(first.len) * row_tiles<RB>(a, first);
@@ -153,42 +164,65 @@ __device__ inline bool find_item(const AttnArgs& a, int at, int target, Item& it
   // of one sequence, its lane's number; of more, the last lane's sum
   auto total = [&](auto v) { return n > 1 ? of_lane(up_to(v), 63) : of_lane(v, 0); };
   work = total(work);
-  const int ct = max(kMinChunk, (int)((work * kv + target - 1) / target));
-  // items of a sequence's whole chunks, and all of them (one, if it is empty)
-  auto whole_of = [&](const KvSeq& s) { return kv_tiles(s.len) / ct * row_tiles<RB>(a, s) * kv; };
-  auto all_of = [&](const KvSeq& s) { return max(1, (kv_tiles(s.len) + ct - 1) / ct) * row_tiles<RB>(a, s) * kv; };
-  int whole = whole_of(first);
-  for (int i = 64 + lane; i < n; i += 64) whole += whole_of(seq(i));
-  whole = total(whole);
-  if (RB == kSharedWaves) {
-    // One or two blocks a CU, the longest first: the second ones in the other
-    // order, so that a CU's two are as long together as any other's.
-    int all = all_of(first);
-    for (int i = 64 + lane; i < n; i += 64) all += all_of(seq(i));
-    all = total(all);
-    if (all > kCus && all <= 2 * kCus && at >= kCus && at < all) at = all - 1 - (at - kCus);
+  const int ct = (int)max((int64_t)kMinChunk, min((work * kv + target - 1) / target, (int64_t)kMostTiles));
+  const float classes = (kClasses - 1.0f) / ct;
+  struct Share {
+    int row_tiles, chunks, whole, rest, kind;  // whole chunks of a row tile; items of whole chunks and others, whose class
+  };
+  auto share_of = [&](const KvSeq& s) {
+    const int t = kv_tiles(s.len), chunks = t / ct, left = t - chunks * ct, rt = row_tiles<RB>(a, s);
+    return Share{rt, chunks, chunks * rt * kv, left > 0 || chunks == 0 ? rt * kv : 0,
+                 kClasses - 1 - min((int)(left * classes), kClasses - 2)};
+  };
+  const Share mine = share_of(first);
+  int kind, start;  // the item's class, 0 for whole chunks; items of the classes before
+  if (n > 1) {
+    int whole = mine.whole;
+    auto add = [&](const Share& x) {
+      if (x.rest) __hip_atomic_fetch_add(hist + x.kind, x.rest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    };
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    add(mine);
+    for (int i = 64 + lane; i < n; i += 64) {
+      const Share x = share_of(seq(i));
+      whole += x.whole;
+      add(x);
+    }
+    whole = total(whole);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int here = lane == 0 ? whole : lane < kClasses ? hist[lane] : 0, upto = up_to(here);
+    at = in_turn<RB>(at, of_lane(upto, 63));
+    const uint64_t past = __ballot(upto > at);
+    if (past == 0) return false;
+    kind = __builtin_ctzll(past);
+    start = of_lane(upto - here, kind);
+  } else {
+    start = of_lane(mine.whole, 0);
+    at = in_turn<RB>(at, start + of_lane(mine.rest, 0));
+    kind = at < start ? 0 : of_lane(mine.kind, 0);
+    if (kind == 0) start = 0;
   }
-  const bool rest = at >= whole;
-  if (rest) at -= whole;
-  int before = 0, ids = 0;  // items of the sequences before: of this kind, and all
+  at -= start;
+  int before = 0, ids = 0;  // items of the sequences before: of this class, and all
   for (int i0 = 0; i0 < n; i0 += 64) {
     const KvSeq s = i0 == 0 ? first : seq(i0 + lane);
-    const int all = all_of(s), mine = rest ? all - whole_of(s) : whole_of(s);
-    const int upto = n > 1 ? up_to(mine) : mine, ids_upto = n > 1 ? up_to(all) : all;
+    const Share x = i0 == 0 ? mine : share_of(s);
+    const int all = x.whole + x.rest, here = kind == 0 ? x.whole : x.kind == kind ? x.rest : 0;
+    const int upto = n > 1 ? up_to(here) : here, ids_upto = n > 1 ? up_to(all) : all;
     const uint64_t past = __ballot(before + upto > at);
     if (past != 0) {
       const int w = __builtin_ctzll(past);
       auto of = [&](int v) { return of_lane(v, w); };
-      const int local = at - before - of(upto - mine), rt = of(row_tiles<RB>(a, s)), chunks = of(kv_tiles(s.len)) / ct;
-      const int per = rest ? 1 : chunks;  // chunks of this kind that a row tile has
+      const int local = at - before - of(upto - here), rt = of(x.row_tiles), chunks = of(x.chunks);
+      const int per = kind == 0 ? chunks : 1;  // chunks of this class that a row tile has
       const int hc = local / kv, t = hc / max(per, 1);
       it.seq = i0 + w;
       it.s = {of(s.row0), of(s.n), of(s.len)};
       it.head = local - hc * kv;
-      it.chunk = rest ? chunks : hc - t * per;
+      it.chunk = kind == 0 ? hc - t * per : chunks;
       it.tile = rt - 1 - t;
       it.chunk_tiles = ct;
-      it.id = ids + of(ids_upto - all) + (t * (of(all) / max(rt * kv, 1)) + it.chunk) * kv + it.head;
+      it.id = ids + of(ids_upto - all) + (t * (chunks + (of(x.rest) != 0)) + it.chunk) * kv + it.head;
       return local >= 0 && it.tile >= 0 && it.id < a.items;  // not so only for a cu_new that decreases
     }
     before += __builtin_amdgcn_readlane(upto, 63);
@@ -765,7 +799,7 @@ __device__ inline Item block_item(const AttnArgs& a, int target, char* lds) {
   Item it{};
   Item* found = reinterpret_cast<Item*>(lds);
   if (threadIdx.x < 64) {
-    if (!find_item<RB>(a, blockIdx.x, target, it)) it.seq = -1;
+    if (!find_item<RB>(a, blockIdx.x, target, reinterpret_cast<int*>(lds + sizeof(Item)), it)) it.seq = -1;
     if (threadIdx.x == 0) *found = it;
   }
   __syncthreads();
@@ -780,7 +814,7 @@ __device__ inline Item block_item(const AttnArgs& a, int target, char* lds) {
 template <int NB, int RB>
 __global__ __launch_bounds__(kThreads, RB > 1 ? 2 : 1) void kv_attend_kernel(AttnArgs a) {
   __shared__ __align__(16) char lds[kLds<NB, RB>];
-  static_assert(sizeof(Item) <= kLds<NB, RB>);
+  static_assert(sizeof(Item) + 4 * kClasses <= kLds<NB, RB>);
   const Item it = block_item<RB>(a, resident(NB, RB > 1), lds);
   if (it.seq >= 0) attend_tile<NB, RB>(a, it, lds);
 }

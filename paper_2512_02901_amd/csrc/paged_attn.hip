@@ -17,8 +17,8 @@
 // What bounds it, with us of a whole call:
 //  - a few tokens a sequence: memory.  One token over 262144 positions, 32 heads
 //    on 8 of dc = 64 (285 MB), 60 us, its first kernel 53 (5.4 TB/s, a copy's
-//    rate); 63 sequences of up to 8192 (302 MB) 76, 72 (4.2 TB/s: blocks start with
-//    a chain of lookups, about 8 us under load, that their own loads wait for);
+//    rate); 63 sequences of up to 8192 (302 MB) 67, 62 (4.8 TB/s: blocks start with
+//    a chain of lookups, about 6 us under load, that their own loads wait for);
 //  - short contexts: that chain and the join's; one token over 40 positions 4.4,
 //    over 2048 (32 heads) 9.2, of which the join 3.0;
 //  - prompts: the vector work of softmax and weights, issued beside the matrix
@@ -58,13 +58,21 @@ constexpr int wide_blocks(int nb) { return shared(nb) ? kSharedWaves : wide_rb(n
 // positions: dc = 64 32 18.6 | 21.5, 128 32.2 | 32.7, 256 52 | 46.
 constexpr int kWideRows = 128;
 // Blocks that are resident at once, which a call is cut into where its rows
-// alone are fewer: by the kernels' registers.  More items than that, and the
-// last ones run beside empty CUs: one token over 262144 positions, 32 heads on
-// 8 of dc = 64 (768 resident), us: 512 64, 768 64, 1024 72, 1536 74, 3072 94;
-// dc = 128 (512), 8 sequences up to 16384: 28, 35, 35, 36, 40.
+// alone are fewer: by the kernels' registers.  us for 512 | 768 | 1024 items:
+// 32 heads on 8, dc = 64 (768 resident), one token over 262144 positions 63 | 61 |
+// 65, 31 over up to 16384 80 | 78 | 80, 15 over 8192 33.7 | 32.7 | 35; 16 on 16,
+// dc = 32 (1024), 31 over up to 16384 97 | 84 | 82; 16 on 4, dc = 128 (512), 7 over
+// up to 16384 25.3 | 30.4 (256: 26.4), 64 over 4096 57 | 62 (65).
 constexpr int resident(int nb, bool wide) { return kCus * (wide ? (nb <= 2 ? 3 : 2) : nb <= 2 ? 4 : nb <= 4 ? 3 : 2); }
 constexpr int kMaxItems = 4 * kCus;
-constexpr int kMinChunk = 8;      // tiles: two a wave
+// Tiles of a chunk at least, by row blocks of a tile: shorter ones cost a join and
+// lookups for little work.  us for 4 | 8 | 16 | 32 tiles: one block, one token over
+// 2048, 32 heads on 32 (dc = 64) 9.7 | 9.1 | 10.4, 6 x up to 5 over up to 4099, 8 on
+// 2 (dc = 128) 17.6 | 15.2 | 16.4; two, a prompt of 600, 16 on 4 (dc = 32) 8: 13.7 |
+// 12.5 | 10.4, 128 tokens over 800 10.6 | 11.9 | 11.3; eight, 3 prompts of up to 400,
+// 32 on 8 (dc = 64) 26.6 | 18.7 | 18.6, 256 over 1500 29 | 26 | 37.6, a prompt of
+// 600 21.7 | 24.8 | 22.1.
+constexpr int min_chunk(int rb) { return rb == 1 ? 8 : rb == kSharedWaves ? 16 : 32; }
 constexpr int kMostTiles = 1 << 25;  // 2^30 positions
 constexpr int kClasses = 9;
 
@@ -146,10 +154,12 @@ __device__ inline int in_turn(int at, int items) {
 }
 
 // Chunks are as long as makes `target` of them over all sequences, and
-// kMinChunk tiles at least.  Whole chunks go first, then what is left of the
+// min_chunk tiles at least.  Whole chunks go first, then what is left of the
 // sequences in kClasses - 1 classes of its length, the longest first, so that the
 // short ones fill the gaps; of a sequence's, the last row tiles (which see most)
-// go first and heads are neighbours.  `hist`: kClasses words of LDS for the wave.
+// go first and heads are neighbours.  (In the sequences' own order 31 tokens over
+// up to 16384 positions, 32 heads on 8, dc = 64, took 92 us for 77, 63 over up to
+// 8192 77 for 67.)  `hist`: kClasses words of LDS for the wave.
 template <int RB>
 __device__ inline bool find_item(const AttnArgs& a, int at, int target, int* hist, Item& it) {
   const int lane = threadIdx.x & 63, n = a.b.n_seqs, kv = a.c.kv_heads;
@@ -164,7 +174,7 @@ __device__ inline bool find_item(const AttnArgs& a, int at, int target, int* his
   // of one sequence, its lane's number; of more, the last lane's sum
   auto total = [&](auto v) { return n > 1 ? of_lane(up_to(v), 63) : of_lane(v, 0); };
   work = total(work);
-  const int ct = (int)max((int64_t)kMinChunk, min((work * kv + target - 1) / target, (int64_t)kMostTiles));
+  const int ct = (int)max((int64_t)min_chunk(RB), min((work * kv + target - 1) / target, (int64_t)kMostTiles));
   const float classes = (kClasses - 1.0f) / ct;
   struct Share {
     int row_tiles, chunks, whole, rest, kind;  // whole chunks of a row tile; items of whole chunks and others, whose class
@@ -1085,7 +1095,7 @@ fairy2i_status fairy2i_kv_attend(const fairy2i_kv_cache* cache, const fairy2i_kv
   a.part = reinterpret_cast<float*>(ws);
   a.ml = reinterpret_cast<float2*>(ws + l.part);
   a.meta = reinterpret_cast<int2*>(ws + l.part + l.ml);
-  const bool one_chunk = (int64_t)batch->max_pages * cache->page_size <= kMinChunk * kKvTile;
+  const bool one_chunk = (int64_t)batch->max_pages * cache->page_size <= min_chunk((int)l.tile_rows / kRows) * kKvTile;
   auto s = static_cast<hipStream_t>(stream);
   switch (cache->dc / 16) {
     case 1: launch<1>(a, l, one_chunk, s); break;

@@ -60,7 +60,7 @@ constexpr int kWideRows = 128;
 // Blocks that are resident at once, which a call is cut into where its rows
 // alone are fewer: by the kernels' registers.  us for 512 | 768 | 1024 items:
 // 32 heads on 8, dc = 64 (768 resident), one token over 262144 positions 63 | 61 |
-// 65, 31 over up to 16384 80 | 78 | 80, 15 over 8192 33.7 | 32.7 | 35; 16 on 16,
+// 65, 31 over up to 16384 80 | 78 | 80, 16 over 8192 33.7 | 32.7 | 35; 16 on 16,
 // dc = 32 (1024), 31 over up to 16384 97 | 84 | 82; 16 on 4, dc = 128 (512), 7 over
 // up to 16384 25.3 | 30.4 (256: 26.4), 64 over 4096 57 | 62 (65).
 constexpr int resident(int nb, bool wide) { return kCus * (wide ? (nb <= 2 ? 3 : 2) : nb <= 2 ? 4 : nb <= 4 ? 3 : 2); }
@@ -447,7 +447,7 @@ __device__ inline void weigh(const f32x4 (&s)[H], float scale, Softmax& x, f32x4
   }
 }
 
-// p as the sum of two bf16 numbers each (2^-17 relative).
+// p as the sum of two bf16 numbers each (2^-16 relative).
 __device__ inline void split_bf16(const float* p, bf16x8& ph, bf16x8& pl) {
   u32x4 hi, lo;
 #pragma unroll

@@ -762,8 +762,9 @@ fairy2i_status fairy2i_add_rmsnorm_i8(const float* x, const float* delta, const 
  *           page_size * m .. page_size * (m + 1) - 1 is pages[i][m].
  * The arrays are read by the kernels, nothing is copied to the host, so a
  * captured graph follows what they hold.  They are bounded before use: rows
- * outside [0, n_new), positions past max_pages * page_size and page numbers
- * outside [0, n_pages) are neither read nor written.
+ * outside [0, n_new), positions below 0 or from max_pages * page_size on (the
+ * table's end) and page numbers outside [0, n_pages) are neither read nor
+ * written, and the other rows stay at their positions.
  */
 typedef struct fairy2i_kv_cache {
   uint8_t* data;
@@ -805,8 +806,9 @@ fairy2i_status fairy2i_rope_table(int64_t n_pos, int32_t dc, double base, float*
  * apart; q: rows of n_heads * dc entries, q_ld apart (so all three may be
  * columns of one product).  q_out: bf16 pairs [n_new][n_heads][dc][2].  q and
  * q_out may both be NULL.  rope: float32 [rope_len][dc][2]
- * (fairy2i_rope_table).  A row at a position past rope_len is not stored, its
- * q_out is NaN.  Each position is to be written by one row of a call.
+ * (fairy2i_rope_table).  A row at a position from rope_len or the table's end
+ * on is not stored, its q_out is NaN.  Each position is to be written by one
+ * row of a call.
  * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for a cache of unsupported
  * sizes, n_seqs outside [1, 2^20], n_new outside [1, 2^26], max_pages < 1,
  * max_pages * page_size above 2^30, n_heads, rope_len < 1 or an ld below its
@@ -820,7 +822,8 @@ fairy2i_status fairy2i_kv_append(const fairy2i_kv_cache* cache, const fairy2i_kv
 /*
  * The values that the cache stands for at the positions of a batch's rows
  * (with cu_new over whole sequences: all of them).  k_out, v_out: bf16 pairs
- * [n_new][n_kv_heads][dc][2], exact.  Positions without a page read as NaN.
+ * [n_new][n_kv_heads][dc][2], exact.  Positions without a page (those outside
+ * the table among them) read as NaN.
  * Errors: as fairy2i_kv_append.
  */
 fairy2i_status fairy2i_kv_read(const fairy2i_kv_cache* cache, const fairy2i_kv_batch* batch, void* k_out, void* v_out,
@@ -829,7 +832,7 @@ fairy2i_status fairy2i_kv_read(const fairy2i_kv_cache* cache, const fairy2i_kv_b
 /*
  * Hermitian-score attention (Sec. 3.1, Eq. hermitian-score) of a batch's rows
  * over the cache, causal: row j of a sequence sees positions 0 .. lens - rows
- * + j.  With query head h reading key head h / (n_heads / n_kv_heads):
+ * + j, as far as the table goes.  With query head h reading key head h / (n_heads / n_kv_heads):
  *   s_m = scale * Re(q^H k_m),  p = softmax(s),  out = sum_m p_m v_m.
  * q: bf16 pairs [n_new][n_heads][dc][2], rotated (fairy2i_kv_append's q_out);
  * out: the same shape, rounded to bf16 once; it may be q's memory only where

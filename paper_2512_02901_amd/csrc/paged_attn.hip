@@ -164,7 +164,7 @@ template <int RB>
 __device__ inline bool find_item(const AttnArgs& a, int at, int target, int* hist, Item& it) {
   const int lane = threadIdx.x & 63, n = a.b.n_seqs, kv = a.c.kv_heads;
   if (n > 1 && lane < kClasses) hist[lane] = 0;
-  auto seq = [&](int i) { return i < n ? kv_seq(a.b, a.c, i) : KvSeq{0, 0, 0}; };
+  auto seq = [&](int i) { return i < n ? kv_seq(a.b, a.c, i) : KvSeq{0, 0, 0, 0}; };
   const KvSeq first = seq(lane);
   int64_t work = (int64_t)kv_tiles(first.len) * row_tiles<RB>(a, first);
   for (int i = 64 + lane; i < n; i += 64) {
@@ -227,7 +227,7 @@ __device__ inline bool find_item(const AttnArgs& a, int at, int target, int* his
       const int per = kind == 0 ? chunks : 1;  // chunks of this class that a row tile has
       const int hc = local / kv, t = hc / max(per, 1);
       it.seq = i0 + w;
-      it.s = {of(s.row0), of(s.n), of(s.len)};
+      it.s = {of(s.row0), of(s.n), of(s.p0), of(s.len)};
       it.head = local - hc * kv;
       it.chunk = kind == 0 ? hc - t * per : chunks;
       it.tile = rt - 1 - t;
@@ -472,10 +472,10 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int r = lane & 15, g = lane >> 4;
   const int rows = it.s.n * a.group, row0 = it.tile * kTileRows;
-  const int p0 = it.s.len - it.s.n;  // position of the first new token
+  const int p0 = it.s.p0;  // position of the first new token
   // the least and the most that any row of the tile sees
   const int least = p0 + row0 / a.group;
-  const int most = p0 + (min(row0 + kTileRows, rows) - 1) / a.group;
+  const int most = min(p0 + (min(row0 + kTileRows, rows) - 1) / a.group, it.s.len - 1);
   const int tiles = kv_tiles(most + 1), chunks = max(1, (tiles + it.chunk_tiles - 1) / it.chunk_tiles);
   if (it.chunk == 0 && threadIdx.x < RB && row0 + kRows * (int)threadIdx.x < rows)
     a.meta[(int64_t)(row_slot(a, it.seq) + it.tile * RB + threadIdx.x) * a.c.kv_heads + it.head] =
@@ -687,8 +687,8 @@ __device__ inline void attend_shared(const AttnArgs& a, const Item& it, char* ld
   };
   int* there = reinterpret_cast<int*>(lds + R * 4096 * NB);  // whether the table has the round's tiles
   const int rows = it.s.n * a.group, tile0 = it.tile * kRows * W, row0 = tile0 + wave * kRows;
-  const int p0 = it.s.len - it.s.n;  // position of the first new token
-  const int tile_most = p0 + (min(tile0 + kRows * W, rows) - 1) / a.group;
+  const int p0 = it.s.p0;  // position of the first new token
+  const int tile_most = min(p0 + (min(tile0 + kRows * W, rows) - 1) / a.group, it.s.len - 1);
   const int tiles = kv_tiles(tile_most + 1), chunks = max(1, (tiles + it.chunk_tiles - 1) / it.chunk_tiles);
   if (it.chunk == 0 && threadIdx.x < W && tile0 + kRows * (int)threadIdx.x < rows)
     a.meta[(int64_t)(row_slot(a, it.seq) + it.tile * W + threadIdx.x) * a.c.kv_heads + it.head] =
@@ -697,7 +697,7 @@ __device__ inline void attend_shared(const AttnArgs& a, const Item& it, char* ld
   const int t_end = min(tiles, (it.chunk + 1) * it.chunk_tiles);
   // the least and the most that any of the wave's rows sees
   const int least = p0 + row0 / a.group;
-  const int most = row0 < rows ? p0 + (min(row0 + kRows, rows) - 1) / a.group : -1;
+  const int most = row0 < rows ? min(p0 + (min(row0 + kRows, rows) - 1) / a.group, it.s.len - 1) : -1;
   const int last = min(p0 + (row0 + r) / a.group, most);  // rows past the end compute what nobody stores
   bf16x8 q[NB];
   load_q<NB>(a, it, row0, q);

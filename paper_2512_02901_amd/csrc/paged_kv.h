@@ -41,9 +41,14 @@ struct KvBatch {
   int32_t n_new;          // rows of q, k, v
 };
 
+// Rows that q, k and v do not have (cu_new past n_new) and positions that the
+// table does not have (lens past it) are left out; the others stay in place, so p0
+// may lie outside [0, len).
 struct KvSeq {
-  int row0, n, len;  // first row, rows, length after them
+  int row0, n, p0, len;  // first row, rows, the first one's position, positions of the table up to the last one's
 };
+
+constexpr int kKvMaxNew = 1 << 26, kKvMaxLen = 1 << 30;  // rows of a call, positions of a table
 
 #if defined(__HIPCC__)
 
@@ -52,8 +57,12 @@ __device__ inline int kv_row(const KvBatch& b, int i) { return min(max(b.cu_new[
 __device__ inline KvSeq kv_seq(const KvBatch& b, const KvCache& c, int i) {
   KvSeq s;
   s.row0 = kv_row(b, i);
-  s.n = max(kv_row(b, i + 1) - s.row0, 0);
-  s.len = (int)min((int64_t)max(b.lens[i], 0), (int64_t)b.max_pages * c.page_size);
+  const int end = b.cu_new[i + 1];  // a row there would stand at lens[i]
+  s.n = max(min(max(end, 0), b.n_new) - s.row0, 0);
+  // saturated and bounded to where all rows are outside as well
+  const int p0 = __builtin_elementwise_add_sat(__builtin_elementwise_sub_sat(b.lens[i], end), s.row0);
+  s.p0 = min(max(p0, -kKvMaxNew), kKvMaxLen);
+  s.len = min(max(s.p0 + s.n, 0), b.max_pages * c.page_size);
   return s;
 }
 
@@ -97,8 +106,8 @@ inline fairy2i_status kv_check(const fairy2i_kv_cache* c, const fairy2i_kv_batch
   if (!c || !b || !c->data || !b->pages || !b->cu_new || !b->lens) return FAIRY2I_ERR_NULL;
   if (fairy2i_kv_cache_bytes(c->n_pages, c->page_size, c->n_kv_heads, c->dc) == 0) return FAIRY2I_ERR_SHAPE;
   if ((reinterpret_cast<uintptr_t>(c->data) & 15) != 0) return FAIRY2I_ERR_UNSUPPORTED;
-  if (b->n_seqs < 1 || b->n_seqs > (1 << 20) || b->max_pages < 1 || b->n_new < 1 || b->n_new > (1 << 26) ||
-      (int64_t)b->max_pages * c->page_size > ((int64_t)1 << 30))
+  if (b->n_seqs < 1 || b->n_seqs > (1 << 20) || b->max_pages < 1 || b->n_new < 1 || b->n_new > kKvMaxNew ||
+      (int64_t)b->max_pages * c->page_size > kKvMaxLen)
     return FAIRY2I_ERR_SHAPE;
   return FAIRY2I_OK;
 }

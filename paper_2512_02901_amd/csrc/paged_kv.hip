@@ -105,7 +105,7 @@ __device__ void append_kv(const AppendArgs& a) {
   const int i = kv_find(a.b.n_seqs, slot, [&](int s) { return slot_of(a.b, s); });
   if (i < 0) return;
   const KvSeq s = kv_seq(a.b, a.c, i);
-  const int p0 = s.len - s.n, group = (max(p0, 0) >> 2) + slot - slot_of(a.b, i), u0 = 4 * group % kKvTile;
+  const int group = (s.p0 >> 2) + slot - slot_of(a.b, i), u0 = 4 * group % kKvTile;
   if (s.n == 0 || group < 0 || 4 * (int64_t)group >= s.len) return;
   const int hpw = dc <= 32 ? 64 / dc : 1;  // heads a wave
   const int sub = hpw > 1 ? lane / dc : 0, h = hg * hpw + sub;
@@ -117,7 +117,7 @@ __device__ void append_kv(const AppendArgs& a) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int p = 4 * group + j;
-    if (p >= p0 && p < s.len && p < a.rope_len) valid |= 1u << j;
+    if (p >= s.p0 && p < s.len && p < a.rope_len) valid |= 1u << j;
   }
   float2 kx[EPL][4], vx[EPL][4];
 #pragma unroll
@@ -127,7 +127,7 @@ __device__ void append_kv(const AppendArgs& a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const bool load = mine && (valid >> j & 1);
-      const int64_t row = s.row0 + (4 * group + j - p0);
+      const int64_t row = s.row0 + (4 * group + j - s.p0);
       const float2 zero = make_float2(0.0f, 0.0f);
       const float2 cs = load ? a.rope[(int64_t)(4 * group + j) * dc + e] : zero;
       const float2 k = load ? a.k[row * a.k_ld + (int64_t)h * dc + e] : zero;
@@ -209,7 +209,7 @@ __device__ void rotate_q(const AppendArgs& a) {
   int64_t p = -1;
   if (i >= 0) {
     const KvSeq s = kv_seq(a.b, a.c, i);
-    if (row < s.row0 + s.n) p = s.len - s.n + (row - s.row0);
+    if (row < s.row0 + s.n && s.p0 + (row - s.row0) < s.len) p = s.p0 + (row - s.row0);
   }
   const bool known = p >= 0 && p < a.rope_len;
   const float2* turns = a.rope + (known ? p : 0) * a.c.dc;
@@ -250,13 +250,15 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
   const int i = kv_find(a.b.n_seqs, slot, [&](int s) { return slot_of(a.b, s); });
   if (i < 0) return;
   const KvSeq s = kv_seq(a.b, a.c, i);
-  const int p0 = s.len - s.n, group = (max(p0, 0) >> 2) + slot - slot_of(a.b, i), u0 = 4 * group % kKvTile;
-  if (s.n == 0 || group < 0 || 4 * (int64_t)group >= s.len) return;
+  const int group = (s.p0 >> 2) + slot - slot_of(a.b, i), u0 = 4 * group & (kKvTile - 1);
+  if (s.n == 0 || 4 * group >= s.p0 + s.n) return;
   const int hpw = dc <= 32 ? 64 / dc : 1;
   const int sub = hpw > 1 ? lane / dc : 0, h = hg * hpw + sub;
   const KvTile t(dc / 16);
   const bool head = h < a.c.kv_heads;
-  const uint8_t* tile = kv_tile(a.c, a.b, i, 4 * group, head ? h : 0, t.bytes);
+  // before position 0 and past the table there is no page either
+  const bool inside = group >= 0 && 4 * (int64_t)group < s.len;
+  const uint8_t* tile = inside ? kv_tile(a.c, a.b, i, 4 * group, head ? h : 0, t.bytes) : nullptr;
 #pragma unroll
   for (int x = 0; x < EPL; ++x) {
     const int e = lane - sub * dc + 64 * x, b = e / 16, r = e % 16;
@@ -278,9 +280,9 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
     };
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int p = 4 * group + j;
-      if (mine && p >= p0 && p < s.len) {
-        const int64_t at = ((int64_t)(s.row0 + (p - p0)) * a.c.kv_heads + h) * dc + e;
+      const int64_t row = 4 * (int64_t)group + j - s.p0;
+      if (mine && row >= 0 && row < s.n) {
+        const int64_t at = ((s.row0 + row) * a.c.kv_heads + h) * dc + e;
         a.k[at] = pair(kd >> (8 * j), ks[j]);
         a.v[at] = pair(vd >> (8 * j), vs[j]);
       }

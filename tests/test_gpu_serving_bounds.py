@@ -1,0 +1,103 @@
+"""The serving operators at the ends of what their arrays may say: lengths past
+the page table, rows past the tensors.  The
+expectations are oracle/serving.py's, or a call's own for arrays that name the
+same rows and positions; tolerances are tests/test_gpu_serving.py's."""
+import numpy as np
+import pytest
+
+from oracle import serving as sv
+from test_gpu_serving import Batch, attend_check, dev, expect_append, host, queries, random_c, rope_of
+
+pytestmark = pytest.mark.gpu
+
+
+def same(x, y):
+    """Equal bit for bit, a NaN to any NaN."""
+    import torch
+    return torch.equal(torch.isnan(x), torch.isnan(y)) and torch.equal(torch.nan_to_num(x), torch.nan_to_num(y))
+
+
+# ------------------------------------------------ lengths past the page table
+
+CAPACITY = 192
+PAST = {
+    "one_past": [(1, CAPACITY + 1)],
+    "three_around": [(3, CAPACITY + 1)],
+    "some_past": [(1, CAPACITY), (3, CAPACITY + 2), (1, CAPACITY + 1), (0, CAPACITY + 9), (5, CAPACITY + 300), (2, 7)],
+    "prompt": [(CAPACITY + 70, CAPACITY + 70)],
+    "prompts": [(150, CAPACITY + 31), (170, 170)],
+}
+
+
+@pytest.mark.parametrize("seqs", list(PAST))
+@pytest.mark.parametrize("kv, heads, dc, page", [(3, 3, 16, 32), (2, 4, 32, 64), (1, 2, 48, 96), (2, 4, 64, 32), (1, 4, 128, 192)])
+def test_rows_past_the_table_are_left_out(gpu, seqs, kv, heads, dc, page):
+    """They are not stored, their q and what is read of them are NaN, and the
+    other rows stand where they stand: a call with a wider table without pages there."""
+    import torch
+    b = Batch(PAST[seqs], kv, dc, page, gpu, seed=31).fill()
+    width = CAPACITY // page
+    b.table[:, width:] = -1
+    b.dev()
+    t = (dev(b.table[:, :width], gpu), *b.t[1:])
+    rope = rope_of(b.width * page, dc, gpu)
+    q, k, v = (random_c(b.rng, b.N, h, dc) for h in (heads, kv, kv))
+    got_q = b.kvc.append(dev(k, gpu), dev(v, gpu), *t, rope, q=dev(q, gpu))
+    np.testing.assert_array_equal(host(b.data), expect_append(b, k, v, host(rope)))
+    pos = np.concatenate([np.arange(c - n, c) for n, c in b.seqs])
+    inside = pos < CAPACITY
+    nan = np.isnan(host(got_q))
+    assert nan[~inside].all() and not nan[inside].any()
+    turn = host(rope)
+    want_q = sv.rotate(q, turn[pos][:, None, :, 0], turn[pos][:, None, :, 1])
+    assert torch.equal(got_q.cpu()[inside], torch.from_numpy(want_q).bfloat16()[inside])
+    out = tuple(torch.full((b.N, kv, dc, 2), 7.0, dtype=torch.bfloat16, device=gpu) for _ in range(2))
+    b.kvc.read(*t, b.N, out=out)
+    for i, (n, length) in enumerate(b.seqs):
+        want = sv.read(host(b.data), page, kv, dc, b.table[i], length)[:, length - n:]
+        np.testing.assert_array_equal(host(out[0])[b.cu[i]:b.cu[i + 1]], want[0])
+        np.testing.assert_array_equal(host(out[1])[b.cu[i]:b.cu[i + 1]], want[1])
+    b.cache = host(b.data)
+    qb = queries(b, heads)
+    attend_check(b, heads, qb.double().numpy(), b.kvc.attend(qb.to(gpu), *t), (2 * dc) ** -0.5)
+
+
+@pytest.mark.parametrize("length", [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 30 + 64])
+def test_far_lengths_touch_nothing(gpu, length):
+    """A length that no table holds: nothing is stored, and the rows see all that there is."""
+    b = Batch([(40, 64)], 2, 32, 32, gpu, seed=32).fill()
+    b.dev()
+    t = (*b.t[:2], dev(np.array([length], np.int32), gpu))
+    q, k, v = (random_c(b.rng, 40, 2, 32) for _ in range(3))
+    rope = rope_of(64, 32, gpu)
+    assert np.isnan(host(b.kvc.append(dev(k, gpu), dev(v, gpu), *t, rope, q=dev(q, gpu)))).all()
+    np.testing.assert_array_equal(host(b.data), b.cache)
+    for x in b.kvc.read(*t, 40):
+        assert np.isnan(host(x)).all()
+    qb = queries(b, 4)
+    got = host(b.kvc.attend(qb.to(gpu), *t)).astype(np.float64)
+    k, v = sv.read(b.cache, 32, 2, 32, b.table[0], 64)
+    want, size, most = sv.attend(qb.double().numpy(), k, v, 64, 64 ** -0.5)
+    assert (np.abs(got - want) <= (2.0 ** -8 + 2.0 ** -18 * most) * size + 1e-37).all()
+
+
+@pytest.mark.parametrize("cu, rows, as_cu", [([0, 3, 9], 7, [0, 3, 7]), ([-2, 3, 7], 7, [0, 3, 7]),
+                                             ([0, 3, 2 ** 31 - 101], 7, [0, 3, 7]), ([0, 140, 300], 290, [0, 140, 290])])
+@pytest.mark.parametrize("dc", [32, 64])
+def test_rows_past_the_tensors_leave_the_others_in_place(gpu, cu, rows, as_cu, dc):
+    """cu_new beyond the rows that q, k and v have: row j of a sequence still stands at lens - rows + j."""
+    import torch
+    n = [b - a for a, b in zip(as_cu, as_cu[1:])]
+    b = Batch([(n[0], n[0] + 20), (n[1], n[1] + 33)], 2, dc, 32, gpu, seed=33).fill()
+    q, k, v = (dev(random_c(b.rng, rows, 2, dc), gpu) for _ in range(3))
+    rope = rope_of(b.width * 32, dc, gpu)
+    results = []
+    for starts in (as_cu, cu):
+        b.dev()
+        lens = (b.lens + (np.array(starts[1:], np.int64) - as_cu[1:])).astype(np.int32)
+        t = (b.t[0], dev(np.array(starts, np.int32), gpu), dev(lens, gpu))
+        qr = b.kvc.append(k, v, *t, rope, q=q)
+        results.append((b.data, qr, b.kvc.attend(qr, *t), *b.kvc.read(*t, rows)))
+    for x, y in zip(*results):
+        assert same(x, y)
+    assert not torch.isnan(results[0][2]).any()

@@ -339,18 +339,16 @@ struct TileRegs {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
   }
 
-  // Scale bytes of the values from position `n` of the tile on, which nobody
-  // wrote: 2^0, so that their codes stay finite under a weight of zero.
-  __device__ inline void end_at(int n) {
-    const int g = (threadIdx.x & 63) >> 4;
+  // For a tile with positions that some row does not see: nobody may have written
+  // them, past the length or past the rotation table, and under a weight of zero
+  // what stands there has to be finite.  Scale bytes of the values above 252, the
+  // largest that is ever stored, become 252.
+  __device__ inline void make_finite() {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (16 * (j / 4) + 4 * g + j % 4 < n) continue;
-#pragma unroll
-      for (int b = 0; b < T.sb; ++b) {
-        const int i = j * T.sb + b;
-        vs[i / 4] = (vs[i / 4] & ~(0xFFu << (8 * (i % 4)))) | 127u << (8 * (i % 4));
-      }
+    for (uint32_t& w : vs) {
+      const uint32_t two = w & w << 1;                                      // bits 7, 5, 3: that and the one below
+      const uint32_t above = two & two << 2 & two << 4 & 0x80808080u;       // bits 7 to 2 all set
+      w &= ~(above >> 6 | above >> 7);
     }
   }
 };
@@ -521,7 +519,7 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
     if constexpr (RB > 1) __builtin_amdgcn_sched_barrier(0);  // the values' conversions would take registers from here on
     const int t0 = t * kKvTile;
     const bool edge = t0 + kKvTile - 1 > least;
-    if (edge && t0 + kKvTile > it.s.len) x.end_at(it.s.len - t0);
+    if (edge) x.make_finite();
     bf16x8 ph[RB], pl[RB];
 #pragma unroll
     for (int y = 0; y < RB; ++y) {
@@ -695,8 +693,8 @@ __device__ inline void attend_shared(const AttnArgs& a, const Item& it, char* ld
         make_int2(it.id * a.tile_rows + kRows * (int)threadIdx.x, chunks);
   if (it.chunk >= chunks) return;
   const int t_end = min(tiles, (it.chunk + 1) * it.chunk_tiles);
-  // the least and the most that any of the wave's rows sees
-  const int least = p0 + row0 / a.group;
+  // the least and the most that any of the wave's rows sees, and the least of all
+  const int least = p0 + row0 / a.group, tile_least = p0 + tile0 / a.group;
   const int most = row0 < rows ? min(p0 + (min(row0 + kRows, rows) - 1) / a.group, it.s.len - 1) : -1;
   const int last = min(p0 + (row0 + r) / a.group, most);  // rows past the end compute what nobody stores
   bf16x8 q[NB];
@@ -739,7 +737,7 @@ __device__ inline void attend_shared(const AttnArgs& a, const Item& it, char* ld
     __syncthreads();  // the last round's readers
     if (have) {
       const int t0 = (t_first + k + mine) * kKvTile;
-      if (t0 + kKvTile > it.s.len) x.end_at(it.s.len - t0);
+      if (t0 + kKvTile - 1 > tile_least) x.make_finite();
       if (wave % 2 == 0) convert(std::integral_constant<int, 0>{});
       else convert(std::integral_constant<int, 1>{});
     }

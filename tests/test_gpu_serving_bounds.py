@@ -1,5 +1,5 @@
 """The serving operators at the ends of what their arrays may say: lengths past
-the page table, rows past the tensors.  The
+the page table, rows past the tensors, positions that nobody stored.  The
 expectations are oracle/serving.py's, or a call's own for arrays that name the
 same rows and positions; tolerances are tests/test_gpu_serving.py's."""
 import numpy as np
@@ -101,3 +101,36 @@ def test_rows_past_the_tensors_leave_the_others_in_place(gpu, cu, rows, as_cu, d
     for x, y in zip(*results):
         assert same(x, y)
     assert not torch.isnan(results[0][2]).any()
+
+
+# ----------------------------------------------- positions that nobody stored
+
+
+@pytest.mark.parametrize("byte", [0xFF, 0xFE, 0xFD])
+@pytest.mark.parametrize("seqs, stored", [([(40, 40)], 21), ([(1, 30), (30, 60)], 45), ([(200, 200)], 150), ([(170, 300), (140, 170)], 161)])
+@pytest.mark.parametrize("kv, heads, dc, page", [(2, 2, 16, 32), (1, 3, 32, 64), (2, 2, 48, 32), (1, 2, 64, 64), (1, 2, 128, 32)])
+def test_unstored_positions_reach_no_earlier_row(gpu, kv, heads, dc, page, seqs, stored, byte):
+    """Rows past the rotation table are not stored: what their positions held
+    before (codes and scales of NaN and infinities) is not in the rows before them."""
+    import torch
+    b = Batch(seqs, kv, dc, page, gpu, seed=34)
+    b.cache[:] = byte
+    b.dev()
+    q, k, v = (random_c(b.rng, b.N, h, dc) for h in (heads, kv, kv))
+    # what stands before the new rows, then the rows as far as the table goes
+    before = [length - n for n, length in seqs]
+    rope = rope_of(b.width * page, dc, gpu)
+    old = [random_c(b.rng, sum(before), kv, dc) for _ in range(2)]
+    cu = np.concatenate([[0], np.cumsum(before)]).astype(np.int32)
+    if sum(before):
+        b.kvc.append(*(dev(x, gpu) for x in old), b.t[0], dev(cu, gpu), dev(np.array(before, np.int32), gpu), rope)
+    qr = b.kvc.append(dev(k, gpu), dev(v, gpu), *b.t, rope[:stored].contiguous(), q=dev(q, gpu))
+    got = b.kvc.attend(qr, *b.t)
+    pos = np.concatenate([np.arange(c - n, c) for n, c in seqs])
+    late = torch.from_numpy(pos >= stored)
+    assert late.any() and torch.isnan(got.cpu()[late]).all()
+    # the rows that are stored, as a call of their own over the clean cache
+    few = [(max(0, min(c, stored) - (c - n)), min(c, max(stored, c - n))) for n, c in seqs]
+    b.cache, b.seqs = host(b.data), few
+    b.cu = np.concatenate([[0], np.cumsum([n for n, _ in few])]).astype(np.int32)
+    attend_check(b, heads, host(qr)[~late.numpy()].astype(np.float64), got.cpu()[~late], (2 * dc) ** -0.5)

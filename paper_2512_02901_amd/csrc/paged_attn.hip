@@ -119,9 +119,9 @@ __device__ inline T up_to(T v) {
     const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xF, false);
     if constexpr (sizeof(T) == 8) {
       const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), ctrl, rows, 0xF, false);
-      v += (T)((uint64_t)hi << 32 | lo);
+      v += (uint64_t)hi << 32 | lo;
     } else {
-      v += (T)lo;
+      v += lo;
     }
   };
   add(std::integral_constant<int, 0x111>{});  // one lane up in rows of 16, two, four, eight
@@ -134,9 +134,10 @@ __device__ inline T up_to(T v) {
 }
 
 __device__ inline int of_lane(int v, int i) { return __builtin_amdgcn_readlane(v, i); }
-__device__ inline int64_t of_lane(int64_t v, int i) {
-  const uint32_t lo = of_lane((int)v, i), hi = of_lane((int)(v >> 32), i);
-  return (int64_t)((uint64_t)hi << 32 | lo);
+__device__ inline uint32_t of_lane(uint32_t v, int i) { return __builtin_amdgcn_readlane((int)v, i); }
+__device__ inline uint64_t of_lane(uint64_t v, int i) {
+  const uint32_t lo = of_lane((uint32_t)v, i), hi = of_lane((uint32_t)(v >> 32), i);
+  return (uint64_t)hi << 32 | lo;
 }
 
 struct Item {
@@ -149,7 +150,7 @@ struct Item {
 // One or two blocks of eight waves a CU, the longest first: the second ones in
 // the other order, so that a CU's two are as long together as any other's.
 template <int RB>
-__device__ inline int in_turn(int at, int items) {
+__device__ inline uint32_t in_turn(uint32_t at, uint32_t items) {
   return RB == kSharedWaves && items > kCus && items <= 2 * kCus && at >= kCus && at < items ? items - 1 - (at - kCus) : at;
 }
 
@@ -160,34 +161,39 @@ __device__ inline int in_turn(int at, int items) {
 // go first and heads are neighbours.  (In the sequences' own order 31 tokens over
 // up to 16384 positions, 32 heads on 8, dc = 64, took 92 us for 77, 63 over up to
 // 8192 77 for 67.)  `hist`: kClasses words of LDS for the wave.
+// A cu_new that decreases somewhere can name more rows than there are: counts may
+// then wrap, and an item is taken only if everything in it is in range.
 template <int RB>
-__device__ inline bool find_item(const AttnArgs& a, int at, int target, int* hist, Item& it) {
+__device__ inline bool find_item(const AttnArgs& a, uint32_t at, int target, uint32_t* hist, Item& it) {
   const int lane = threadIdx.x & 63, n = a.b.n_seqs, kv = a.c.kv_heads;
   if (n > 1 && lane < kClasses) hist[lane] = 0;
   auto seq = [&](int i) { return i < n ? kv_seq(a.b, a.c, i) : KvSeq{0, 0, 0, 0}; };
   const KvSeq first = seq(lane);
-  int64_t work = (int64_t)kv_tiles(first.len) * row_tiles<RB>(a, first);
+  uint64_t work = (uint64_t)kv_tiles(first.len) * row_tiles<RB>(a, first);
   for (int i = 64 + lane; i < n; i += 64) {
     const KvSeq s = seq(i);
-    work += (int64_t)kv_tiles(s.len) * row_tiles<RB>(a, s);
+    work += (uint64_t)kv_tiles(s.len) * row_tiles<RB>(a, s);
   }
   // of one sequence, its lane's number; of more, the last lane's sum
   auto total = [&](auto v) { return n > 1 ? of_lane(up_to(v), 63) : of_lane(v, 0); };
   work = total(work);
-  const int ct = (int)max((int64_t)min_chunk(RB), min((work * kv + target - 1) / target, (int64_t)kMostTiles));
+  const int ct = (int)max((uint64_t)min_chunk(RB), min((work * kv + target - 1) / target, (uint64_t)kMostTiles));
   const float classes = (kClasses - 1.0f) / ct;
   struct Share {
-    int row_tiles, chunks, whole, rest, kind;  // whole chunks of a row tile; items of whole chunks and others, whose class
+    int row_tiles, chunks, kind;  // row tiles, whole chunks of each, the class of what is left
+    uint32_t whole, rest;         // items of whole chunks and others
   };
   auto share_of = [&](const KvSeq& s) {
     const int t = kv_tiles(s.len), chunks = t / ct, left = t - chunks * ct, rt = row_tiles<RB>(a, s);
-    return Share{rt, chunks, chunks * rt * kv, left > 0 || chunks == 0 ? rt * kv : 0,
-                 kClasses - 1 - min((int)(left * classes), kClasses - 2)};
+    const uint32_t items = (uint32_t)rt * kv;
+    return Share{rt, chunks, kClasses - 1 - min((int)(left * classes), kClasses - 2), chunks * items,
+                 left > 0 || chunks == 0 ? items : 0};
   };
   const Share mine = share_of(first);
-  int kind, start;  // the item's class, 0 for whole chunks; items of the classes before
+  int kind;        // the item's class, 0 for whole chunks
+  uint32_t start;  // items of the classes before
   if (n > 1) {
-    int whole = mine.whole;
+    uint32_t whole = mine.whole;
     auto add = [&](const Share& x) {
       if (x.rest) __hip_atomic_fetch_add(hist + x.kind, x.rest, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     };
@@ -200,7 +206,7 @@ __device__ inline bool find_item(const AttnArgs& a, int at, int target, int* his
     }
     whole = total(whole);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int here = lane == 0 ? whole : lane < kClasses ? hist[lane] : 0, upto = up_to(here);
+    const uint32_t here = lane == 0 ? whole : lane < kClasses ? hist[lane] : 0, upto = up_to(here);
     at = in_turn<RB>(at, of_lane(upto, 63));
     const uint64_t past = __ballot(upto > at);
     if (past == 0) return false;
@@ -213,17 +219,17 @@ __device__ inline bool find_item(const AttnArgs& a, int at, int target, int* his
     if (kind == 0) start = 0;
   }
   at -= start;
-  int before = 0, ids = 0;  // items of the sequences before: of this class, and all
+  uint32_t before = 0, ids = 0;  // items of the sequences before: of this class, and all
   for (int i0 = 0; i0 < n; i0 += 64) {
     const KvSeq s = i0 == 0 ? first : seq(i0 + lane);
     const Share x = i0 == 0 ? mine : share_of(s);
-    const int all = x.whole + x.rest, here = kind == 0 ? x.whole : x.kind == kind ? x.rest : 0;
-    const int upto = n > 1 ? up_to(here) : here, ids_upto = n > 1 ? up_to(all) : all;
+    const uint32_t all = x.whole + x.rest, here = kind == 0 ? x.whole : x.kind == kind ? x.rest : 0;
+    const uint32_t upto = n > 1 ? up_to(here) : here, ids_upto = n > 1 ? up_to(all) : all;
     const uint64_t past = __ballot(before + upto > at);
     if (past != 0) {
       const int w = __builtin_ctzll(past);
-      auto of = [&](int v) { return of_lane(v, w); };
-      const int local = at - before - of(upto - here), rt = of(x.row_tiles), chunks = of(x.chunks);
+      auto of = [&](auto v) { return of_lane(v, w); };
+      const int local = (int)(at - before - of(upto - here)), rt = of(x.row_tiles), chunks = of(x.chunks);
       const int per = kind == 0 ? chunks : 1;  // chunks of this class that a row tile has
       const int hc = local / kv, t = hc / max(per, 1);
       it.seq = i0 + w;
@@ -232,11 +238,12 @@ __device__ inline bool find_item(const AttnArgs& a, int at, int target, int* his
       it.chunk = kind == 0 ? hc - t * per : chunks;
       it.tile = rt - 1 - t;
       it.chunk_tiles = ct;
-      it.id = ids + of(ids_upto - all) + (t * (chunks + (of(x.rest) != 0)) + it.chunk) * kv + it.head;
-      return local >= 0 && it.tile >= 0 && it.id < a.items;  // not so only for a cu_new that decreases
+      const uint32_t id = ids + of(ids_upto - all) + ((uint32_t)t * (chunks + (of(x.rest) != 0)) + it.chunk) * kv + it.head;
+      it.id = (int)id;
+      return local >= 0 && it.tile >= 0 && id < (uint32_t)a.items;  // not so only for a cu_new that decreases
     }
-    before += __builtin_amdgcn_readlane(upto, 63);
-    ids += __builtin_amdgcn_readlane(ids_upto, 63);
+    before += of_lane(upto, 63);
+    ids += of_lane(ids_upto, 63);
   }
   return false;
 }
@@ -807,7 +814,7 @@ __device__ inline Item block_item(const AttnArgs& a, int target, char* lds) {
   Item it{};
   Item* found = reinterpret_cast<Item*>(lds);
   if (threadIdx.x < 64) {
-    if (!find_item<RB>(a, blockIdx.x, target, reinterpret_cast<int*>(lds + sizeof(Item)), it)) it.seq = -1;
+    if (!find_item<RB>(a, blockIdx.x, target, reinterpret_cast<uint32_t*>(lds + sizeof(Item)), it)) it.seq = -1;
     if (threadIdx.x == 0) *found = it;
   }
   __syncthreads();

@@ -134,3 +134,39 @@ def test_unstored_positions_reach_no_earlier_row(gpu, kv, heads, dc, page, seqs,
     b.cache, b.seqs = host(b.data), few
     b.cu = np.concatenate([[0], np.cumsum([n for n, _ in few])]).astype(np.int32)
     attend_check(b, heads, host(qr)[~late.numpy()].astype(np.float64), got.cpu()[~late], (2 * dc) ** -0.5)
+
+
+# ------------------------------------------------------ a cu_new that decreases
+
+
+def fenced(n, gpu, pad=1 << 16):
+    """n bytes between two runs of `pad` marked ones: (all of them, the n)."""
+    import torch
+    whole = torch.full((n + 2 * pad,), 0xA5, dtype=torch.uint8, device=gpu)
+    return whole, whole[pad:pad + n]
+
+
+def fences_stand(whole, n):
+    pad = (whole.numel() - n) // 2
+    return bool((whole[:pad] == 0xA5).all()) and bool((whole[pad + n:] == 0xA5).all())
+
+
+def test_counts_that_wrap_stay_in_the_workspace(gpu):
+    """Half a million times the same 4096 rows (cu_new goes up and down): the work
+    counted over the sequences passes 2^31, the last one's numbers with it."""
+    import torch
+    import paper_2512_02901_amd as f2
+    n_seqs, rows, heads, pages = 1 << 20, 4096, 24, 10
+    kv = f2.PagedKv(pages, 32, 1, 16, data=torch.zeros(f2.PagedKv.bytes(pages, 32, 1, 16), dtype=torch.uint8, device=gpu))
+    cu = torch.zeros(n_seqs + 1, dtype=torch.int32, device=gpu)
+    cu[1::2] = rows
+    lens = torch.zeros(n_seqs, dtype=torch.int32, device=gpu)
+    lens[n_seqs - 2] = 320  # the last one with rows: more than one chunk
+    table = torch.arange(pages, dtype=torch.int32, device=gpu).expand(n_seqs, pages).contiguous()
+    q = torch.ones((rows, heads, 16, 2), dtype=torch.bfloat16, device=gpu)
+    need = kv.attend_workspace_bytes(rows, n_seqs, heads)
+    ws, mid = fenced(need, gpu)
+    buf, out = fenced(q.numel() * 2, gpu)
+    kv.attend(q, table, cu, lens, out=out.view(torch.bfloat16).view(q.shape), workspace=mid)
+    assert fences_stand(ws, need) and fences_stand(buf, q.numel() * 2)
+    assert (host(kv.data) == 0).all()

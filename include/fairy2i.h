@@ -813,7 +813,8 @@ fairy2i_status fairy2i_rope_table(int64_t n_pos, int32_t dc, double base, float*
  * sizes, n_seqs outside [1, 2^20], n_new outside [1, 2^26], max_pages < 1,
  * max_pages * page_size above 2^30, n_heads, rope_len < 1 or an ld below its
  * row; FAIRY2I_ERR_UNSUPPORTED for a misaligned cache or more work than a
- * launch takes.
+ * launch takes: 2^24 blocks or more, one for 1024 entries of a row of q, and a
+ * quarter of one for four rows of a key head (of 64 / dc heads for dc <= 32).
  */
 fairy2i_status fairy2i_kv_append(const fairy2i_kv_cache* cache, const fairy2i_kv_batch* batch, const float* q,
                                  int64_t q_ld, int32_t n_heads, const float* k, int64_t k_ld, const float* v,

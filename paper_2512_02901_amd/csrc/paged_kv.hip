@@ -22,6 +22,7 @@ namespace fairy2i {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kMostBlocks = ((int64_t)1 << 32) / kThreads - 1;  // a launch takes fewer than 2^32 threads
 
 // Groups of four positions: sequence i's start at slot cu_new[i] / 4 + 2 i, so
 // a slot's sequence is found without adding up anything.  (n positions touch
@@ -291,12 +292,12 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
 }
 
 __global__ __launch_bounds__(kThreads) void rope_table_kernel(int64_t n, int dc, double base, float2* __restrict__ out) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= n) return;
-  const int64_t p = i / dc;
-  double sn, cs;
-  sincos((double)p * pow(base, -(double)(i - p * dc) / dc), &sn, &cs);
-  out[i] = make_float2((float)cs, (float)sn);
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
+    const int64_t p = i / dc;
+    double sn, cs;
+    sincos((double)p * pow(base, -(double)(i - p * dc) / dc), &sn, &cs);
+    out[i] = make_float2((float)cs, (float)sn);
+  }
 }
 
 int head_groups(int kv_heads, int dc) {
@@ -324,8 +325,7 @@ fairy2i_status fairy2i_rope_table(int64_t n_pos, int32_t dc, double base, float*
   if (!out) return FAIRY2I_ERR_NULL;
   if (n_pos < 1 || n_pos > ((int64_t)1 << 30) || dc < 1 || dc > 4096 || !(base > 0.0) || !(base <= 1e300))
     return FAIRY2I_ERR_SHAPE;
-  const int64_t n = n_pos * dc, blocks = (n + kThreads - 1) / kThreads;
-  if (blocks > INT32_MAX) return FAIRY2I_ERR_SHAPE;
+  const int64_t n = n_pos * dc, blocks = min((n + kThreads - 1) / kThreads, kMostBlocks);
   hipLaunchKernelGGL(rope_table_kernel, dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream), n,
                      (int)dc, base, reinterpret_cast<float2*>(out));
   return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
@@ -355,7 +355,7 @@ fairy2i_status fairy2i_kv_append(const fairy2i_kv_cache* cache, const fairy2i_kv
   a.head_groups = head_groups(cache->n_kv_heads, cache->dc);
   const int64_t waves = slots(batch->n_new, batch->n_seqs) * a.head_groups, kv_blocks = (waves + 3) / 4;
   const int64_t chunks = (nq + 1023) / 1024, blocks = kv_blocks + chunks * batch->n_new;
-  if (waves > INT32_MAX - 4 || blocks > INT32_MAX) return FAIRY2I_ERR_UNSUPPORTED;
+  if (blocks > kMostBlocks) return FAIRY2I_ERR_UNSUPPORTED;
   a.kv_blocks = (int32_t)kv_blocks;
   a.q_chunks = (int32_t)chunks;
   auto kernel = cache->dc <= 64 ? kv_append_kernel<1> : kv_append_kernel<2>;
@@ -373,10 +373,10 @@ fairy2i_status fairy2i_kv_read(const fairy2i_kv_cache* cache, const fairy2i_kv_b
   a.k = static_cast<uint32_t*>(k_out);
   a.v = static_cast<uint32_t*>(v_out);
   a.head_groups = head_groups(cache->n_kv_heads, cache->dc);
-  const int64_t waves = slots(batch->n_new, batch->n_seqs) * a.head_groups;
-  if (waves > INT32_MAX - 4) return FAIRY2I_ERR_UNSUPPORTED;
+  const int64_t waves = slots(batch->n_new, batch->n_seqs) * a.head_groups, blocks = (waves + 3) / 4;
+  if (blocks > kMostBlocks) return FAIRY2I_ERR_UNSUPPORTED;
   auto kernel = cache->dc <= 64 ? kv_read_kernel<1> : kv_read_kernel<2>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)((waves + 3) / 4)), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
   return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
 }
 

@@ -184,18 +184,10 @@ void launch_vec(const float* x, const float* delta, const float* gain, float eps
                      reinterpret_cast<uint2*>(q), x_scale);
 }
 
-}  // namespace
+constexpr int64_t kMostTokens = 1 << 22;  // of a launch, which takes fewer than 2^32 threads
 
-}  // namespace fairy2i
-
-using namespace fairy2i;
-
-extern "C" fairy2i_status fairy2i_add_rmsnorm_i8(const float* x, const float* delta, const float* gain, float eps,
-                                                 int64_t B, int64_t n, float* h, int8_t* q, float* x_scale,
-                                                 void* stream) {
-  if (!x || !gain || !q || !x_scale) return FAIRY2I_ERR_NULL;
-  if (B <= 0 || n <= 0 || B > INT32_MAX || n > ((int64_t)1 << 24) || !(eps > 0.0f) || eps > FLT_MAX) return FAIRY2I_ERR_SHAPE;
-  auto s = static_cast<hipStream_t>(stream);
+void launch(const float* x, const float* delta, const float* gain, float eps, int64_t B, int64_t n, float* h,
+            int8_t* q, float* x_scale, hipStream_t s) {
   auto at = [](const void* p) { return reinterpret_cast<uintptr_t>(p); };
   // As many threads as take a token at a group each, up to 512, then up to four
   // groups each.  us for 1 | 2048 tokens (a launch in a graph is about 2 of them):
@@ -220,5 +212,23 @@ extern "C" fairy2i_status fairy2i_add_rmsnorm_i8(const float* x, const float* de
     launch_vec<512, 2>(x, delta, gain, eps, B, n, h, q, x_scale, s);
   else
     launch_vec<512, 4>(x, delta, gain, eps, B, n, h, q, x_scale, s);
+}
+
+}  // namespace
+
+}  // namespace fairy2i
+
+using namespace fairy2i;
+
+extern "C" fairy2i_status fairy2i_add_rmsnorm_i8(const float* x, const float* delta, const float* gain, float eps,
+                                                 int64_t B, int64_t n, float* h, int8_t* q, float* x_scale,
+                                                 void* stream) {
+  if (!x || !gain || !q || !x_scale) return FAIRY2I_ERR_NULL;
+  if (B <= 0 || n <= 0 || B > INT32_MAX || n > ((int64_t)1 << 24) || !(eps > 0.0f) || eps > FLT_MAX) return FAIRY2I_ERR_SHAPE;
+  for (int64_t b = 0; b < B; b += kMostTokens) {
+    const int64_t e = b * n;  // entries before
+    launch(x + 2 * e, delta ? delta + 2 * e : nullptr, gain, eps, min(B - b, kMostTokens), n, h ? h + 2 * e : nullptr,
+           q + 2 * e, x_scale + b, static_cast<hipStream_t>(stream));
+  }
   return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
 }

@@ -103,3 +103,13 @@ def test_rope_validation(lib):
     assert f(4, 4, 1e4, None, None) == ERR_NULL
     for n, dc, base in ((0, 4, 1e4), (4, 0, 1e4), (4, 4, 0.0), (4, 4, -1.0), (4, 4, float("inf")), ((1 << 30) + 1, 4, 1e4)):
         assert f(n, dc, base, P, None) == ERR_SHAPE
+
+
+def test_more_work_than_a_launch_takes(lib):
+    """2^24 blocks of 256 threads: refused before the launch, which takes fewer than 2^32 threads."""
+    def append(c, b, q_ld=16, heads=1, k_ld=512, q=P):
+        return lib.fairy2i_kv_append(c, b, q, q_ld, heads, P, k_ld, P, k_ld, P, 16, q, None)
+    assert append(cache(dc=16), batch(n_new=1 << 24)) == ERR_UNSUPPORTED
+    assert append(cache(dc=16), batch(n_new=1 << 23), q_ld=1040, heads=65) == ERR_UNSUPPORTED
+    assert append(cache(kv=8), batch(n_new=1 << 26), q=None) == ERR_UNSUPPORTED
+    assert lib.fairy2i_kv_read(cache(kv=8), batch(n_new=1 << 26), P, P, None) == ERR_UNSUPPORTED

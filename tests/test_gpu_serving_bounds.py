@@ -170,3 +170,39 @@ def test_counts_that_wrap_stay_in_the_workspace(gpu):
     kv.attend(q, table, cu, lens, out=out.view(torch.bfloat16).view(q.shape), workspace=mid)
     assert fences_stand(ws, need) and fences_stand(buf, q.numel() * 2)
     assert (host(kv.data) == 0).all()
+
+
+# --------------------------------------------------- more than a launch takes
+
+
+@pytest.mark.parametrize("B, n", [((1 << 24) + 7, 1), ((1 << 26) + 7, 4)])
+def test_norm_of_more_tokens_than_a_launch_takes(gpu, B, n):
+    """2^32 threads and more: the same tokens over and over give the same results."""
+    import torch
+    import paper_2512_02901_amd as f2
+    few = 4099
+    rng = np.random.default_rng(n)
+    x = dev(random_c(rng, few, n), gpu)
+    gain = dev((1 + 0.1 * rng.standard_normal(2 * n)).astype(np.float32), gpu)
+    want = f2.add_rmsnorm_i8(x, gain, delta=x)
+    again = -(-B // few)
+    many = x.repeat(again, 1)[:B]
+    got = f2.add_rmsnorm_i8(many, gain, delta=many)
+    for w, g in zip(want, got):
+        whole = B // few * few
+        assert (g[:whole].view(-1, *w.shape) == w).all()
+        assert torch.equal(g[whole:], w[:B - whole])
+    del many, got
+    torch.cuda.empty_cache()
+
+
+def test_rope_table_of_more_entries_than_a_launch_takes(gpu):
+    import torch
+    n, dc = 1 << 20, 4096
+    got = rope_of(n, dc, gpu)
+    for p in (0, 1, 77777, n // 2, n - 2, n - 1):
+        angle = p * 10000.0 ** (-np.arange(dc) / dc)
+        # the angle is off by some 2^-51 of itself
+        np.testing.assert_allclose(host(got[p]), np.stack([np.cos(angle), np.sin(angle)], -1), rtol=0, atol=2.0 ** -24 + 2.0 ** -30)
+    del got
+    torch.cuda.empty_cache()

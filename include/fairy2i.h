@@ -765,6 +765,9 @@ fairy2i_status fairy2i_add_rmsnorm_i8(const float* x, const float* delta, const 
  * outside [0, n_new), positions below 0 or from max_pages * page_size on (the
  * table's end) and page numbers outside [0, n_pages) are neither read nor
  * written, and the other rows stay at their positions.
+ *
+ * q, k, v, rope and the outputs of the calls below may begin at any of their
+ * elements (a complex64, a float, a bf16); only data and the workspace need more.
  */
 typedef struct fairy2i_kv_cache {
   uint8_t* data;

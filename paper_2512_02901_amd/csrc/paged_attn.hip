@@ -88,8 +88,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 struct AttnArgs {
   KvCache c;
   KvBatch b;
-  const uint32_t* q;  // [n_new][heads][dc] bf16 pairs
-  uint32_t* out;      // the same
+  const u32_any* q;   // [n_new][heads][dc] bf16 pairs
+  u32_any* out;       // the same
   int32_t heads, group;
   float scale;        // log2(e) times the score scale
   float* part;        // [items][rows of a tile][D] unnormalised sums
@@ -402,10 +402,10 @@ template <int NB>
 __device__ inline void load_q(const AttnArgs& a, const Item& it, int row0, bf16x8 (&q)[NB]) {
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   const int row = row0 + r, token = row / a.group, hq = it.head * a.group + (row - token * a.group);
-  const u32x4* at = reinterpret_cast<const u32x4*>(a.q + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
+  const u32x4_any* at = reinterpret_cast<const u32x4_any*>(a.q + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
   const bool real = row < it.s.n * a.group;
 #pragma unroll
-  for (int b = 0; b < NB; ++b) q[b] = __builtin_bit_cast(bf16x8, real ? at[4 * b] : u32x4{0, 0, 0, 0});
+  for (int b = 0; b < NB; ++b) q[b] = __builtin_bit_cast(bf16x8, real ? u32x4(at[4 * b]) : u32x4{0, 0, 0, 0});
 }
 
 // Scores past what the lane's row sees, in tiles from position t0 on.
@@ -622,7 +622,7 @@ __device__ inline void attend_tile(const AttnArgs& a, const Item& it, char* lds)
       if (row >= rows) continue;
       if (chunks == 1) {
         const float inv = sm[y].l == 0.0f ? 0.0f : 1.0f / sm[y].l;
-        u32x4* to = reinterpret_cast<u32x4*>(a.out + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
+        u32x4_any* to = reinterpret_cast<u32x4_any*>(a.out + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           u32x4 v;
@@ -788,7 +788,7 @@ __device__ inline void attend_shared(const AttnArgs& a, const Item& it, char* ld
   if (row >= rows) return;
   if (chunks == 1) {
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    u32x4* to = reinterpret_cast<u32x4*>(a.out + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
+    u32x4_any* to = reinterpret_cast<u32x4_any*>(a.out + ((int64_t)(it.s.row0 + token) * a.heads + hq) * (16 * NB)) + g;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       u32x4 v;
@@ -874,8 +874,8 @@ __global__ __launch_bounds__(kJoinThreads) void kv_attend_join_kernel(AttnArgs a
   auto store = [&](int w, int c, const float4& y, float sum) {
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     const int tk = w / a.group, hh = head * a.group + (w - tk * a.group);
-    *reinterpret_cast<uint2*>(a.out + ((int64_t)(row0 + tk) * a.heads + hh) * (D / 2) + 2 * c) =
-        make_uint2(pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv));
+    *reinterpret_cast<u32x2_any*>(a.out + ((int64_t)(row0 + tk) * a.heads + hh) * (D / 2) + 2 * c) =
+        u32x2_any{pack_bf16(y.x * inv, y.y * inv), pack_bf16(y.z * inv, y.w * inv)};
   };
   if (chunks <= kAhead) {
     constexpr int kPer = 64 / kLanes;
@@ -1089,8 +1089,8 @@ fairy2i_status fairy2i_kv_attend(const fairy2i_kv_cache* cache, const fairy2i_kv
   AttnArgs a{};
   a.c = kv_cache_of(cache);
   a.b = kv_batch_of(batch);
-  a.q = static_cast<const uint32_t*>(q);
-  a.out = static_cast<uint32_t*>(out);
+  a.q = static_cast<const u32_any*>(q);
+  a.out = static_cast<u32_any*>(out);
   a.heads = n_heads;
   a.group = n_heads / cache->n_kv_heads;
   a.scale = scale * 1.44269504088896341f;

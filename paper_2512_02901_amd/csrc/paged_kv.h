@@ -25,6 +25,13 @@ struct KvTile {
   }
 };
 
+// Tensors of bf16 pairs and of floats may begin at any element.  Accesses to them
+// promise no more than that and are one instruction all the same.
+typedef uint32_t u32_any __attribute__((aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+
 struct KvCache {
   uint8_t* data;
   int64_t n_pages;

@@ -41,6 +41,11 @@ __device__ inline uint32_t transpose4(uint32_t x) {
   return r;
 }
 
+__device__ inline float2 turn_at(const f32x2_any* p) {
+  const f32x2_any t = *p;
+  return make_float2(t.x, t.y);
+}
+
 // (re + i im)(c + i s), each product and sum rounded once.
 __device__ inline float2 turn(float2 v, float2 cs) {
 #pragma clang fp contract(off)
@@ -88,9 +93,9 @@ struct AppendArgs {
   KvBatch b;
   const float2 *q, *k, *v;
   int64_t q_ld, k_ld, v_ld;
-  const float2* rope;  // [rope_len][dc]
+  const f32x2_any* rope;  // [rope_len][dc]
   int64_t rope_len;
-  uint32_t* q_out;     // [n_new][heads][dc] bf16 pairs, or null
+  u32_any* q_out;      // [n_new][heads][dc] bf16 pairs, or null
   int32_t heads;
   int32_t head_groups; // of keys and values: waves that a slot takes
   int32_t kv_blocks, q_chunks;
@@ -130,7 +135,7 @@ __device__ void append_kv(const AppendArgs& a) {
       const bool load = mine && (valid >> j & 1);
       const int64_t row = s.row0 + (4 * group + j - s.p0);
       const float2 zero = make_float2(0.0f, 0.0f);
-      const float2 cs = load ? a.rope[(int64_t)(4 * group + j) * dc + e] : zero;
+      const float2 cs = load ? turn_at(a.rope + (int64_t)(4 * group + j) * dc + e) : zero;
       const float2 k = load ? a.k[row * a.k_ld + (int64_t)h * dc + e] : zero;
       kx[x][j] = turn(k, cs);
       vx[x][j] = load ? a.v[row * a.v_ld + (int64_t)h * dc + e] : zero;
@@ -213,16 +218,16 @@ __device__ void rotate_q(const AppendArgs& a) {
     if (row < s.row0 + s.n && s.p0 + (row - s.row0) < s.len) p = s.p0 + (row - s.row0);
   }
   const bool known = p >= 0 && p < a.rope_len;
-  const float2* turns = a.rope + (known ? p : 0) * a.c.dc;
+  const f32x2_any* turns = a.rope + (known ? p : 0) * a.c.dc;
   int c = (e0 + (int)threadIdx.x) % a.c.dc;
   const int step = kThreads % a.c.dc;
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
-    cs[m] = known ? turns[c] : make_float2(__builtin_nanf(""), __builtin_nanf(""));
+    cs[m] = known ? turn_at(turns + c) : make_float2(__builtin_nanf(""), __builtin_nanf(""));
     c += step;
     if (c >= a.c.dc) c -= a.c.dc;
   }
-  uint32_t* out = a.q_out + (int64_t)row * n;
+  u32_any* out = a.q_out + (int64_t)row * n;
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
     const int e = e0 + m * kThreads + threadIdx.x;
@@ -239,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendArgs a) {
 struct ReadArgs {
   KvCache c;
   KvBatch b;
-  uint32_t *k, *v;  // [n_new][kv_heads][dc] bf16 pairs
+  u32_any *k, *v;  // [n_new][kv_heads][dc] bf16 pairs
   int32_t head_groups;
 };
 
@@ -348,9 +353,9 @@ fairy2i_status fairy2i_kv_append(const fairy2i_kv_cache* cache, const fairy2i_kv
   a.q_ld = q_ld;
   a.k_ld = k_ld;
   a.v_ld = v_ld;
-  a.rope = reinterpret_cast<const float2*>(rope);
+  a.rope = reinterpret_cast<const f32x2_any*>(rope);
   a.rope_len = rope_len;
-  a.q_out = static_cast<uint32_t*>(q_out);
+  a.q_out = static_cast<u32_any*>(q_out);
   a.heads = n_heads;
   a.head_groups = head_groups(cache->n_kv_heads, cache->dc);
   const int64_t waves = slots(batch->n_new, batch->n_seqs) * a.head_groups, kv_blocks = (waves + 3) / 4;
@@ -370,8 +375,8 @@ fairy2i_status fairy2i_kv_read(const fairy2i_kv_cache* cache, const fairy2i_kv_b
   ReadArgs a{};
   a.c = kv_cache_of(cache);
   a.b = kv_batch_of(batch);
-  a.k = static_cast<uint32_t*>(k_out);
-  a.v = static_cast<uint32_t*>(v_out);
+  a.k = static_cast<u32_any*>(k_out);
+  a.v = static_cast<u32_any*>(v_out);
   a.head_groups = head_groups(cache->n_kv_heads, cache->dc);
   const int64_t waves = slots(batch->n_new, batch->n_seqs) * a.head_groups, blocks = (waves + 3) / 4;
   if (blocks > kMostBlocks) return FAIRY2I_ERR_UNSUPPORTED;

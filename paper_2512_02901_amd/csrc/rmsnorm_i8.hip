@@ -70,11 +70,13 @@ __device__ inline uint32_t quantise(float t, const Norm& k) {
 
 __device__ inline uint32_t abs_bits(float t) { return __float_as_uint(t) & 0x7FFFFFFFu; }
 
+typedef int8_t i8x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
 // Any size and alignment.  A token is read twice (the second time from h
 // where that is written, which may be x or delta).
 __global__ __launch_bounds__(256) void add_rmsnorm_i8_any_kernel(const float2* x, const float2* delta,
                                                                  const float* __restrict__ gain, float eps, int64_t n,
-                                                                 float2* h, char2* __restrict__ q,
+                                                                 float2* h, i8x2_any* __restrict__ q,
                                                                  float* __restrict__ x_scale) {
   const int64_t base = (int64_t)blockIdx.x * n;
   double sum = 0.0;
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(256) void add_rmsnorm_i8_any_kernel(const float2* x
       v.x += d.x;
       v.y += d.y;
     }
-    q[base + j] = make_char2((char)quantise(v.x * gain[j], k), (char)quantise(v.y * gain[n + j], k));
+    q[base + j] = i8x2_any{(int8_t)quantise(v.x * gain[j], k), (int8_t)quantise(v.y * gain[n + j], k)};
   }
   if (threadIdx.x == 0) x_scale[blockIdx.x] = k.scale;
 }
@@ -201,7 +203,7 @@ void launch(const float* x, const float* delta, const float* gain, float eps, in
   if (n % 4 != 0 || n > 8192 || ((at(x) | at(delta) | at(gain) | at(h)) & 15) != 0 || (at(q) & 7) != 0)
     hipLaunchKernelGGL(add_rmsnorm_i8_any_kernel, dim3((unsigned)B), dim3(256), 0, s,
                        reinterpret_cast<const float2*>(x), reinterpret_cast<const float2*>(delta), gain, eps, n,
-                       reinterpret_cast<float2*>(h), reinterpret_cast<char2*>(q), x_scale);
+                       reinterpret_cast<float2*>(h), reinterpret_cast<i8x2_any*>(q), x_scale);
   else if (n <= 256)
     launch_vec<64, 1>(x, delta, gain, eps, B, n, h, q, x_scale, s);
   else if (n <= 1024)

@@ -206,3 +206,50 @@ def test_rope_table_of_more_entries_than_a_launch_takes(gpu):
         np.testing.assert_allclose(host(got[p]), np.stack([np.cos(angle), np.sin(angle)], -1), rtol=0, atol=2.0 ** -24 + 2.0 ** -30)
     del got
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------ tensors at any element
+
+
+def placed(t, off):
+    """t at `off` elements past a 512-byte boundary."""
+    import torch
+    buf = torch.empty(t.numel() + off, dtype=t.dtype, device=t.device)
+    out = buf[off:].view(t.shape)
+    out.copy_(t)
+    assert out.is_contiguous() and out.data_ptr() % 512 == off * t.element_size()
+    return out
+
+
+@pytest.mark.parametrize("off", [1, 2, 5])
+@pytest.mark.parametrize("seqs", [[(1, 40), (3, 1500)], [(150, 170), (140, 900)]])
+@pytest.mark.parametrize("kv, heads, dc", [(2, 4, 32), (1, 4, 64), (1, 2, 128)])
+def test_tensors_at_any_element(gpu, kv, heads, dc, seqs, off):
+    import torch
+    b = Batch(seqs, kv, dc, 32, gpu, seed=35).fill()
+    q, k, v = (dev(random_c(b.rng, b.N, h, dc), gpu) for h in (heads, kv, kv))
+    rope = rope_of(b.width * 32, dc, gpu)
+    b.dev()
+    qr = b.kvc.append(k, v, *b.t, rope, q=q)
+    want = (b.data, qr, b.kvc.attend(qr, *b.t), *b.kvc.read(*b.t, b.N))
+    b.dev()
+    got_q = b.kvc.append(placed(k, off), placed(v, off), *b.t, placed(rope, off), q=placed(q, off),
+                         q_out=placed(torch.zeros_like(qr), off))
+    out = b.kvc.attend(got_q, *b.t, out=placed(torch.zeros_like(qr), off + 1))
+    both = tuple(placed(torch.zeros_like(x), off) for x in want[3:])
+    b.kvc.read(*b.t, b.N, out=both)
+    for x, y in zip(want, (b.data, got_q, out, *both)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("off", [1, 3, 8])
+@pytest.mark.parametrize("n", [64, 1500, 77])
+def test_norm_into_any_byte(gpu, n, off):
+    import torch
+    import paper_2512_02901_amd as f2
+    rng = np.random.default_rng(n)
+    x, gain = dev(random_c(rng, 5, n), gpu), dev(rng.standard_normal(2 * n).astype(np.float32), gpu)
+    h, q, s = f2.add_rmsnorm_i8(x, gain, delta=x)
+    q0, s0 = placed(torch.zeros_like(q), off), placed(torch.zeros_like(s), off)
+    f2.add_rmsnorm_i8(placed(x, off), placed(gain, off), delta=placed(x, off), h_out=placed(h, off), out=(q0, s0))
+    assert torch.equal(q, q0) and torch.equal(s, s0)

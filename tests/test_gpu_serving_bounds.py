@@ -253,3 +253,145 @@ def test_norm_into_any_byte(gpu, n, off):
     q0, s0 = placed(torch.zeros_like(q), off), placed(torch.zeros_like(s), off)
     f2.add_rmsnorm_i8(placed(x, off), placed(gain, off), delta=placed(x, off), h_out=placed(h, off), out=(q0, s0))
     assert torch.equal(q, q0) and torch.equal(s, s0)
+
+
+# ------------------------------------------- numbers of any value, memory around
+
+
+def in_fences(t, gpu):
+    """A copy of t between two marked runs: (all bytes, the copy)."""
+    import torch
+    whole, mid = fenced(t.numel() * t.element_size(), gpu)
+    out = mid.view(t.dtype).view(t.shape)
+    out.copy_(t)
+    return whole, out
+
+
+@pytest.mark.parametrize("n, heads, dc", [(4, 2, 32), (4, 4, 64), (150, 2, 48), (150, 2, 16)])
+def test_numbers_out_of_range_write_nothing_outside(gpu, n, heads, dc):
+    """Whatever cu_new, lens and pages hold: the bytes around every output, around
+    the workspace and of pages that no table names stay, and so do the inputs."""
+    import torch
+    import paper_2512_02901_amd as f2
+    b = Batch([(n, 2 * n + 40)] * 3, 2, dc, 32, gpu, seed=36, spare=5).fill()
+    N = b.N
+    rope = rope_of(b.width * 32, dc, gpu)
+    q, k, v = (dev(random_c(b.rng, N, h, dc), gpu) for h in (heads, 2, 2))
+    inputs = [x.clone() for x in (q, k, v, rope)]
+    qb = torch.zeros((N, heads, dc, 2), dtype=torch.bfloat16, device=gpu)
+    kb = torch.zeros((N, 2, dc, 2), dtype=torch.bfloat16, device=gpu)
+    named = np.unique(b.table[b.table >= 0])
+    spare = np.setdiff1d(np.arange(b.n_pages), named)
+    tables = [b.table.copy() for _ in range(2)]
+    tables[1][0, ::2], tables[1][0, 1::2] = -1, b.n_pages
+    tables[1][1, ::2], tables[1][2, 0] = 2 ** 31 - 1, -2 ** 31
+    far = 2 ** 31 - 1
+    for cu in ([0, 2 * n + 1, n + 1, 3 * n], [-7, n, far, n - 1], [3 * n, 0, 3 * n, 0], [5, 5, 5, 5], [-far, far, -far, far]):
+        for lens in ([far, -far - 1, 40], [0, 3, 63], [b.width * 32 + 1, b.width * 32 - 1, n]):
+            for table in tables:
+                t = tuple(dev(np.array(a, np.int32), gpu) for a in (table, cu, lens))
+                whole, data = in_fences(dev(b.cache, gpu), gpu)
+                kv = f2.PagedKv(b.n_pages, 32, 2, dc, data=data)
+                w1, q_out = in_fences(qb, gpu)
+                qr = kv.append(k, v, *t, rope, q=q, q_out=q_out)
+                w2, out = in_fences(qb, gpu)
+                need = kv.attend_workspace_bytes(N, 3, heads)
+                w3, ws = fenced(need, gpu)
+                kv.attend(torch.nan_to_num(qr), *t, out=out, workspace=ws)
+                (w4, rk), (w5, rv) = in_fences(kb, gpu), in_fences(kb, gpu)
+                kv.read(*t, N, out=(rk, rv))
+                for w, size in ((whole, data.numel()), (w1, 2 * qb.numel()), (w2, 2 * qb.numel()), (w3, need),
+                                (w4, 2 * kb.numel()), (w5, 2 * kb.numel())):
+                    assert fences_stand(w, size), (cu, lens)
+                pages = host(data).reshape(b.n_pages, -1)
+                np.testing.assert_array_equal(pages[spare], b.cache.reshape(b.n_pages, -1)[spare])
+    for x, y in zip((q, k, v, rope), inputs):
+        assert torch.equal(x, y)
+
+
+PLANS = {
+    "decode": [(1, 40), (1, 3000), (0, 0), (1, 700)],
+    "verify": [(5, 1300), (3, 700)],
+    "prompt": [(300, 300)],
+    "prompts": [(140, 2000), (200, 260), (1, 900)],
+}
+
+
+@pytest.mark.parametrize("seqs", list(PLANS))
+@pytest.mark.parametrize("kv, heads, dc", [(2, 2, 16), (1, 4, 32), (2, 2, 48), (1, 3, 64), (1, 2, 128)])
+def test_workspace_and_output_memory(gpu, kv, heads, dc, seqs):
+    """A workspace of exactly the bytes asked for, holding anything, and an output
+    in q's own memory give what a call of its own gives."""
+    import torch
+    b = Batch(PLANS[seqs], kv, dc, 32, gpu, seed=37).fill()
+    q = queries(b, heads).to(gpu)
+    kvc = b.dev()
+    want = kvc.attend(q, *b.t)
+    need = kvc.attend_workspace_bytes(b.N, len(b.seqs), heads)
+    for byte in (0x00, 0x7F, 0xFF):
+        whole, ws = fenced(need, gpu)
+        ws.fill_(byte)
+        whole_out, out = in_fences(q, gpu)
+        kvc.attend(out, *b.t, out=out, workspace=ws)
+        assert torch.equal(out, want)
+        assert fences_stand(whole, need) and fences_stand(whole_out, 2 * q.numel())
+
+
+# --------------------------------------- plans that short sequences never reach
+
+
+def sampled_check(b, heads, q, got, scale, every):
+    """attend_check's bound for every `every`-th row of each sequence and its last."""
+    got = host(got).astype(np.float64)
+    for i, (n, length) in enumerate(b.seqs):
+        k, v = sv.read(b.cache, b.page, b.kv, b.dc, b.table[i], length)
+        for j in sorted({*range(0, n, every), n - 1}):
+            want, size, most = sv.attend(q[b.cu[i] + j:b.cu[i] + j + 1], k, v, length - n + j, scale)
+            d = np.abs(got[b.cu[i] + j:b.cu[i] + j + 1] - want)
+            assert (d <= (2.0 ** -8 + 2.0 ** -18 * most) * size + 1e-37).all(), (i, j)
+
+
+# more than 64 chunks of 8 tiles a row (a block joins each row); chunks longer than
+# the least, by one row block and by two; 336 and 512 items of 128 rows, whose second
+# half goes the other way round
+@pytest.mark.parametrize("seqs, kv, heads, dc, every", [
+    ([(1, 17000)], 1, 2, 64, 1), ([(3, 17111), (1, 20)], 1, 2, 16, 1), ([(1, 16700)], 1, 3, 128, 1), ([(2, 17300)], 1, 1, 48, 1),
+    ([(100, 3000)] * 8, 2, 2, 16, 37), ([(1, 8200)] * 2, 17, 17, 16, 1),
+    ([(1200, 4000)] * 2, 2, 4, 32, 173),
+    ([(700, 700), (600, 650)], 8, 16, 64, 83), ([(2048, 2048)], 8, 8, 64, 293)])
+def test_plans_of_long_calls(gpu, seqs, kv, heads, dc, every):
+    b = Batch(seqs, kv, dc, 64, gpu, seed=38)
+    at = 64 * dc
+    c = b.cache.reshape(-1, b.tile)
+    c[:, at:] = np.clip(np.round(127 + 0.7 * b.rng.standard_normal(c[:, at:].shape)), 2, 252)
+    q = queries(b, heads)
+    got = b.dev().attend(q.to(gpu), *b.t)
+    sampled_check(b, heads, q.double().numpy(), got, (2 * dc) ** -0.5, every)
+
+
+# ------------------------------------------------------------------ midpoints
+
+
+def midpoint_block(e, sign):
+    """32 reals of scale 2^e (dtype float32): every midpoint between two e2m1 values, the
+    floats next to it, and a largest value that asks for that scale."""
+    mid = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], np.float32)
+    v = np.concatenate([mid, np.nextafter(mid, np.float32(9)), np.nextafter(mid, np.float32(0)), -mid,
+                        np.array([7.0, 6.0, 0.0, -0.0], np.float32)])
+    return np.ldexp(v * np.float32(sign), e).astype(np.float32)
+
+
+@pytest.mark.parametrize("dc", [16, 64, 80])
+def test_midpoints_round_to_the_even_code(gpu, dc):
+    """Keys at position 0 (turned by nothing) and values, at scales over the whole range."""
+    n, nb = 63, dc // 16
+    b = Batch([(1, 1)] * n, 2, dc, 32, gpu, seed=39)
+    es = np.linspace(-122, 124, n * 2 * nb).astype(int)  # the smallest neighbours stay normal numbers
+    x = np.stack([midpoint_block(e, 1 - 2 * (i % 2)) for i, e in enumerate(es)])
+    k = x.reshape(n, 2, dc, 2)
+    v = x[::-1].reshape(n, 2, dc, 2)
+    k, v = (np.ascontiguousarray(t).view(np.complex64)[..., 0] for t in (k, v))
+    rope = rope_of(32, dc, gpu)
+    assert (host(rope[0]) == [1, 0]).all()
+    b.dev().append(dev(k, gpu), dev(v, gpu), *b.t, rope)
+    np.testing.assert_array_equal(host(b.data), expect_append(b, k, v, host(rope)))

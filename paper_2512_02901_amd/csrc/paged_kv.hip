@@ -81,8 +81,8 @@ __device__ inline uint32_t row_top(uint32_t v) {
 
 // Byte J of `to`: v / 2^e, each part to the nearest of 0 .5 1 1.5 2 3 4 6 (ties
 // to the even code, above 6 as 6), the real one in the low nibble.  The
-// conversion takes the exponent of the scale; held against comparisons at every
-// midpoint for every third float and every fourth, scales from 2^-125 to 2^125.
+// conversion takes the exponent of the scale.  The tests hold it at every midpoint
+// and the floats next to it, scales from 2^-122 to 2^124.
 template <int J>
 __device__ inline uint32_t e2m1(uint32_t to, float2 v, uint32_t scale) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(to, v.x, v.y, __uint_as_float(scale << 23), J);
@@ -248,6 +248,9 @@ struct ReadArgs {
   int32_t head_groups;
 };
 
+// For checks and for moving sequences, between steps and not in them, so it is the
+// plain form, scales a byte at a time: 3926 tokens (20 MB) 7.5 us, where a copy's
+// rate would be 3.9.
 template <int EPL>
 __global__ __launch_bounds__(kThreads) void kv_read_kernel(ReadArgs a) {
   const int lane = threadIdx.x & 63, dc = a.c.dc;

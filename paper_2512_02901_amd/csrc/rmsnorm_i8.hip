@@ -73,7 +73,8 @@ __device__ inline uint32_t abs_bits(float t) { return __float_as_uint(t) & 0x7FF
 typedef int8_t i8x2_any __attribute__((ext_vector_type(2), aligned(1)));
 
 // Any size and alignment.  A token is read twice (the second time from h
-// where that is written, which may be x or delta).
+// where that is written, which may be x or delta): a size that no number of
+// registers a thread is right for has nowhere else to wait for its maximum.
 __global__ __launch_bounds__(256) void add_rmsnorm_i8_any_kernel(const float2* x, const float2* delta,
                                                                  const float* __restrict__ gain, float eps, int64_t n,
                                                                  float2* h, i8x2_any* __restrict__ q,

@@ -860,6 +860,131 @@ fairy2i_status fairy2i_kv_attend(const fairy2i_kv_cache* cache, const fairy2i_kv
                                  void* stream);
 
 /*
+ * Training operators around the layers: the norm in front of a layer with its
+ * gradient, the 8-bit form in which a layer's input is kept for the backward
+ * pass, and the product of two 8-bit matrices.
+ *
+ * fairy2i_fp8_matrix: rows x cols reals (each 1 to 2^22) in e4m3 (sign, four
+ * exponent bits, three mantissa bits; largest value 448, code 0x7F a NaN) with
+ * one power of two for 128 neighbours of a row:
+ *   codes   [rows][cp] bytes, cp = cols rounded up to a multiple of 128, 16-byte
+ *           aligned; codes past cols are 0;
+ *   scales  [ceil(cols / 512)][rows][4] bytes, 4-byte aligned: byte b of entry
+ *           (g, r) is e + 127 of the block of columns 128 (4 g + b) .. + 127 of
+ *           row r.  Bytes of blocks that begin past cols are not looked at.
+ * A code stands for its value times 2^e, e in [-117, 119]: what a matrix holds is
+ * a bf16 number.  The quantisers below choose the smallest e with
+ * max |x| <= 448 * 2^e and round to nearest, ties to even; magnitudes above
+ * 448 * 2^119 become that.  A value that is not finite is held as a NaN and does
+ * not count for e.  Codes and scales are the caller's memory (device).
+ */
+typedef struct fairy2i_fp8_matrix {
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t rows;
+  int64_t cols;
+} fairy2i_fp8_matrix;
+
+/* Bytes of codes and of scales; 0 for sizes that are not supported. */
+size_t fairy2i_fp8_codes_bytes(int64_t rows, int64_t cols);
+size_t fairy2i_fp8_scales_bytes(int64_t rows, int64_t cols);
+
+/*
+ * x: rows x cols reals of dtype (FAIRY2I_ACT_F32 or FAIRY2I_ACT_BF16), ld >=
+ * cols elements from row to row, at any element's address.  Complex rows of n
+ * entries are rows of 2n reals.  direct: rows x cols, blocks along the rows of
+ * x; turned: cols x rows, the transposed matrix with blocks along the columns of
+ * x; either may be NULL.  Both together read x once.  Results do not depend on
+ * which is asked for.
+ * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for sizes out of range or that
+ * disagree, ld < cols; FAIRY2I_ERR_DTYPE; FAIRY2I_ERR_UNSUPPORTED for misaligned
+ * codes or scales, or 2^24 or more tiles of 128 x 128.
+ */
+fairy2i_status fairy2i_fp8_quantize(const void* x, int32_t dtype, int64_t ld, const fairy2i_fp8_matrix* direct,
+                                    const fairy2i_fp8_matrix* turned, void* stream);
+
+/*
+ * out (cols x rows) = the transposed matrix of `in` (rows x cols): its values
+ * with new scales along the other axis.  A value keeps all its bits unless it is
+ * below 2^-14 of what its new block's scale can hold.  The two must not overlap.
+ * Errors: as fairy2i_fp8_quantize.
+ */
+fairy2i_status fairy2i_fp8_transpose(const fairy2i_fp8_matrix* in, const fairy2i_fp8_matrix* out, void* stream);
+
+/* out: bf16 [rows][cols], what the matrix stands for, exact.  Errors: as above. */
+fairy2i_status fairy2i_fp8_dequantize(const fairy2i_fp8_matrix* in, void* out, void* stream);
+
+/*
+ * C (+)= A B^T: A is M x K, B is N x K, C[m][n] = sum over k of A[m][k] B[n][k];
+ * C has dtype FAIRY2I_ACT_F32 or FAIRY2I_ACT_BF16, rows ldc >= N elements apart,
+ * at any element's address, and must not overlap an operand.  accumulate = 1
+ * adds to C.  With tokens in rows the three products of a layer with real form R
+ * (fairy2i_wl_realify) are
+ *   Y = X R^T       A = X, B = R,
+ *   G_X = G_Y R     A = G_Y, B = R turned,
+ *   G_R = G_Y^T X   A = G_Y turned, B = X turned (from the 8-bit X that the
+ *                   forward product took: fairy2i_fp8_transpose).
+ * Products are exact.  The matrix cores sum them in float32, neighbouring ones
+ * in groups whose terms keep 13 bits below the group's largest: with what the
+ * operands hold taken as exact, relative L2 1.5e-5 for N(0, 1) values, up to 8e-5
+ * where values of a block differ by e^(N(0, 1)); a C in float32 is no closer.
+ * Repeated calls give the same bits.  workspace:
+ * fairy2i_gemm_fp8_workspace_bytes(M, N, K) bytes (none where that is 0),
+ * 4-byte aligned, contents ignored; calls that share one must not overlap.
+ * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for sizes out of range or that
+ * disagree, ldc < N; FAIRY2I_ERR_DTYPE; FAIRY2I_ERR_UNSUPPORTED for misaligned
+ * operands or 2^22 or more tiles of C; FAIRY2I_ERR_WORKSPACE.
+ */
+size_t fairy2i_gemm_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K);
+fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_matrix* B, void* C, int32_t dtype,
+                                int64_t ldc, int32_t accumulate, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/*
+ * The norm in front of a layer, over the 2n reals of each token:
+ *   h = x + delta (x alone where delta is NULL),
+ *   mu = mean(h) for center = 1 (layer norm), 0 for center = 0 (RMSNorm),
+ *   r = 1 / sqrt(mean((h - mu)^2) + eps),  z = (h - mu) * r * gain + bias.
+ * x, delta, h: complex64 [B][n]; h may be NULL (not stored), x or delta.
+ * gain, bias: float32 [2n], the real parts' values, then the imaginary parts'
+ * (as in fairy2i_add_rmsnorm_i8); bias may be NULL.  One of z (bf16 pairs
+ * [B][n][2]) and z8 (B x 2n, as fairy2i_fp8_quantize would write z) is given.
+ * stats: float32 [B][2] = (mu, r), what the backward pass takes.  Both sums are
+ * taken in double, the rest is float32.  x, delta, gain, bias, h, z and stats
+ * may begin at any of their elements.
+ * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for B < 1 or above 2^31 - 1, n < 1
+ * or above 2^24 (with z8: the matrix's own limits), a matrix of other sizes, eps
+ * not positive and finite, center not 0 or 1; FAIRY2I_ERR_UNSUPPORTED for both of
+ * z and z8 or a misaligned matrix.
+ */
+fairy2i_status fairy2i_add_layernorm(const float* x, const float* delta, const float* gain, const float* bias,
+                                     float eps, int32_t center, int64_t B, int64_t n, float* h, void* z,
+                                     const fairy2i_fp8_matrix* z8, float* stats, void* stream);
+
+/*
+ * Its gradient.  With y = (h - mu) r and w = dz * gain, means over a token's 2n
+ * reals and sums over the B tokens:
+ *   dx = dh + r (w - mean(w) - y mean(w y))  (without mean(w) for center = 0),
+ *   dgain = sum dz y,  dbias = sum dz.
+ * dz: pairs [B][n][2] of dtype FAIRY2I_ACT_F32 or FAIRY2I_ACT_BF16; h, stats: as
+ * the forward pass left them; dh: complex64 [B][n], the gradient that reaches h by
+ * the residual, or NULL; dx: complex64 [B][n] output (dL/dRe + i dL/dIm), may be
+ * dh or h; dgain, dbias: float32 [2n] outputs, dbias may be NULL.  dx is also the
+ * gradient of the forward pass's x and of its delta.  Float32 sums of a block's
+ * tokens, joined in double in a fixed order: repeated calls give the same bits.
+ * workspace: fairy2i_layernorm_backward_workspace_bytes(B, n) bytes (none where
+ * that is 0), 4-byte aligned, contents ignored; calls that share one must not
+ * overlap.
+ * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE as above; FAIRY2I_ERR_DTYPE;
+ * FAIRY2I_ERR_WORKSPACE.
+ */
+size_t fairy2i_layernorm_backward_workspace_bytes(int64_t B, int64_t n);
+fairy2i_status fairy2i_layernorm_backward(const void* dz, int32_t dtype, const float* h, const float* stats,
+                                          const float* gain, const float* dh, int32_t center, int64_t B, int64_t n,
+                                          float* dx, float* dgain, float* dbias, void* workspace,
+                                          size_t workspace_bytes, void* stream);
+
+/*
  * Matrix-core rate probe, for the roofline figures (not part of the method):
  * the sustained rate of the prefill GEMM's instruction (kind
  * FAIRY2I_PROBE_MFMA_I8: v_mfma_i32_16x16x64_i8, 32768 operations), of the

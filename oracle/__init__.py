@@ -15,3 +15,4 @@ from . import block  # noqa: F401,E402
 from . import groups  # noqa: F401,E402
 from . import qat  # noqa: F401,E402
 from . import serving  # noqa: F401,E402
+from . import training  # noqa: F401,E402

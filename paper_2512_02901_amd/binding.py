@@ -78,6 +78,18 @@ _SIGNATURES = {
     "fairy2i_kv_read": (_c_i32, [_c_p, _c_p, _c_p, _c_p, _c_p]),
     "fairy2i_kv_attend_workspace_bytes": (_c_size, [_c_p, _c_i64, _c_i64, _c_i32]),
     "fairy2i_kv_attend": (_c_i32, [_c_p, _c_p, _c_p, _c_i32, ctypes.c_float, _c_p, _c_p, _c_size, _c_p]),
+    "fairy2i_fp8_codes_bytes": (_c_size, [_c_i64, _c_i64]),
+    "fairy2i_fp8_scales_bytes": (_c_size, [_c_i64, _c_i64]),
+    "fairy2i_fp8_quantize": (_c_i32, [_c_p, _c_i32, _c_i64, _c_p, _c_p, _c_p]),
+    "fairy2i_fp8_transpose": (_c_i32, [_c_p, _c_p, _c_p]),
+    "fairy2i_fp8_dequantize": (_c_i32, [_c_p, _c_p, _c_p]),
+    "fairy2i_gemm_fp8_workspace_bytes": (_c_size, [_c_i64, _c_i64, _c_i64]),
+    "fairy2i_gemm_fp8": (_c_i32, [_c_p, _c_p, _c_p, _c_i32, _c_i64, _c_i32, _c_p, _c_size, _c_p]),
+    "fairy2i_add_layernorm": (_c_i32, [_c_p, _c_p, _c_p, _c_p, ctypes.c_float, _c_i32, _c_i64, _c_i64, _c_p, _c_p,
+                                       _c_p, _c_p, _c_p]),
+    "fairy2i_layernorm_backward_workspace_bytes": (_c_size, [_c_i64, _c_i64]),
+    "fairy2i_layernorm_backward": (_c_i32, [_c_p, _c_i32, _c_p, _c_p, _c_p, _c_p, _c_i32, _c_i64, _c_i64, _c_p, _c_p,
+                                            _c_p, _c_p, _c_size, _c_p]),
     "fairy2i_cpu_lut_workspace_bytes": (_c_size, [_c_i32, _c_i64, _c_i64, _c_i32]),
     "fairy2i_cpu_lut_wl_matmul": (_c_i32, [_c_p, _c_p, _c_p, _c_p, _c_i32, _c_i64, _c_i64, _c_p, _c_p, _c_i64,
                                            _c_p, _c_p, _c_p, _c_size, _c_i32]),
@@ -115,6 +127,11 @@ class KvBatchDesc(ctypes.Structure):
     """fairy2i_kv_batch of include/fairy2i.h."""
     _fields_ = [("pages", _c_p), ("cu_new", _c_p), ("lens", _c_p), ("n_new", _c_i64), ("n_seqs", _c_i32),
                 ("max_pages", _c_i32)]
+
+
+class Fp8Desc(ctypes.Structure):
+    """fairy2i_fp8_matrix of include/fairy2i.h."""
+    _fields_ = [("codes", _c_p), ("scales", _c_p), ("rows", _c_i64), ("cols", _c_i64)]
 
 
 class Fairy2iError(RuntimeError):
@@ -1187,3 +1204,308 @@ class PagedKv:
                                      workspace.data_ptr(), workspace.numel(), _raw_stream(index)),
                "fairy2i_kv_attend")
         return out
+
+
+# ------------------------------------------------------------- training ---
+
+def _call(name, index, *args):
+    """A library call on the current stream of device `index`, which is made the current one for it."""
+    fn = getattr(_lib, name)
+    torch = _torch_module
+    if torch.cuda.current_device() == index:
+        status = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    _check(status, name)
+
+
+class Fp8Matrix:
+    """rows x cols reals in e4m3 with a power-of-two scale for 128 neighbours of
+    a row (fairy2i_fp8_matrix; the format is in include/fairy2i.h).
+
+    ``codes``: float8_e4m3fn [rows, cols rounded up to 128], zeros past cols;
+    ``scales``: uint8 [ceil(cols / 512), rows, 4]; both device tensors, new ones
+    (their contents undefined) where they are not given.  rows and cols up to
+    2^22."""
+
+    def __init__(self, rows, cols, codes=None, scales=None, device="cuda"):
+        torch = _torch_module or _torch()
+        if _lib is None:
+            load()
+        if not (1 <= rows <= 1 << 22 and 1 <= cols <= 1 << 22):
+            raise ValueError("rows and cols must be in [1, 2^22]")
+        shape, scale_shape = (rows, -(-cols // 128) * 128), (-(-cols // 512), rows, 4)
+        if codes is None:
+            codes = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device if scales is None else scales.device)
+        if scales is None:
+            scales = torch.empty(scale_shape, dtype=torch.uint8, device=codes.device)
+        _require(codes, torch.float8_e4m3fn, "codes")
+        _require(scales, torch.uint8, "scales", codes.device)
+        if codes.shape != shape or scales.shape != scale_shape:
+            raise ValueError(f"codes must be {shape} and scales {scale_shape}")
+        self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
+        self._index = codes.get_device()
+        self._desc = Fp8Desc(codes.data_ptr(), scales.data_ptr(), rows, cols)
+        self._ref = ctypes.byref(self._desc)
+
+    def dequantize(self, out=None):
+        """What the matrix stands for: bf16 [rows, cols], exact (out: such a tensor to write)."""
+        torch = _torch_module
+        if out is None:
+            out = torch.empty((self.rows, self.cols), dtype=torch.bfloat16, device=self.codes.device)
+        else:
+            _require(out, torch.bfloat16, "out", self.codes.device)
+            if out.shape != (self.rows, self.cols):
+                raise ValueError(f"out must have shape {(self.rows, self.cols)}")
+        _call("fairy2i_fp8_dequantize", self._index, self._ref, out.data_ptr())
+        return out
+
+    def transpose(self, out=None):
+        """The transposed matrix, scales along the other axis (fairy2i_fp8_transpose;
+        out: a Fp8Matrix to write)."""
+        out = _fp8_out(out, self.cols, self.rows, self.codes.device, "out")
+        if out.codes.data_ptr() == self.codes.data_ptr() or out.scales.data_ptr() == self.scales.data_ptr():
+            raise ValueError("out must be other memory than the matrix itself")
+        _call("fairy2i_fp8_transpose", self._index, self._ref, out._ref)
+        return out
+
+
+def _fp8_out(out, rows, cols, device, name):
+    if out is None:
+        return Fp8Matrix(rows, cols, device=device)
+    if not isinstance(out, Fp8Matrix):
+        raise TypeError(f"{name} must be a Fp8Matrix")
+    if out.codes.device != device:
+        raise ValueError(f"{name} is on {out.codes.device}, expected {device}")
+    if (out.rows, out.cols) != (rows, cols):
+        raise ValueError(f"{name} must be {rows} x {cols}, got {out.rows} x {out.cols}")
+    return out
+
+
+def _real_rows(x, name):
+    """(dtype, rows, cols, row stride) of a matrix of reals: float32 or bf16 [rows, cols], its pairs [rows, n, 2], or
+    complex64 [rows, n]; each row contiguous."""
+    torch = _torch_module or _torch()
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if x.dtype is torch.complex64:
+        if x.is_conj():
+            raise ValueError(f"{name} is a conjugated view: resolve_conj() it first")
+        if x.dim() != 2:
+            raise ValueError(f"{name} must be [rows, n] where it is complex")
+        dt, per = ACT_F32, 2
+    elif x.dtype is torch.float32 or x.dtype is torch.bfloat16:
+        if x.is_neg():
+            raise ValueError(f"{name} is a negated view: resolve_neg() it first")
+        dt, per = (ACT_F32 if x.dtype is torch.float32 else ACT_BF16), 1
+    else:
+        raise TypeError(f"{name} must be float32, bfloat16 or complex64, got {x.dtype}")
+    shape, stride = x.shape, x.stride()
+    if len(shape) == 3 and shape[2] == 2:
+        cols, whole = 2 * shape[1], stride[2] == 1 and (shape[1] == 1 or stride[1] == 2)
+    elif len(shape) == 2:
+        cols, whole = per * shape[1], shape[1] == 1 or stride[1] == 1
+    else:
+        raise ValueError(f"{name} must be [rows, cols] or [rows, n, 2]")
+    if not whole:
+        raise ValueError(f"{name}'s rows must be contiguous")
+    ld = per * stride[0] if shape[0] > 1 else cols
+    if ld < cols:
+        raise ValueError(f"{name}'s rows overlap")
+    return dt, shape[0], cols, ld
+
+
+def quantize_fp8(x, transposed=False, out=None):
+    """The 8-bit form of a matrix of reals (fairy2i_fp8_quantize).
+
+    x: float32 or bf16 [rows, cols], the pairs [rows, n, 2] or complex64 [rows,
+    n] (cols = 2n); rows may be columns of a wider tensor.  Returns a Fp8Matrix
+    rows x cols with blocks along the rows; with transposed=True the transposed
+    matrix, cols x rows, with blocks along the columns of x; with
+    transposed="both" the pair of them from one pass.  out: such a Fp8Matrix (or
+    pair) to write."""
+    dt, rows, cols, ld = _real_rows(x, "x")
+    if _lib is None:
+        load()
+    if transposed not in (False, True, "both"):
+        raise ValueError('transposed must be False, True or "both"')
+    if transposed == "both":
+        a, b = (None, None) if out is None else out
+    else:
+        a = b = out
+    direct = turned = None
+    if transposed is not True:
+        direct = _fp8_out(a, rows, cols, x.device, "out")
+    if transposed is not False:
+        turned = _fp8_out(b, cols, rows, x.device, "out")
+    _call("fairy2i_fp8_quantize", x.get_device(), x.data_ptr(), dt, ld, None if direct is None else direct._ref,
+          None if turned is None else turned._ref)
+    if transposed == "both":
+        return direct, turned
+    return turned if transposed else direct
+
+
+def gemm_fp8(A, B, out=None, dtype=None, accumulate=False, workspace=None):
+    """C = A B^T of two Fp8Matrix, A [M, K] and B [N, K] (fairy2i_gemm_fp8).
+
+    Returns C [M, N] in dtype (bfloat16 by default, or float32); out: such a
+    tensor to write, whose rows may be columns of a wider one; accumulate=True
+    adds to it.  With tokens in rows a layer of real form R (wl_realify) has
+    Y = gemm_fp8(X, R), G_X = gemm_fp8(G_Y, R transposed) and
+    G_R = gemm_fp8(G_Y transposed, X transposed)."""
+    torch = _torch_module or _torch()
+    for m, name in ((A, "A"), (B, "B")):
+        if not isinstance(m, Fp8Matrix):
+            raise TypeError(f"{name} must be a Fp8Matrix")
+    if A.cols != B.cols:
+        raise ValueError(f"A has {A.cols} columns, B {B.cols}")
+    index = A._index
+    if B._index != index:
+        raise ValueError(f"B is on {B.codes.device}, expected {A.codes.device}")
+    M, N = A.rows, B.rows
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty((M, N), dtype=torch.bfloat16 if dtype is None else dtype, device=A.codes.device)
+        ldc = N
+    else:
+        if not isinstance(out, torch.Tensor):
+            raise TypeError("out must be a torch.Tensor")
+        if out.get_device() != index:
+            raise ValueError(f"out is on {out.device}, expected {A.codes.device}")
+        if dtype is not None and out.dtype is not dtype:
+            raise TypeError(f"out must be {dtype}, got {out.dtype}")
+        if out.shape != (M, N) or (N > 1 and out.stride(1) != 1):
+            raise ValueError(f"out must have shape ({M}, {N}), each row contiguous")
+        ldc = out.stride(0) if M > 1 else N
+        if ldc < N:
+            raise ValueError("out's rows overlap")
+    if out.dtype is torch.bfloat16:
+        dt = ACT_BF16
+    elif out.dtype is torch.float32:
+        dt = ACT_F32
+    else:
+        raise TypeError(f"the product is bfloat16 or float32, not {out.dtype}")
+    if workspace is None:
+        need = _lib.fairy2i_gemm_fp8_workspace_bytes(M, N, A.cols)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
+    else:  # its size is the library's to check
+        _require(workspace, torch.uint8, "workspace", out.device)
+    _call("fairy2i_gemm_fp8", index, A._ref, B._ref, out.data_ptr(), dt, ldc, int(bool(accumulate)),
+          None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel())
+    return out
+
+
+def add_layernorm(x, gain, bias=None, delta=None, eps=1e-5, center=True, h_out=None, out=None, fp8=False):
+    """h = x + delta and its layer norm, or RMSNorm for center=False
+    (fairy2i_add_layernorm).
+
+    x, delta: complex64 [B, n] (delta may be None: h is x); gain, bias: float32
+    [2n], the real parts' values, then the imaginary parts' (bias may be None).
+    Returns (h, z, stats): z in bf16 [B, n, 2], or with fp8=True a Fp8Matrix B x
+    2n, what gemm_fp8 takes; stats float32 [B, 2], for layernorm_backward.
+    h_out: where h goes (x and delta themselves are allowed; by default a new
+    tensor, and x as it is where there is no delta); out: the z to write."""
+    torch = _torch_module or _torch()
+    lib = _lib or load()
+    # launch latency counts: everything is looked over in one expression, _check_layernorm names what is wrong
+    try:
+        index = x.get_device()
+        ok = (index >= 0 and x.dtype is torch.complex64 and x.is_contiguous() and not x.is_conj()
+              and gain.dtype is torch.float32 and gain.get_device() == index and gain.is_contiguous()
+              and (bias is None or (bias.dtype is torch.float32 and bias.get_device() == index
+                                    and bias.is_contiguous() and bias.shape == gain.shape))
+              and (delta is None or (delta.dtype is torch.complex64 and delta.get_device() == index
+                                     and delta.is_contiguous() and not delta.is_conj() and delta.shape == x.shape)))
+        B, n = x.shape
+        ok = ok and gain.shape == (2 * n,)
+    except (AttributeError, TypeError, ValueError):
+        ok = False
+    if not ok:
+        _check_layernorm(x, gain, bias, delta)
+    if h_out is not None:
+        _require(h_out, torch.complex64, "h_out", x.device)
+        if h_out.shape != x.shape or h_out.is_conj():
+            raise ValueError("h_out must have x's shape, and not be a conjugated view")
+    elif delta is not None:
+        h_out = torch.empty_like(x)
+    if fp8:
+        out = _fp8_out(out, B, 2 * n, x.device, "out")
+    elif out is None:
+        out = torch.empty((B, n, 2), dtype=torch.bfloat16, device=x.device)
+    else:
+        _require(out, torch.bfloat16, "out", x.device)
+        if out.shape != (B, n, 2):
+            raise ValueError(f"out must have shape ({B}, {n}, 2)")
+    stats = torch.empty((B, 2), dtype=torch.float32, device=x.device)
+    _call("fairy2i_add_layernorm", index, x.data_ptr(), None if delta is None else delta.data_ptr(), gain.data_ptr(),
+          None if bias is None else bias.data_ptr(), eps, int(bool(center)), B, n,
+          None if h_out is None else h_out.data_ptr(), None if fp8 else out.data_ptr(), out._ref if fp8 else None,
+          stats.data_ptr())
+    return x if h_out is None else h_out, out, stats
+
+
+def _check_layernorm(x, gain, bias, delta):
+    _check_norm(x, gain, delta)
+    if bias is not None:
+        _require(bias, _torch().float32, "bias", x.device)
+        if bias.shape != gain.shape:
+            raise ValueError("bias must have gain's shape")
+
+
+def layernorm_backward(dz, h, stats, gain, dh=None, center=True, bias=True, out=None, workspace=None):
+    """The gradient of add_layernorm (fairy2i_layernorm_backward).
+
+    dz: the gradient of z, bf16 [B, n, 2] or complex64 [B, n]; h, stats: what
+    add_layernorm returned; dh: complex64 [B, n], the gradient that reaches h by
+    the residual, or None; center: as there.  Returns (dx, dgain, dbias): dx
+    complex64 [B, n], of x and of delta alike (out: such a tensor to write, dh
+    and h themselves are allowed); dgain, dbias float32 [2n], dbias None for
+    bias=False."""
+    torch = _torch_module or _torch()
+    lib = _lib or load()
+    _require(h, torch.complex64, "h")
+    if h.dim() != 2:
+        raise ValueError("h must be [B, n]")
+    (B, n), dev, index = h.shape, h.device, h.get_device()
+    _require(dz, None, "dz", dev)
+    if dz.dtype is torch.bfloat16:
+        dt, shape = ACT_BF16, (B, n, 2)
+    elif dz.dtype is torch.complex64:
+        dt, shape = ACT_F32, (B, n)
+    else:
+        raise TypeError(f"dz must be bfloat16 or complex64, got {dz.dtype}")
+    if dz.shape != shape:
+        raise ValueError(f"dz must have shape {shape}, got {tuple(dz.shape)}")
+    _require(stats, torch.float32, "stats", dev)
+    if stats.shape != (B, 2):
+        raise ValueError(f"stats must have shape ({B}, 2)")
+    _require(gain, torch.float32, "gain", dev)
+    if gain.shape != (2 * n,):
+        raise ValueError(f"gain must have shape ({2 * n},), got {tuple(gain.shape)}")
+    for t, name in ((dh, "dh"), (out, "out")):
+        if t is not None:
+            _require(t, torch.complex64, name, dev)
+            if t.shape != h.shape:
+                raise ValueError(f"{name} must have h's shape")
+    for t, name in ((dz, "dz"), (h, "h"), (dh, "dh"), (out, "out")):
+        if t is not None and t.is_conj():
+            raise ValueError(f"{name} is a conjugated view: resolve_conj() it first")
+    dx = torch.empty_like(h) if out is None else out
+    sums = torch.empty(4 * n if bias else 2 * n, dtype=torch.float32, device=dev)
+    dgain, dbias = sums[:2 * n], sums[2 * n:] if bias else None
+    if workspace is None:
+        need = lib.fairy2i_layernorm_backward_workspace_bytes(B, n)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    else:  # its size is the library's to check
+        _require(workspace, torch.uint8, "workspace", dev)
+    _call("fairy2i_layernorm_backward", index, dz.data_ptr(), dt, h.data_ptr(), stats.data_ptr(), gain.data_ptr(),
+          None if dh is None else dh.data_ptr(), int(bool(center)), B, n, dx.data_ptr(), dgain.data_ptr(),
+          dbias.data_ptr() if bias else None, None if workspace is None else workspace.data_ptr(),
+          0 if workspace is None else workspace.numel())
+    return dx, dgain, dbias

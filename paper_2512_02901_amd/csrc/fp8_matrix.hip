@@ -1,0 +1,256 @@
+// 8-bit matrices: from float32 or bf16 along the rows, along the columns
+// (transposed) or both in one pass; an 8-bit matrix turned; and back to bf16.
+//
+// A product C = A B^T on the matrix cores wants both operands along the axis
+// that is summed over, and a block of 128 along that axis to share its scale.
+// A training step's three products sum over three axes, so X, G_Y and R are
+// wanted in both forms.  A block of threads takes 128 x 128 reals into
+// registers once: a thread holds 8 rows x 8 columns, so a row's maximum is 8
+// values and a DPP row of 16 lanes, a column's 8 values, the wave's four DPP
+// rows and four waves.  The turned codes go through 16 KB of LDS (8-byte slots
+// exchanged by column so that neither side conflicts) and leave as whole
+// 128-byte rows.
+#include <algorithm>
+
+#include "fp8.h"
+
+namespace fairy2i {
+
+namespace {
+
+enum { kF32, kBf16, kFp8 };  // what is read
+
+struct Source {
+  const void* x;
+  const uint8_t* scales;  // kFp8
+  int64_t ld;             // elements of a row
+};
+
+// Eight neighbours of row r from column c on; zeros outside.
+template <int SRC>
+__device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_t r, int64_t c, float v[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+  if (r >= rows) return;
+  if constexpr (SRC == kFp8) {  // rows are padded with zeros to whole blocks
+    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.x) + r * s.ld + c);
+    const float unit = fp8_power(s.scales[fp8_scale_at(rows, r, c / kFp8Block)]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int word = (int)(h ? w.y : w.x);
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(word, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(word, true);
+      v[4 * h] = lo[0] * unit;
+      v[4 * h + 1] = lo[1] * unit;
+      v[4 * h + 2] = hi[0] * unit;
+      v[4 * h + 3] = hi[1] * unit;
+    }
+  } else if constexpr (SRC == kF32) {
+    const float* p = static_cast<const float*>(s.x) + r * s.ld + c;
+    if (c + 8 <= cols) {
+      const f32x4_any a = reinterpret_cast<const f32x4_any*>(p)[0], b = reinterpret_cast<const f32x4_any*>(p)[1];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[j] = a[j];
+        v[4 + j] = b[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < cols) v[j] = p[j];
+    }
+  } else {
+    const uint16_t* p = static_cast<const uint16_t*>(s.x) + r * s.ld + c;
+    if (c + 8 <= cols) {
+      const u32x4_any a = *reinterpret_cast<const u32x4_any*>(p);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v[2 * j] = bf16_lo(a[j]);
+        v[2 * j + 1] = bf16_hi(a[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < cols) v[j] = __uint_as_float((uint32_t)p[j] << 16);
+    }
+  }
+}
+
+template <int SRC, bool DIRECT, bool TURNED>
+__global__ __launch_bounds__(256) void fp8_quantize_kernel(Source src, int64_t rows, int64_t cols, int col_tiles,
+                                                           uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                           uint8_t* __restrict__ codes_t,
+                                                           uint8_t* __restrict__ scales_t) {
+  __shared__ __attribute__((aligned(16))) uint2 tile[TURNED ? 128 * 16 : 1];
+  __shared__ uint32_t tops[TURNED ? 4 * 128 : 1];
+  const int t = threadIdx.x, cg = t & 15, rg = t >> 4;
+  const int64_t rb = blockIdx.x / (uint32_t)col_tiles, cb = blockIdx.x % (uint32_t)col_tiles;
+  const int64_t r0 = rb * 128 + 8 * rg, c0 = cb * 128 + 8 * cg;
+  float v[8][8];
+#pragma unroll
+  for (int p = 0; p < 8; ++p) load8<SRC>(src, rows, cols, r0 + p, c0, v[p]);
+
+  if constexpr (TURNED) {
+    uint32_t top[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      top[j] = 0;
+#pragma unroll
+      for (int p = 0; p < 8; ++p) top[j] = max(top[j], fp8_magnitude(v[p][j]));
+      top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
+      top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
+    }
+    if ((t & 63) < 16) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) tops[(t >> 6) * 128 + 8 * cg + j] = top[j];
+    }
+  }
+  if constexpr (DIRECT) {
+    const int64_t ld = (cols + 127) / 128 * 128;
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, fp8_magnitude(v[p][j]));
+      const int byte = fp8_scale_byte(row16_max(top));
+      const float inv = fp8_power(254 - byte);
+      const uint2 w = make_uint2(fp8_codes4(v[p][0], v[p][1], v[p][2], v[p][3], inv),
+                                 fp8_codes4(v[p][4], v[p][5], v[p][6], v[p][7], inv));
+      if (r0 + p < rows) {
+        *reinterpret_cast<uint2*>(codes + (r0 + p) * ld + c0) = w;
+        if (cg == 0) scales[fp8_scale_at(rows, r0 + p, cb)] = (uint8_t)byte;
+      }
+    }
+  }
+  if constexpr (TURNED) {
+    __syncthreads();
+    const int64_t ld = (rows + 127) / 128 * 128;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int c = 8 * cg + j;
+      const int byte = fp8_scale_byte(max(max(tops[c], tops[128 + c]), max(tops[256 + c], tops[384 + c])));
+      const float inv = fp8_power(254 - byte);
+      tile[c * 16 + (rg ^ cg)] = make_uint2(fp8_codes4(v[0][j], v[1][j], v[2][j], v[3][j], inv),
+                                            fp8_codes4(v[4][j], v[5][j], v[6][j], v[7][j], inv));
+      if (rg == j && cb * 128 + c < cols) scales_t[fp8_scale_at(cols, cb * 128 + c, rb)] = (uint8_t)byte;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = 32 * i + (t >> 3), pair = t & 7, swap = (c >> 3) & 1;
+      const uint4 w = *reinterpret_cast<const uint4*>(&tile[c * 16 + 2 * (pair ^ (c >> 4))]);
+      if (cb * 128 + c < cols)
+        *reinterpret_cast<uint4*>(codes_t + (cb * 128 + c) * ld + rb * 128 + 16 * pair) =
+            swap ? make_uint4(w.z, w.w, w.x, w.y) : w;
+    }
+  }
+}
+
+template <int SRC>
+hipError_t launch(const Source& src, int64_t rows, int64_t cols, const fairy2i_fp8_matrix* direct,
+                  const fairy2i_fp8_matrix* turned, hipStream_t s) {
+  const int64_t row_tiles = (rows + 127) / 128, col_tiles = (cols + 127) / 128;
+  const dim3 grid((unsigned)(row_tiles * col_tiles)), block(256);
+  uint8_t *c = direct ? direct->codes : nullptr, *f = direct ? direct->scales : nullptr;
+  uint8_t *ct = turned ? turned->codes : nullptr, *ft = turned ? turned->scales : nullptr;
+  if (direct && turned)
+    hipLaunchKernelGGL((fp8_quantize_kernel<SRC, true, true>), grid, block, 0, s, src, rows, cols, (int)col_tiles, c,
+                       f, ct, ft);
+  else if (direct)
+    hipLaunchKernelGGL((fp8_quantize_kernel<SRC, true, false>), grid, block, 0, s, src, rows, cols, (int)col_tiles, c,
+                       f, ct, ft);
+  else
+    hipLaunchKernelGGL((fp8_quantize_kernel<SRC, false, true>), grid, block, 0, s, src, rows, cols, (int)col_tiles, c,
+                       f, ct, ft);
+  return hipGetLastError();
+}
+
+// Eight codes a thread -> eight bf16 values: exact (four significant bits, a
+// normal power of two).
+__global__ __launch_bounds__(256) void fp8_dequantize_kernel(Source src, int64_t rows, int64_t cols,
+                                                             uint16_t* __restrict__ out) {
+  const int64_t groups = src.ld / 8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * groups; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / groups, c = i % groups * 8;
+    if (c >= cols) continue;
+    float v[8];
+    load8<kFp8>(src, rows, cols, r, c, v);
+    uint16_t* p = out + r * cols + c;
+    if (c + 8 <= cols) {
+      *reinterpret_cast<u32x4_any*>(p) =
+          u32x4_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (c + j < cols) p[j] = bf16_one(v[j]);
+    }
+  }
+}
+
+// A launch takes fewer than 2^32 threads.
+bool too_many_tiles(int64_t rows, int64_t cols) {
+  return ((rows + 127) / 128) * ((cols + 127) / 128) >= ((int64_t)1 << 24);
+}
+
+}  // namespace
+
+}  // namespace fairy2i
+
+using namespace fairy2i;
+
+extern "C" {
+
+size_t fairy2i_fp8_codes_bytes(int64_t rows, int64_t cols) {
+  if (rows < 1 || cols < 1 || rows > kFp8MostSide || cols > kFp8MostSide) return 0;
+  return (size_t)(rows * fp8_ld(cols));
+}
+
+size_t fairy2i_fp8_scales_bytes(int64_t rows, int64_t cols) {
+  if (rows < 1 || cols < 1 || rows > kFp8MostSide || cols > kFp8MostSide) return 0;
+  return (size_t)((cols + 511) / 512 * rows * 4);
+}
+
+fairy2i_status fairy2i_fp8_quantize(const void* x, int32_t dtype, int64_t ld, const fairy2i_fp8_matrix* direct,
+                                    const fairy2i_fp8_matrix* turned, void* stream) {
+  if (!x || (!direct && !turned)) return FAIRY2I_ERR_NULL;
+  for (const fairy2i_fp8_matrix* m : {direct, turned})
+    if (m) {
+      const fairy2i_status st = fp8_check(m);
+      if (st != FAIRY2I_OK) return st;
+    }
+  const int64_t rows = direct ? direct->rows : turned->cols, cols = direct ? direct->cols : turned->rows;
+  if (turned && (turned->cols != rows || turned->rows != cols)) return FAIRY2I_ERR_SHAPE;
+  if (ld < cols) return FAIRY2I_ERR_SHAPE;
+  if (dtype != FAIRY2I_ACT_F32 && dtype != FAIRY2I_ACT_BF16) return FAIRY2I_ERR_DTYPE;
+  if (too_many_tiles(rows, cols)) return FAIRY2I_ERR_UNSUPPORTED;
+  const Source src{x, nullptr, ld};
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = dtype == FAIRY2I_ACT_F32 ? launch<kF32>(src, rows, cols, direct, turned, s)
+                                                : launch<kBf16>(src, rows, cols, direct, turned, s);
+  return e == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
+}
+
+fairy2i_status fairy2i_fp8_transpose(const fairy2i_fp8_matrix* in, const fairy2i_fp8_matrix* out, void* stream) {
+  for (const fairy2i_fp8_matrix* m : {in, out}) {
+    const fairy2i_status st = fp8_check(m);
+    if (st != FAIRY2I_OK) return st;
+  }
+  if (out->rows != in->cols || out->cols != in->rows) return FAIRY2I_ERR_SHAPE;
+  if (too_many_tiles(in->rows, in->cols)) return FAIRY2I_ERR_UNSUPPORTED;
+  const Source src{in->codes, in->scales, fp8_ld(in->cols)};
+  const hipError_t e = launch<kFp8>(src, in->rows, in->cols, nullptr, out, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
+}
+
+fairy2i_status fairy2i_fp8_dequantize(const fairy2i_fp8_matrix* in, void* out, void* stream) {
+  const fairy2i_status st = fp8_check(in);
+  if (st != FAIRY2I_OK) return st;
+  if (!out) return FAIRY2I_ERR_NULL;
+  const Source src{in->codes, in->scales, fp8_ld(in->cols)};
+  const int64_t work = in->rows * (src.ld / 8);
+  const unsigned blocks = (unsigned)std::min<int64_t>((work + 255) / 256, 1 << 20);
+  hipLaunchKernelGGL(fp8_dequantize_kernel, dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(stream), src,
+                     in->rows, in->cols, static_cast<uint16_t*>(out));
+  return hipGetLastError() == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,121 @@
+"""Host-side checks of the training entry points (no GPU): sizes, and arguments
+rejected before anything is launched."""
+import ctypes
+
+import pytest
+
+from paper_2512_02901_amd import binding
+from paper_2512_02901_amd.binding import ACT_BF16, ACT_F32, ACT_I8, ERR_DTYPE, ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ERR_WORKSPACE, Fp8Desc
+
+P = ctypes.c_void_p(0x1000)  # never used: every call below is refused first
+MOST = 1 << 22
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return binding.load()
+
+
+def mat(rows=4, cols=300, codes=0x1000, scales=0x1000):
+    return ctypes.byref(Fp8Desc(codes, scales, rows, cols))
+
+
+def test_bytes(lib):
+    for rows, cols, codes, scales in ((1, 1, 128, 4), (3, 128, 384, 12), (3, 129, 768, 12), (5, 512, 2560, 20), (5, 513, 3200, 40),
+                                      (MOST, MOST, 1 << 44, 1 << 37)):
+        assert lib.fairy2i_fp8_codes_bytes(rows, cols) == codes
+        assert lib.fairy2i_fp8_scales_bytes(rows, cols) == scales
+    for rows, cols in ((0, 1), (1, 0), (-1, 4), (MOST + 1, 1), (1, MOST + 1)):
+        assert lib.fairy2i_fp8_codes_bytes(rows, cols) == 0
+        assert lib.fairy2i_fp8_scales_bytes(rows, cols) == 0
+
+
+def bad_matrices(call):
+    assert call(None) == ERR_NULL
+    assert call(mat(codes=None)) == ERR_NULL
+    assert call(mat(scales=None)) == ERR_NULL
+    for kw in (dict(rows=0), dict(cols=0), dict(rows=-3), dict(rows=MOST + 1), dict(cols=MOST + 1)):
+        assert call(mat(**kw)) == ERR_SHAPE, kw
+    assert call(mat(codes=0x1008)) == ERR_UNSUPPORTED
+    assert call(mat(scales=0x1002)) == ERR_UNSUPPORTED
+
+
+def test_quantize_validation(lib):
+    f = lib.fairy2i_fp8_quantize
+    bad_matrices(lambda m: f(P, ACT_F32, MOST + 9, m, None, None))
+    bad_matrices(lambda m: f(P, ACT_F32, MOST + 9, None, m, None))
+    assert f(None, ACT_F32, 300, mat(), None, None) == ERR_NULL
+    assert f(P, ACT_F32, 299, mat(), None, None) == ERR_SHAPE
+    assert f(P, ACT_F32, 3, None, mat(), None) == ERR_SHAPE                    # turned: x has 4 columns
+    assert f(P, ACT_F32, 300, mat(), mat(), None) == ERR_SHAPE                 # not each other's transpose
+    assert f(P, ACT_F32, 300, mat(), mat(rows=300, cols=5), None) == ERR_SHAPE
+    for dt in (ACT_I8, -1, 3):
+        assert f(P, dt, 300, mat(), None, None) == ERR_DTYPE
+    assert f(P, ACT_F32, MOST, mat(rows=1 << 21, cols=1 << 17), None, None) == ERR_UNSUPPORTED  # 2^24 tiles
+
+
+def test_transpose_validation(lib):
+    f = lib.fairy2i_fp8_transpose
+    bad_matrices(lambda m: f(m, mat(), None))
+    bad_matrices(lambda m: f(mat(), m, None))
+    assert f(mat(), mat(), None) == ERR_SHAPE
+    assert f(mat(), mat(rows=300, cols=3), None) == ERR_SHAPE
+    assert f(mat(rows=1 << 21, cols=1 << 17), mat(rows=1 << 17, cols=1 << 21), None) == ERR_UNSUPPORTED
+
+
+def test_dequantize_validation(lib):
+    f = lib.fairy2i_fp8_dequantize
+    bad_matrices(lambda m: f(m, P, None))
+    assert f(mat(), None, None) == ERR_NULL
+
+
+def test_gemm_validation(lib):
+    def f(a=mat(), b=mat(rows=7), c=P, dt=ACT_BF16, ldc=7, acc=0, ws=P, size=1 << 40):
+        return lib.fairy2i_gemm_fp8(a, b, c, dt, ldc, acc, ws, size, None)
+    bad_matrices(lambda m: f(a=m))
+    bad_matrices(lambda m: f(b=m))
+    assert f(c=None) == ERR_NULL
+    for kw in (dict(b=mat(cols=301)), dict(ldc=6), dict(acc=2), dict(acc=-1)):
+        assert f(**kw) == ERR_SHAPE, kw
+    assert f(dt=ACT_I8) == ERR_DTYPE
+    assert f(a=mat(rows=MOST), b=mat(rows=MOST), ldc=MOST) == ERR_UNSUPPORTED
+    need = lib.fairy2i_gemm_fp8_workspace_bytes
+    assert need(0, 1, 1) == need(1, 0, 1) == need(1, 1, 0) == need(MOST + 1, 1, 1) == 0
+    few = need(3, 64, 8192)  # few tiles over a long axis: split
+    assert few > 0 and few % (4 * 3 * 64) == 0
+    a, b = mat(rows=3, cols=8192), mat(rows=64, cols=8192)
+    assert f(a=a, b=b, ldc=64, size=few - 1) == ERR_WORKSPACE
+    assert f(a=a, b=b, ldc=64, ws=None) == ERR_WORKSPACE
+    assert f(a=a, b=b, ldc=64, ws=ctypes.c_void_p(0x1002)) == ERR_WORKSPACE
+
+
+def test_layernorm_validation(lib):
+    def f(x=P, delta=P, gain=P, bias=P, eps=1e-5, center=1, B=4, n=150, h=P, z=P, z8=None, stats=P):
+        return lib.fairy2i_add_layernorm(x, delta, gain, bias, eps, center, B, n, h, z, z8, stats, None)
+    for kw in (dict(x=None), dict(gain=None), dict(stats=None), dict(z=None)):
+        assert f(**kw) == ERR_NULL, kw
+    for kw in (dict(B=0), dict(B=1 << 31), dict(n=0), dict(n=(1 << 24) + 1), dict(eps=0.0), dict(eps=-1.0), dict(eps=float("inf")),
+               dict(eps=float("nan")), dict(center=2), dict(center=-1)):
+        assert f(**kw) == ERR_SHAPE, kw
+    assert f(z8=mat()) == ERR_UNSUPPORTED
+    bad = lambda m: f(z=None, z8=m)  # noqa: E731
+    assert bad(mat(codes=None)) == bad(mat(scales=None)) == ERR_NULL
+    assert bad(mat(rows=5)) == bad(mat(cols=299)) == bad(mat(rows=0)) == ERR_SHAPE
+    assert bad(mat(codes=0x1008)) == bad(mat(scales=0x1001)) == ERR_UNSUPPORTED
+
+
+def test_layernorm_backward_validation(lib):
+    def f(dz=P, dt=ACT_BF16, h=P, stats=P, gain=P, dh=P, center=1, B=600, n=150, dx=P, dgain=P, dbias=P, ws=P, size=1 << 40):
+        return lib.fairy2i_layernorm_backward(dz, dt, h, stats, gain, dh, center, B, n, dx, dgain, dbias, ws, size, None)
+    for kw in (dict(dz=None), dict(h=None), dict(stats=None), dict(gain=None), dict(dx=None), dict(dgain=None)):
+        assert f(**kw) == ERR_NULL, kw
+    for kw in (dict(B=0), dict(B=1 << 31), dict(n=0), dict(n=(1 << 24) + 1), dict(center=2)):
+        assert f(**kw) == ERR_SHAPE, kw
+    assert f(dt=ACT_I8) == ERR_DTYPE
+    for B, n in ((600, 150), (5, 9000)):
+        need = lib.fairy2i_layernorm_backward_workspace_bytes(B, n)
+        assert need > 0
+        assert f(B=B, n=n, size=need - 1) == ERR_WORKSPACE
+        assert f(B=B, n=n, ws=None) == ERR_WORKSPACE
+        assert f(B=B, n=n, ws=ctypes.c_void_p(0x1002)) == ERR_WORKSPACE
+    assert lib.fairy2i_layernorm_backward_workspace_bytes(0, 8) == lib.fairy2i_layernorm_backward_workspace_bytes(8, 0) == 0

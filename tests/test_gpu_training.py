@@ -1,0 +1,653 @@
+"""The training operators (Fp8Matrix, quantize_fp8, gemm_fp8, add_layernorm,
+layernorm_backward) against oracle/training.py in 64 bits.  Tolerances, from
+the arithmetic (u = 2^-24, half a step of float32):
+
+quantise   every step is exact but the rounding, which is the definition's:
+           codes and scale bytes are equal.  So are the transposed matrix's, and
+           what it all stands for.
+gemm       a product of two codes is exact.  The matrix cores sum small groups
+           of products keeping 13 bits below the group's largest: a term loses
+           at most 2^-13 of it, eight terms of a group 7 * 2^-13 < 2^-10 of the
+           group's sum |a||b|; the rest are float32 additions, one or two for
+           32 products.  With A = sum |a||b|: 2^-10 A + (K / 16 + 40) u A, and
+           half a step of the result's type.  Products whose exponents are
+           within 2^10 of each other and whose sums fit 24 bits are exact.
+norm       h is one float32 addition: equal.  stats: sums in double, one
+           rounding of mu (u), three of r (mean, square root, cast are double:
+           one, kept as 4 u).  z: two subtractions, r, two factors, bias: within
+           8 u (|t| + |bias|), t = (h - mu) r gain, and half a step of bf16
+           (2^-8) or of e4m3 (2^-4, below the smallest normal 2^-10 of the
+           block's power of two).
+backward   y: subtraction, factor: 2 u |y|; w: u |w|.  A token's sums are float32
+           trees: at most 8 * 8 values in a thread and 6 + 8 additions, so the
+           means are within 90 u of the mean of absolute values.  dx: 4 more
+           roundings of each term.  Sums over tokens: one rounding for each
+           token of a block (B / 256 and 8 more) and 4 for a term.
+"""
+import numpy as np
+import pytest
+
+from oracle import training as tr
+
+pytestmark = pytest.mark.gpu
+
+u = 2.0 ** -24
+
+
+def dev(a, gpu):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).to(gpu)
+
+
+def host(t):
+    import torch
+    return t.float().cpu().numpy() if t.dtype == torch.bfloat16 else t.cpu().numpy()
+
+
+def raw(m):
+    """(codes, scale bytes) of a Fp8Matrix, bytes of blocks that are not there as 0."""
+    import torch
+    codes, scales = host(m.codes.view(torch.uint8)), host(m.scales).copy()
+    for k in range(-(-m.cols // 128), 4 * scales.shape[0]):
+        scales[k // 4, :, k % 4] = 0
+    return codes, scales
+
+
+def same(m, want):
+    codes, scales = raw(m)
+    np.testing.assert_array_equal(scales, want[1])
+    # any NaN is one
+    np.testing.assert_array_equal(np.where(codes & 127 == 127, 127, codes), np.where(want[0] & 127 == 127, 127, want[0]))
+
+
+def fp8(gpu, codes, scales, cols):
+    import torch
+    import paper_2512_02901_amd as f2
+    return f2.Fp8Matrix(codes.shape[0], cols, dev(codes, gpu).view(torch.float8_e4m3fn), dev(scales, gpu))
+
+
+def reals(rows, cols, seed, spread=1.0):
+    rng = np.random.default_rng((seed, rows, cols))
+    x = rng.standard_normal((rows, cols)) * np.exp(spread * rng.standard_normal((rows, 1)))
+    return (x * np.exp(0.5 * rng.standard_normal((1, cols)))).astype(np.float32)
+
+
+# ---------------------------------------------------------------- quantise
+
+
+@pytest.mark.parametrize("rows, cols", [(1, 1), (1, 128), (128, 1), (3, 130), (127, 129), (128, 128), (129, 127), (5, 511), (2, 513),
+                                        (200, 1030), (513, 260)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_quantise(gpu, rows, cols, dtype):
+    import paper_2512_02901_amd as f2
+    x = dev(reals(rows, cols, 1), gpu)
+    x = x if dtype == "float32" else x.bfloat16()
+    want, turned = tr.quantize(host(x)), tr.quantize(host(x).T)
+    same(f2.quantize_fp8(x), want)
+    same(f2.quantize_fp8(x, transposed=True), turned)
+    a, b = f2.quantize_fp8(x, transposed="both")
+    same(a, want)
+    same(b, turned)
+    for m, w, shape in ((a, want, (rows, cols)), (b, turned, (cols, rows))):
+        v = m.dequantize()
+        assert tuple(v.shape) == shape
+        np.testing.assert_array_equal(host(v), tr.dequantize(*w, shape[1]))
+    t = a.transpose()
+    same(t, tr.quantize(tr.dequantize(*want, cols).T))
+    same(t.transpose(), tr.quantize(tr.dequantize(*raw(t), rows).T))
+
+
+def test_every_midpoint_and_the_values_beside_it(gpu):
+    import paper_2512_02901_amd as f2
+    grid = tr.E4M3[:127]
+    mid = ((grid[1:] + grid[:-1]) / 2).astype(np.float32)
+    v = np.concatenate([grid.astype(np.float32), mid, np.nextafter(mid, np.float32(0)), np.nextafter(mid, np.float32(500))])
+    v = v[v <= 448]
+    v = np.concatenate([v, -v])
+    x = np.zeros((-(-len(v) // 127), 128), np.float32)
+    x[:, 0] = 448.0  # the block's power of two is 1
+    flat = np.zeros(x.shape[0] * 127, np.float32)
+    flat[:len(v)] = v
+    x[:, 1:] = flat.reshape(-1, 127)
+    for scale in (1.0, 2.0 ** -100, 2.0 ** 110):
+        y = (x * np.float32(scale)).astype(np.float32)
+        a, b = f2.quantize_fp8(dev(y, gpu), transposed="both")
+        same(a, tr.quantize(y))
+        same(b, tr.quantize(y.T))
+
+
+def test_block_maxima_at_their_borders_and_extremes(gpu):
+    import paper_2512_02901_amd as f2
+    big = np.float32(3.4028235e38)
+    tops = [0.0, 448.0, np.nextafter(np.float32(448), np.float32(500)), 224.0, np.nextafter(np.float32(224), np.float32(0)), 1e-45, 1e-38,
+            2.0 ** -117, 2.0 ** -109, 2.0 ** -126, 448 * 2.0 ** 119, big, 1.0, 1.75, 1.7500001]
+    x = reals(len(tops), 256, 2)
+    x = x / np.abs(x).max(1, keepdims=True) * 0.99
+    x = (x * np.array(tops)[:, None]).astype(np.float32)
+    x[:, 200] = np.array(tops, np.float32)
+    x[:, 7] = -np.array(tops, np.float32)
+    a, b = f2.quantize_fp8(dev(x, gpu), transposed="both")
+    same(a, tr.quantize(x))
+    same(b, tr.quantize(x.T))
+    assert np.isfinite(host(a.dequantize())).all()
+
+
+def test_values_that_are_not_finite(gpu):
+    import paper_2512_02901_amd as f2
+    x = reals(130, 300, 3)
+    x[0, 0], x[5, 200], x[129, 299], x[64, 128] = np.nan, np.inf, -np.inf, np.nan
+    x[7, 128:256] = np.inf  # a whole block
+    a, b = f2.quantize_fp8(dev(x, gpu), transposed="both")
+    same(a, tr.quantize(x))
+    same(b, tr.quantize(x.T))
+    v = host(a.dequantize())
+    np.testing.assert_array_equal(np.isnan(v), ~np.isfinite(x))
+    np.testing.assert_array_equal(np.isnan(host(a.transpose().dequantize())), ~np.isfinite(x.T))
+    # in a product they reach their row's (or column's) results, no others
+    c = host(f2.gemm_fp8(a, f2.quantize_fp8(dev(np.ones((3, 300), np.float32), gpu)), dtype=__import__("torch").float32))
+    np.testing.assert_array_equal(np.isnan(c).all(1), (~np.isfinite(x)).any(1))
+    np.testing.assert_array_equal(np.isnan(c).any(1), (~np.isfinite(x)).any(1))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "complex64", "pairs"])
+def test_quantise_views(gpu, dtype):
+    """Rows that are columns of a wider tensor, at odd addresses."""
+    import torch
+    import paper_2512_02901_amd as f2
+    x = dev(reals(70, 402, 4), gpu)
+    if dtype == "bfloat16":
+        x = x.bfloat16()
+    elif dtype == "complex64":
+        x = torch.view_as_complex(x.reshape(70, 201, 2))
+    elif dtype == "pairs":
+        x = x.bfloat16().reshape(70, 201, 2)
+    for lo, hi in ((1, 200), (3, 131), (5, 6), (0, 201)):
+        part = x[:, lo:hi]
+        v = host(torch.view_as_real(part).float() if dtype == "complex64" else part).reshape(70, -1)
+        a, b = f2.quantize_fp8(part, transposed="both")
+        same(a, tr.quantize(v))
+        same(b, tr.quantize(v.T))
+    one = x[3:4, 1:200]  # one row: its stride says nothing
+    v = host(torch.view_as_real(one).float() if dtype == "complex64" else one).reshape(1, -1)
+    same(f2.quantize_fp8(one), tr.quantize(v))
+
+
+def test_nothing_around_the_outputs_changes(gpu):
+    import torch
+    import paper_2512_02901_amd as f2
+    rows, cols = 131, 267
+    x = dev(reals(rows, cols, 5), gpu)
+
+    def framed(r, c):
+        cp, ng = -(-c // 128) * 128, -(-c // 512)
+        cb = torch.full((r * cp + 512,), 0xA5, dtype=torch.uint8, device=gpu)
+        sb = torch.full((ng * r * 4 + 512,), 0xA5, dtype=torch.uint8, device=gpu)
+        m = f2.Fp8Matrix(r, c, cb[256:256 + r * cp].view(r, cp).view(torch.float8_e4m3fn), sb[256:256 + ng * r * 4].view(ng, r, 4))
+        return m, cb, sb
+
+    def kept(bufs):
+        for buf in bufs:
+            h = host(buf)
+            assert (h[:256] == 0xA5).all() and (h[-256:] == 0xA5).all()
+
+    a, *ab = framed(rows, cols)
+    b, *bb = framed(cols, rows)
+    t, *tb = framed(cols, rows)
+    f2.quantize_fp8(x, transposed="both", out=(a, b))
+    a.transpose(out=t)
+    buf = torch.full((rows * cols + 64,), 7.0, dtype=torch.bfloat16, device=gpu)
+    a.dequantize(out=buf[31:31 + rows * cols].view(rows, cols))
+    kept(ab + bb + tb)
+    assert (host(buf)[:31] == 7).all() and (host(buf)[31 + rows * cols:] == 7).all()
+    np.testing.assert_array_equal(host(buf)[31:31 + rows * cols].reshape(rows, cols), tr.dequantize(*raw(a), cols))
+    same(t, tr.quantize(tr.dequantize(*raw(a), cols).T))
+    for dtype, off in ((torch.bfloat16, 3), (torch.float32, 1)):
+        out = torch.full((rows * (cols + 5) + 64,), 7.0, dtype=dtype, device=gpu)
+        c = out[off:off + rows * (cols + 5)].view(rows, cols + 5)[:, 2:2 + cols]
+        f2.gemm_fp8(f2.quantize_fp8(x), f2.quantize_fp8(dev(reals(cols, cols, 6), gpu)), out=c)
+        h = host(out)
+        inside = np.zeros(h.size, bool)
+        inside[off:off + rows * (cols + 5)].reshape(rows, cols + 5)[:, 2:2 + cols] = True
+        assert (h[~inside] == 7).all() and (h[inside] != 7).any()
+
+
+# -------------------------------------------------------------------- gemm
+
+
+def operand(gpu, rows, cols, seed, spread=1.0):
+    codes, scales = tr.quantize(reals(rows, cols, seed, spread))
+    return fp8(gpu, codes, scales, cols), tr.dequantize(codes, scales, cols)
+
+
+def gemm_check(got, a, b, dtype, before=None):
+    want, A = a @ b.T, np.abs(a) @ np.abs(b).T
+    tol = (2.0 ** -10 + (a.shape[1] / 16 + 40) * u) * A
+    if before is not None:
+        want = want + before
+        tol = tol + u * np.abs(want)
+    tol = tol + (2.0 ** -8 if dtype == "bfloat16" else u) * (np.abs(want) + tol)
+    err = np.abs(host(got).astype(np.float64) - want)
+    assert (err <= tol).all(), (err / np.maximum(tol, 1e-300)).max()
+
+
+SHAPES = [(1, 1, 1), (1, 16, 128), (16, 1, 129), (3, 5, 700), (63, 65, 128), (64, 64, 1024), (65, 130, 513), (127, 129, 2000),
+          (128, 640, 384), (300, 257, 1100), (1, 2000, 3000), (77, 33, 9000), (1030, 1290, 260), (2049, 1600, 150)]
+
+
+@pytest.mark.parametrize("M, N, K", SHAPES)
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_gemm(gpu, M, N, K, dtype):
+    import torch
+    import paper_2512_02901_amd as f2
+    (A, a), (B, b) = operand(gpu, M, K, 7), operand(gpu, N, K, 8)
+    c = f2.gemm_fp8(A, B, dtype=getattr(torch, dtype))
+    assert c.dtype is getattr(torch, dtype) and tuple(c.shape) == (M, N)
+    gemm_check(c, a, b, dtype)
+    again = f2.gemm_fp8(A, B, dtype=getattr(torch, dtype))
+    assert torch.equal(c, again)
+    # added to what is there
+    before = dev(reals(M, N, 9), gpu).to(c.dtype)
+    out = before.clone()
+    assert f2.gemm_fp8(A, B, out=out, accumulate=True) is out
+    gemm_check(out, a, b, dtype, host(before).astype(np.float64))
+
+
+@pytest.mark.parametrize("M, N, K", [(37, 70, 300), (300, 200, 1500), (129, 1100, 640), (2050, 1700, 200), (9, 100, 9000)])
+def test_gemm_of_small_integers_is_exact(gpu, M, N, K):
+    """Codes 0, +-1, +-2, +-3 with powers of two: every sum is exact, so any mistaken index shows."""
+    import torch
+    import paper_2512_02901_amd as f2
+    rng = np.random.default_rng((10, M, N, K))
+    code = np.array([0x00, 0x38, 0x40, 0x44, 0xB8, 0xC0, 0xC4], np.uint8)
+
+    def one(rows):
+        cp, ng = -(-K // 128) * 128, -(-K // 512)
+        codes = np.zeros((rows, cp), np.uint8)
+        codes[:, :K] = code[rng.integers(0, len(code), (rows, K))]
+        return codes, rng.integers(126, 129, (ng, rows, 4)).astype(np.uint8)
+
+    (ca, sa), (cb, sb) = one(M), one(N)
+    want = tr.dequantize(ca, sa, K) @ tr.dequantize(cb, sb, K).T
+    got = f2.gemm_fp8(fp8(gpu, ca, sa, K), fp8(gpu, cb, sb, K), dtype=torch.float32)
+    np.testing.assert_array_equal(host(got), want)
+
+
+def test_gemm_scales_far_apart(gpu):
+    import torch
+    import paper_2512_02901_amd as f2
+    x, w = reals(40, 700, 11), reals(30, 700, 12)
+    x[:, :128] *= np.float32(2.0 ** 60)
+    x[:, 512:640] *= np.float32(2.0 ** -60)
+    w[:, 512:640] *= np.float32(2.0 ** 100)
+    w[:, :128] *= np.float32(2.0 ** -80)
+    (ca, sa), (cb, sb) = tr.quantize(x), tr.quantize(w)
+    got = f2.gemm_fp8(fp8(gpu, ca, sa, 700), fp8(gpu, cb, sb, 700), dtype=torch.float32)
+    gemm_check(got, tr.dequantize(ca, sa, 700), tr.dequantize(cb, sb, 700), "float32")
+
+
+def test_gemm_ignores_scale_bytes_past_the_columns(gpu):
+    import torch
+    import paper_2512_02901_amd as f2
+    codes, scales = tr.quantize(reals(50, 200, 13))
+    scales[:, :, 2:] = 255
+    m = fp8(gpu, codes, scales, 200)
+    v = tr.dequantize(codes, scales, 200)
+    gemm_check(f2.gemm_fp8(m, m, dtype=torch.float32), v, v, "float32")
+
+
+# -------------------------------------------------------------------- norm
+
+
+def norm_inputs(B, n, seed):
+    rng = np.random.default_rng((seed, B, n))
+
+    def c():
+        return (rng.standard_normal((B, n)) + 1j * rng.standard_normal((B, n))).astype(np.complex64)
+    x = c() * np.exp(rng.standard_normal((1, n))).astype(np.float32) + np.float32(0.7)
+    return x.astype(np.complex64), c(), (1 + 0.1 * rng.standard_normal(2 * n)).astype(np.float32), rng.standard_normal(2 * n).astype(np.float32)
+
+
+def pairs(v, n):
+    return np.asarray(v, np.float64).reshape(2, n).T
+
+
+def norm_check(h, z, stats, x, delta, gain, bias, center, eps=1e-5):
+    n = x.shape[1]
+    want_h, want, s = tr.layernorm(x, delta, gain, bias, eps, center)
+    np.testing.assert_array_equal(host(h), want_h)
+    got = host(stats).astype(np.float64)
+    np.testing.assert_allclose(got[:, 0], s[:, 0], rtol=u, atol=2.0 ** -48 * np.abs(want_h).max())
+    np.testing.assert_allclose(got[:, 1], s[:, 1], rtol=4 * u)
+    b = np.abs(pairs(bias, n)) if bias is not None else 0.0
+    t = np.abs(want - (pairs(bias, n) if bias is not None else 0.0))
+    tol = 8 * u * (t + b)
+    if hasattr(z, "codes"):
+        codes, scales = raw(z)
+        v = tr.dequantize(codes, scales, 2 * n).reshape(want.shape)
+        flat, ft = want.reshape(len(want), -1), np.broadcast_to(tol, want.shape).reshape(len(want), -1)
+        for k in range(-(-2 * n // 128)):
+            at = slice(128 * k, min(2 * n, 128 * k + 128))
+            e = scales[k // 4, :, k % 4].astype(int) - 127
+            top, slack = np.abs(flat[:, at]).max(1), ft[:, at].max(1)
+            assert (top - slack <= 448 * 2.0 ** e).all() and ((top + slack > 224 * 2.0 ** e) | (e == -117)).all()
+        unit = 2.0 ** (scales.transpose(1, 0, 2).reshape(len(want), -1).astype(np.float64) - 127)
+        unit = np.repeat(unit, 128, 1)[:, :2 * n].reshape(want.shape)
+        tol = tol + np.maximum(2.0 ** -4 * (np.abs(want) + tol), 2.0 ** -10 * unit)
+        assert (codes[:, 2 * n:] == 0).all()
+    else:
+        v = host(z).astype(np.float64)
+        tol = tol + 2.0 ** -8 * (np.abs(want) + tol)
+    assert (np.abs(v - want) <= tol).all(), (np.abs(v - want) / np.maximum(tol, 1e-300)).max()
+
+
+NORM_SIZES = [(1, 1), (2, 3), (3, 4), (1, 63), (4, 64), (2, 65), (3, 256), (5, 257), (2, 1001), (9, 1024), (77, 1500), (3, 2048), (2, 2052),
+              (2, 4096), (2, 4099), (3, 8192), (2, 8193), (1, 20001), (300, 40)]
+
+
+@pytest.mark.parametrize("B, n", NORM_SIZES)
+@pytest.mark.parametrize("fp8", [False, True])
+def test_norm(gpu, B, n, fp8):
+    import paper_2512_02901_amd as f2
+    x, delta, gain, bias = norm_inputs(B, n, 20)
+    for with_delta, with_bias, center in ((True, True, True), (False, False, False), (True, False, True)):
+        h, z, s = f2.add_layernorm(dev(x, gpu), dev(gain, gpu), bias=dev(bias, gpu) if with_bias else None,
+                                   delta=dev(delta, gpu) if with_delta else None, center=center, fp8=fp8)
+        norm_check(h, z, s, x, delta if with_delta else None, gain, bias if with_bias else None, center)
+
+
+@pytest.mark.parametrize("n", [257, 1500, 9001])
+@pytest.mark.parametrize("where", ["x", "delta", "offset", "kept"])
+def test_norm_in_place_and_at_odd_addresses(gpu, n, where):
+    import torch
+    import paper_2512_02901_amd as f2
+    x, delta, gain, bias = norm_inputs(3, n, 21)
+    xd, dd = dev(x, gpu), dev(delta, gpu)
+    buf = torch.zeros(2 * n + 1, device=gpu)
+    buf[1:] = dev(gain, gpu)
+    z0 = None
+    if where == "offset":  # 8 bytes past a 16-byte boundary, the output 2 bytes past one
+        b = torch.empty(3 * n + 1, dtype=torch.complex64, device=gpu)
+        b[1:] = xd.reshape(-1)
+        xd = b[1:].view(3, n)
+        z0 = torch.full((6 * n + 9,), 5.0, dtype=torch.bfloat16, device=gpu)
+    h_out = {"x": xd, "delta": dd, "offset": None, "kept": torch.empty_like(xd)}[where]
+    h, z, s = f2.add_layernorm(xd, buf[1:], bias=dev(bias, gpu), delta=dd, h_out=h_out,
+                               out=None if z0 is None else z0[1:6 * n + 1].view(3, n, 2))
+    assert h_out is None or h is h_out
+    norm_check(h, z, s, x, delta, gain, bias, True)
+    if z0 is not None:
+        assert host(z0)[0] == 5 and (host(z0)[6 * n + 1:] == 5).all()
+
+
+def test_norm_extremes(gpu):
+    import paper_2512_02901_amd as f2
+    for n in (128, 129, 8200):
+        x, _, gain, bias = norm_inputs(8, n, 22)
+        x[0] = 0
+        x[1] *= np.float32(1e30)             # the squares overflow float32
+        x[2] *= np.float32(1e-30)            # eps decides
+        x[3] = np.complex64(5 + 5j)          # no spread at all
+        x[4] = x[4] * np.float32(1e-3) + np.complex64(1e4 + 1e4j)  # a mean far above the spread
+        x[5, 1] = np.nan
+        x[6, n - 1] = np.inf
+        ok = [0, 1, 2, 3, 4, 7]
+        for fp8 in (False, True):
+            for center in (True, False):
+                h, z, s = f2.add_layernorm(dev(x, gpu), dev(gain, gpu), bias=dev(bias, gpu), center=center, fp8=fp8)
+                v = host(z.dequantize()) if fp8 else host(z).reshape(8, -1)
+                assert np.isnan(v[5]).all()
+                assert np.isnan(v[6]).any() and np.isnan(host(s)[5, 1])
+                h, z, s = f2.add_layernorm(dev(x[ok], gpu), dev(gain, gpu), bias=dev(bias, gpu), center=center, fp8=fp8)
+                norm_check(h, z, s, x[ok], None, gain, bias, center)
+
+
+# ---------------------------------------------------------------- backward
+
+
+def backward_check(got, dz, h, stats, gain, dh, center):
+    B, n = h.shape
+    dx, dgain, dbias = tr.layernorm_backward(dz, h, stats, gain, dh, center)
+    mu, r = (np.asarray(stats, np.float64)[:, i, None, None] for i in (0, 1))
+    y = np.abs((np.stack([h.real, h.imag], -1).astype(np.float64) - mu) * r)
+    w = np.abs(dz.astype(np.float64) * pairs(gain, n))
+    m1 = w.mean((1, 2), keepdims=True) if center else 0.0
+    m2 = (w * y).mean((1, 2), keepdims=True)
+    d = np.abs(np.stack([dh.real, dh.imag], -1)).astype(np.float64) if dh is not None else 0.0
+    tol = u * (2 * d + np.abs(r) * (8 * w + 100 * m1 + 100 * y * m2))
+    e = host(got[0]).astype(np.complex128) - dx
+    err = np.abs(np.stack([e.real, e.imag], -1))
+    assert (err <= tol + 1e-45).all(), (err / np.maximum(tol, 1e-300)).max()
+    steps = B / 256 + 8 + 8
+    ga = (np.abs(dz) * y).sum(0).T.reshape(-1)
+    assert (np.abs(host(got[1]) - dgain) <= (steps + 4) * u * ga + 1e-45).all()
+    if got[2] is not None:
+        ba = np.abs(dz).astype(np.float64).sum(0).T.reshape(-1)
+        assert (np.abs(host(got[2]) - dbias) <= steps * u * ba + 1e-45).all()
+
+
+def grad_inputs(B, n, seed, center, bf16):
+    import torch
+    rng = np.random.default_rng((seed, B, n))
+    x, dh, gain, _ = norm_inputs(B, n, seed)
+    _, _, stats = tr.layernorm(x, None, gain, None, 1e-5, center)
+    dz = torch.from_numpy(rng.standard_normal((B, n, 2)).astype(np.float32))
+    dz = dz.bfloat16() if bf16 else dz
+    return x, stats.astype(np.float32), gain, dh, dz
+
+
+@pytest.mark.parametrize("B, n", NORM_SIZES + [(5, 512), (70, 300), (1029, 130), (21, 5000), (40, 8200)])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_backward(gpu, B, n, bf16):
+    import torch
+    import paper_2512_02901_amd as f2
+    for center, bias, with_dh in ((True, True, True), (False, False, False), (True, False, True), (False, True, True)):
+        x, stats, gain, dh, dz = grad_inputs(B, n, 30, center, bf16)
+        dzd = dz.to(gpu) if bf16 else torch.view_as_complex(dz.to(gpu))
+        args = (dzd, dev(x, gpu), dev(stats, gpu), dev(gain, gpu))
+        got = f2.layernorm_backward(*args, dh=dev(dh, gpu) if with_dh else None, center=center, bias=bias)
+        assert (got[2] is not None) == bias
+        backward_check(got, host(dz), x, stats, gain, dh if with_dh else None, center)
+        again = f2.layernorm_backward(*args, dh=dev(dh, gpu) if with_dh else None, center=center, bias=bias)
+        assert all(p is None or torch.equal(p, q) for p, q in zip(got, again))
+
+
+@pytest.mark.parametrize("n", [33, 1500, 9001])
+@pytest.mark.parametrize("where", ["dh", "h", "offset"])
+def test_backward_in_place_and_at_odd_addresses(gpu, n, where):
+    import torch
+    import paper_2512_02901_amd as f2
+    B = 11
+    x, stats, gain, dh, dz = grad_inputs(B, n, 31, True, True)
+    h, d = dev(x, gpu), dev(dh, gpu)
+    zd = dz.to(gpu)
+    out = {"dh": d, "h": h, "offset": None}[where]
+    if where == "offset":
+        b = torch.full((B * n + 2,), 3 + 4j, dtype=torch.complex64, device=gpu)
+        out = b[1:-1].view(B, n)
+        zb = torch.empty(2 * B * n + 1, dtype=torch.bfloat16, device=gpu)
+        zb[1:] = zd.reshape(-1)
+        zd = zb[1:].view(B, n, 2)
+    got = f2.layernorm_backward(zd, h, dev(stats, gpu), dev(gain, gpu), dh=d, out=out)
+    assert got[0] is out
+    backward_check(got, host(dz), x, stats, gain, dh, True)
+    if where == "offset":
+        assert host(b)[0] == 3 + 4j and host(b)[-1] == 3 + 4j
+
+
+def test_backward_against_differences_of_the_forward_pass(gpu):
+    """The kernels' own forward pass, in the direction of a random change: the loss <z, dz> moves by <dx, change>."""
+    import torch
+    import paper_2512_02901_amd as f2
+    B, n = 6, 700
+    x, stats, gain, _, dz = grad_inputs(B, n, 32, True, False)
+    xd, gd, dzd = dev(x, gpu), dev(gain, gpu), dz.to(gpu).double()
+    _, _, s = f2.add_layernorm(xd, gd)
+    dx, dgain, _ = f2.layernorm_backward(torch.view_as_complex(dz.to(gpu)), xd, s, gd)
+    rng = np.random.default_rng(33)
+    change = (rng.standard_normal((B, n)) + 1j * rng.standard_normal((B, n))).astype(np.complex64)
+    step = 2.0 ** -4
+    out = []
+    for sign in (1, -1):
+        _, z, _ = f2.add_layernorm((xd + sign * step * dev(change, gpu)), gd)
+        out.append((z.double() * dzd).sum().item())
+    got = (out[0] - out[1]) / (2 * step)
+    want = (torch.view_as_real(dx).double() * torch.view_as_real(dev(change, gpu)).double()).sum().item()
+    # z is rounded to bf16: independent errors of at most 2^-8 |z| each side; the third derivative's part step^2
+    noise = 6 * 2.0 ** -8 * np.sqrt(2.0 / 3) * np.linalg.norm(host(z).astype(np.float64) * host(dz)) / (2 * step)
+    size = np.linalg.norm(host(dz)) * np.linalg.norm(change) * float(s[:, 1].max())
+    assert abs(got - want) <= noise + step ** 2 * size * float(s[:, 1].max()) ** 2
+
+
+# ------------------------------------------------- together, graphs, streams
+
+
+def layer_inputs(gpu, M, K, N, seed):
+    rng = np.random.default_rng((seed, M, K, N))
+    x, _, gain, _ = norm_inputs(M, K, seed)
+    R = dev((0.05 * rng.standard_normal((2 * N, 2 * K))).astype(np.float32), gpu).bfloat16()
+    gy = dev(rng.standard_normal((M, N, 2)).astype(np.float32), gpu).bfloat16()
+    return dev(x, gpu), dev(gain, gpu), R, gy
+
+
+def layer_step(f2, x, gain, R, gy):
+    """Norm, product, and everything backward: (y, dx, dgain, G_U, G_W)."""
+    import torch
+    h, z, stats = f2.add_layernorm(x, gain, center=False, fp8=True)
+    R8, RT8 = f2.quantize_fp8(R, transposed="both")
+    y = f2.gemm_fp8(z, R8, dtype=torch.float32)
+    g8, gt8 = f2.quantize_fp8(gy, transposed="both")
+    dz = f2.gemm_fp8(g8, RT8).view(x.shape[0], x.shape[1], 2)
+    G_R = f2.gemm_fp8(gt8, z.transpose(), dtype=torch.float32)
+    dx, dgain, _ = f2.layernorm_backward(dz, h, stats, gain, center=False, bias=False)
+    G_U, G_W = f2.wl_unrealify_grad(G_R, R.shape[0] // 2, x.shape[1])
+    return y, dx, dgain, G_U, G_W
+
+
+@pytest.mark.parametrize("M, K, N", [(1, 64, 64), (77, 150, 90), (260, 320, 200)])
+def test_a_layers_training_step(gpu, M, K, N):
+    """Against the step in 64 bits without any 8-bit form: a code is off by at most 2^-4 of its value, evenly spread
+    (2^-4 / sqrt(3) in the mean square for the worst mantissa, less than 0.7 of that over all), two in a product:
+    relative L2 below 2^-4."""
+    import paper_2512_02901_amd as f2
+    x, gain, R, gy = layer_inputs(gpu, M, K, N, 40)
+    got = layer_step(f2, x, gain, R, gy)
+    h, z, stats = tr.layernorm(host(x), None, host(gain), None, 1e-5, False)
+    zr, Rr, g = z.reshape(M, 2 * K), host(R).astype(np.float64), host(gy).astype(np.float64).reshape(M, 2 * N)
+    dx, dgain, _ = tr.layernorm_backward((g @ Rr).reshape(M, K, 2), h, stats, host(gain), None, False)
+    G = g.T @ zr
+    GU = G[0::2, 0::2] + G[1::2, 1::2] + 1j * (G[1::2, 0::2] - G[0::2, 1::2])
+    GW = G[0::2, 0::2] - G[1::2, 1::2] + 1j * (G[0::2, 1::2] + G[1::2, 0::2])
+    for a, b in zip(got, (zr @ Rr.T, dx, dgain, GU, GW)):
+        assert np.linalg.norm(host(a) - b) <= 2.0 ** -4 * np.linalg.norm(b)
+
+
+def test_captured_and_replayed(gpu):
+    import torch
+    import paper_2512_02901_amd as f2
+    sets = [layer_inputs(gpu, 300, 320, 200, 50 + i) for i in range(3)]
+    want = [layer_step(f2, *s) for s in sets]
+    static = [t.clone() for t in sets[0]]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        layer_step(f2, *static)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = layer_step(f2, *static)
+    with torch.cuda.graph(other):
+        out2 = layer_step(f2, *static)
+    for i in (1, 2, 0, 1):
+        for t, v in zip(static, sets[i]):
+            t.copy_(v)
+        graph.replay()
+        layer_step(f2, *sets[(i + 1) % 3])  # the program's own work between
+        torch.cuda.synchronize()
+        for a, b in zip(out, want[i]):
+            assert torch.equal(a, b)
+        other.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out2, want[i]):
+            assert torch.equal(a, b)
+
+
+def test_on_another_stream_and_two_at_once(gpu):
+    import torch
+    import paper_2512_02901_amd as f2
+    sets = [layer_inputs(gpu, 520, 640, 300, 60 + i) for i in range(2)]
+    want = [layer_step(f2, *s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for s, st in zip(sets, streams):
+        with torch.cuda.stream(st):
+            got.append(layer_step(f2, *s))
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        for a, b in zip(g, w):
+            assert torch.equal(a, b)
+
+
+def test_refusals(gpu):
+    import torch
+    import paper_2512_02901_amd as f2
+    c = lambda *s: torch.zeros(s, dtype=torch.complex64, device=gpu)  # noqa: E731
+    r = lambda *s: torch.zeros(s, device=gpu)  # noqa: E731
+    m = f2.quantize_fp8(r(4, 130))
+    bad = [
+        (ValueError, lambda: f2.Fp8Matrix(0, 4)),
+        (ValueError, lambda: f2.Fp8Matrix(4, 130, m.codes[:, :128])),
+        (ValueError, lambda: f2.Fp8Matrix(4, 130, m.codes, m.scales[:, :2])),
+        (TypeError, lambda: f2.Fp8Matrix(4, 130, m.codes.view(torch.uint8), m.scales)),
+        (ValueError, lambda: f2.Fp8Matrix(4, 130, m.codes.cpu(), m.scales)),
+        (TypeError, lambda: f2.quantize_fp8(r(4, 130).half())),
+        (TypeError, lambda: f2.quantize_fp8([1.0])),
+        (ValueError, lambda: f2.quantize_fp8(r(4, 130).cpu())),
+        (ValueError, lambda: f2.quantize_fp8(r(4, 130).t())),
+        (ValueError, lambda: f2.quantize_fp8(r(4, 130)[:, ::2])),
+        (ValueError, lambda: f2.quantize_fp8(r(1, 130).expand(4, 130))),
+        (ValueError, lambda: f2.quantize_fp8(r(4, 5, 3))),
+        (ValueError, lambda: f2.quantize_fp8(c(4, 5).conj())),
+        (ValueError, lambda: f2.quantize_fp8(r(4, 130), transposed="rows")),
+        (ValueError, lambda: f2.quantize_fp8(r(4, 130), out=f2.Fp8Matrix(4, 131))),
+        (ValueError, lambda: f2.quantize_fp8(r(4, 130), transposed=True, out=m)),
+        (TypeError, lambda: f2.quantize_fp8(r(4, 130), out=r(4, 130))),
+        (f2.Fairy2iError, lambda: f2.quantize_fp8(r(4, 130), out=f2.Fp8Matrix(
+            4, 130, torch.zeros(4 * 256 + 8, dtype=torch.uint8, device=gpu)[8:].view(4, 256).view(torch.float8_e4m3fn)))),
+        (ValueError, lambda: f2.quantize_fp8(r(0, 130))),
+        (ValueError, lambda: m.transpose(out=f2.Fp8Matrix(4, 130))),
+        (ValueError, lambda: m.dequantize(out=torch.zeros(4, 131, dtype=torch.bfloat16, device=gpu))),
+        (TypeError, lambda: m.dequantize(out=r(4, 130))),
+        (TypeError, lambda: f2.gemm_fp8(m, r(4, 130))),
+        (ValueError, lambda: f2.gemm_fp8(m, f2.quantize_fp8(r(4, 129)))),
+        (ValueError, lambda: f2.gemm_fp8(m, m, accumulate=True)),
+        (TypeError, lambda: f2.gemm_fp8(m, m, dtype=torch.float16)),
+        (ValueError, lambda: f2.gemm_fp8(m, m, out=r(4, 5))),
+        (ValueError, lambda: f2.gemm_fp8(m, m, out=r(4, 4).t())),
+        (TypeError, lambda: f2.gemm_fp8(m, m, out=r(4, 4), dtype=torch.bfloat16)),
+        (TypeError, lambda: f2.gemm_fp8(m, m, workspace=r(4))),
+        (TypeError, lambda: f2.add_layernorm(r(4, 8), r(16))),
+        (ValueError, lambda: f2.add_layernorm(c(4, 8), r(8))),
+        (ValueError, lambda: f2.add_layernorm(c(4, 8), r(16), bias=r(8))),
+        (ValueError, lambda: f2.add_layernorm(c(4, 8), r(16), delta=c(4, 9))),
+        (ValueError, lambda: f2.add_layernorm(c(4, 8).conj(), r(16))),
+        (ValueError, lambda: f2.add_layernorm(c(8, 4).t(), r(16))),
+        (f2.Fairy2iError, lambda: f2.add_layernorm(c(4, 8), r(16), eps=0.0)),
+        (f2.Fairy2iError, lambda: f2.add_layernorm(c(0, 8), r(16))),
+        (ValueError, lambda: f2.add_layernorm(c(4, 8), r(16), fp8=True, out=m)),
+        (ValueError, lambda: f2.add_layernorm(c(4, 8), r(16), h_out=c(4, 9))),
+        (TypeError, lambda: f2.layernorm_backward(r(4, 8, 2), c(4, 8), r(4, 2), r(16))),
+        (ValueError, lambda: f2.layernorm_backward(c(4, 9), c(4, 8), r(4, 2), r(16))),
+        (ValueError, lambda: f2.layernorm_backward(c(4, 8), c(4, 8), r(2, 4), r(16))),
+        (ValueError, lambda: f2.layernorm_backward(c(4, 8), c(4, 8), r(4, 2), r(8))),
+        (ValueError, lambda: f2.layernorm_backward(c(4, 8), c(4, 8), r(4, 2), r(16), dh=c(4, 9))),
+        (ValueError, lambda: f2.layernorm_backward(c(4, 8).conj(), c(4, 8), r(4, 2), r(16))),
+        (f2.Fairy2iError, lambda: f2.layernorm_backward(c(900, 8), c(900, 8), r(900, 2), r(16),
+                                                        workspace=torch.zeros(4, dtype=torch.uint8, device=gpu))),
+    ]
+    for i, (error, call) in enumerate(bad):
+        with pytest.raises(error):
+            call()
+            print("not refused:", i)

@@ -12,6 +12,7 @@
 // arrange, so neither side of LDS meets a bank conflict.  Scales come four
 // steps at a time, a dword a row.
 #include <algorithm>
+#include <utility>
 
 #include "fp8.h"
 
@@ -23,6 +24,64 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr_t;
+
+__device__ inline __amdgpu_buffer_rsrc_t rsrc(const void* base, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), (short)0, (int)bytes, 0x00020000);
+}
+
+template <int V>
+struct Constant {
+  static constexpr int value = V;
+};
+
+// f(Constant<0>) .. f(Constant<N - 1>): what stands between two products is placed at compile time.
+template <int... I, typename F>
+__device__ __attribute__((always_inline)) inline void each_of(std::integer_sequence<int, I...>, F&& f) {
+  (f(Constant<I>{}), ...);
+}
+template <int N, typename F>
+__device__ __attribute__((always_inline)) inline void each(F&& f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
+}
+// Slot T's share of N things that are spread over IN slots.
+template <int N, int IN, int T, typename F>
+__device__ __attribute__((always_inline)) inline void some(F&& f) {
+  if constexpr (T < IN)
+    each<(T + 1) * N / IN - T * N / IN>(
+        [&](auto i) __attribute__((always_inline)) { f(Constant<T * N / IN + decltype(i)::value>{}); });
+}
+
+// c += 16 x 128 codes of a times those of b, scaled by byte U of sa and sb.  The
+// sums are asked for in accumulation registers and the operands in vector ones:
+// left to itself the compiler moves both to and fro where a wave has 256 sums.
+// It does not see the hazards of an instruction written so: an operand that it
+// has just written needs two wait states (the s_nop), a sum read by anything but a
+// product needs settle() first.
+template <int U>
+__device__ __attribute__((always_inline)) inline void product(v4f& c, const v8i& a, const v8i& b, uint32_t sa, uint32_t sb) {
+  if constexpr (U == 0)
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]"
+                 : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+  else if constexpr (U == 1)
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[0,0,0]"
+                 : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+  else if constexpr (U == 2)
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[1,1,0]"
+                 : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+  else
+    asm volatile("s_nop 1\n\tv_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel:[1,1,0] op_sel_hi:[1,1,0]"
+                 : "+a"(c) : "v"(a), "v"(b), "v"(sa), "v"(sb));
+}
+
+// Past the last product's eight passes: its sums may be read.
+template <int TM, int TN>
+__device__ __attribute__((always_inline)) inline void settle(v4f (&acc)[TM][TN]) {
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) asm volatile("" : "+a"(acc[i][j]));
+}
 
 struct Gemm {
   const uint8_t* a;
@@ -97,10 +156,13 @@ template <int BM, int BN, int WM, int WN, int BLOCKS>
 __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) {
 #if defined(__HIP_DEVICE_COMPILE__)  // LDS-DMA and buffer-descriptor code: device pass only
   constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-  constexpr int PIECES = (BM + BN) / 8 / WAVES;  // 1 KB loads of a wave and step
-  constexpr int SCALE_LOADS = (BM + BN) / 64;    // of 64 rows
-  __shared__ __attribute__((aligned(16))) uint8_t codes[2][(BM + BN) * 128];
-  __shared__ uint32_t scales[2][BM + BN];
+  constexpr int PA = BM / 8 / WAVES, PB = BN / 8 / WAVES;  // 1 KB loads of a wave and step
+  constexpr int SCALE_LOADS = (BM + BN) / 64;              // of 64 rows
+  constexpr int SLOTS = TM * TN, HALF = SLOTS / 2;
+  // two arrays and not one of two: loads into one never order reads of the other
+  __shared__ __attribute__((aligned(16))) uint8_t codes0[(BM + BN) * 128];
+  __shared__ __attribute__((aligned(16))) uint8_t codes1[(BM + BN) * 128];
+  __shared__ uint32_t scales[2 * (BM + BN)];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wm = wave % WM, wn = wave / WM;
@@ -110,35 +172,33 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   const int split = (int)blockIdx.y;
   const int k0 = split * g.steps_per_split, k1 = min(k0 + g.steps_per_split, g.steps);
 
-  // This wave's pieces of a step: eight rows each, of A's tile first, then of B's.
-  // Rows past the matrix's end read its last row.
-  const uint8_t* piece_at[PIECES];
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int p = wave * PIECES + i;
-    const bool of_a = p < BM / 8;
-    const int64_t r = (of_a ? m0 + 8 * p : n0 + 8 * (p - BM / 8)) + (lane >> 3);
-    const int64_t row = min(r, (of_a ? g.M : g.N) - 1);
-    piece_at[i] = (of_a ? g.a : g.b) + row * g.ld + 16 * ((lane & 7) ^ (lane >> 3));
-  }
-  auto issue = [&](int k, int buf) {
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(piece_at[i] + (int64_t)k * 128),
-          (lds_ptr_t)&codes[buf][(wave * PIECES + i) * 1024], 16, 0, 0);
+  // A tile's rows as a buffer: rows past the matrix's end are past the buffer's
+  // and read as zeros, steps past the last one find an empty buffer.
+  const uint32_t ld = (uint32_t)g.ld;
+  const uint8_t *base_a = g.a + m0 * g.ld, *base_b = g.b + n0 * g.ld;
+  const uint32_t bytes_a = (uint32_t)min((int64_t)BM, g.M - m0) * ld;
+  const uint32_t bytes_b = (uint32_t)min((int64_t)BN, g.N - n0) * ld;
+  const uint32_t at = (uint32_t)(8 * wave + (lane >> 3)) * ld + 16u * (uint32_t)((lane & 7) ^ (lane >> 3));
+  auto issue = [&](int k, int i, uint8_t* codes) {  // load i (A's, then B's) of step k
+    const bool of_a = i < PA;
+    const int p = of_a ? i : i - PA;
+    const __amdgpu_buffer_rsrc_t r = rsrc(of_a ? base_a : base_b, k < k1 ? (of_a ? bytes_a : bytes_b) : 0u);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)&codes[((of_a ? 0 : BM / 8) + p * WAVES + wave) * 1024], 16,
+                                             at + (uint32_t)(p * WAVES * 8) * ld, (uint32_t)k * 128u, 0, 0);
   };
-  auto issue_scales = [&](int k4, int buf) {
+  // Scales of four steps, a dword a row: 64 rows a load.
+  auto issue_scales = [&](int k4) {
 #pragma unroll
     for (int i = 0; i < (SCALE_LOADS + WAVES - 1) / WAVES; ++i) {
       const int p = wave + i * WAVES;
-      if (p >= SCALE_LOADS) break;
       const bool of_a = p < BM / 64;
-      const int64_t rows = of_a ? g.M : g.N;
-      const int64_t row = min((of_a ? m0 + 64 * p : n0 + 64 * (p - BM / 64)) + lane, rows - 1);
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)((of_a ? g.a_scales : g.b_scales) + (k4 * rows + row) * 4),
-          (lds_ptr_t)&scales[buf][p * 64], 4, 0, 0);
+      const int64_t rows = of_a ? g.M : g.N, first = of_a ? m0 : n0;
+      const bool there = p < SCALE_LOADS && 4 * k4 < k1;
+      const __amdgpu_buffer_rsrc_t r = rsrc((of_a ? g.a_scales : g.b_scales) + (k4 * rows + first) * 4,
+                                            there ? (uint32_t)min(rows - first, (int64_t)256) * 4u : 0u);
+      if (SCALE_LOADS % WAVES == 0 || p < SCALE_LOADS)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)&scales[(k4 & 1) * (BM + BN) + p * 64], 4,
+                                                 4u * (uint32_t)(64 * (of_a ? p : p - BM / 64) + lane), 0, 0, 0);
     }
   };
 
@@ -147,59 +207,111 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-  uint32_t sa[TM], sb[TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i) sa[i] = 0;
-#pragma unroll
-  for (int j = 0; j < TN; ++j) sb[j] = 0;
 
   const int r16 = lane & 15, q = lane >> 4;
   // chunks q and q + 4 of a row are this lane's 32 codes (of both operands alike)
-  const int lo = 16 * (q ^ (r16 & 7)), hi = 16 * ((q + 4) ^ (r16 & 7));
-  auto load = [&](int buf, int row) {
-    const uint8_t* p = &codes[buf][(row + r16) * 128];
-    const v4i x = *reinterpret_cast<const v4i*>(p + lo), y = *reinterpret_cast<const v4i*>(p + hi);
-    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+  const int lo = r16 * 128 + 16 * (q ^ (r16 & 7)), hi = r16 * 128 + 16 * ((q + 4) ^ (r16 & 7));
+  const int row_a = wm * TM * 16, row_b = BM + wn * TN * 16;
+  auto half = [&](const uint8_t* codes, int row, int h) {
+    return *reinterpret_cast<const v4i*>(&codes[row * 128 + (h ? hi : lo)]);
   };
-  auto compute = [&](int k, int buf) {
-    if ((k & 3) == 0) {
-      const int sbuf = (k >> 2) & 1;
+  auto whole = [](const v4i& x, const v4i& y) { return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7); };
+
+  uint32_t sa[TM], sb[TN], sa_next[TM], sb_next[TN];
+  auto read_scale = [&](int k4, int i) {
+    const uint32_t* f = &scales[(k4 & 1) * (BM + BN)];
+    if (i < TM)
+      sa_next[i] = f[row_a + 16 * i + r16];
+    else
+      sb_next[i - TM] = f[row_b + 16 * (i - TM) + r16];
+  };
+  // Step k, whose first fragments (A's first, B's all) are in registers and whose
+  // codes are in `mine`.  First half, rows of tiles 0 .. TM / 2 - 1: reads of the
+  // rest of its A fragments.  Then `mine` is free and step k + 1 is in `other`: one
+  // barrier.  Second half, the other rows' tiles column by column: step k + 2's
+  // loads into `mine`, and as a column's B fragment has served, step k + 1's in its
+  // place.  A product keeps the matrix core busy for 32 cycles, an instruction or
+  // two stand between two of them.
+  v4i fb[TN][2], first[2];
+  auto step = [&](int k, auto which, uint8_t* mine, uint8_t* other) __attribute__((always_inline)) {
+    constexpr int U = decltype(which)::value;
+    v4i fa[TM][2];
+    fa[0][0] = first[0];
+    fa[0][1] = first[1];
+    each<SLOTS>([&](auto slot) __attribute__((always_inline)) {
+      constexpr int s = decltype(slot)::value, t = s - HALF, R = TM / 2;
+      constexpr int i = s < HALF ? s / TN : R + t % R, j = s < HALF ? s % TN : t / R;
+      product<U>(acc[i][j], whole(fb[j][0], fb[j][1]), whole(fa[i][0], fa[i][1]), sb[j], sa[i]);
+      if constexpr (s < HALF) {
+        constexpr int READS = 2 * (TM - 1), IN = HALF > 8 ? HALF - 4 : HALF > 2 ? HALF - 2 : 1;
+        some<READS, IN, s>([&](auto r) __attribute__((always_inline)) {
+          constexpr int n = 1 + decltype(r)::value / 2, h = decltype(r)::value % 2;
+          fa[n][h] = half(mine, row_a + 16 * n, h);
+        });
+      } else {
+        constexpr int IN = HALF - 1;
+        some<PA + PB, IN, t>([&](auto r) __attribute__((always_inline)) { issue(k + 2, decltype(r)::value, mine); });
+        if constexpr (t < 2) first[t] = half(other, row_a, t);
+        if constexpr (t % R == R - 1) {
+          fb[j][0] = half(other, row_b + 16 * j, 0);
+          fb[j][1] = half(other, row_b + 16 * j, 1);
+        }
+        if constexpr (U == 3)
+          some<TM + TN, IN, t>([&](auto r) __attribute__((always_inline)) { read_scale((k >> 2) + 1, decltype(r)::value); });
+        if constexpr (U == 0 && s == SLOTS - 1) issue_scales((k >> 2) + 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (s == HALF - 1) {
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    });
+    if (U == 3) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) sa[i] = scales[sbuf][wm * TM * 16 + 16 * i + r16];
+      for (int i = 0; i < TM; ++i) sa[i] = sa_next[i];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) sb[j] = scales[sbuf][BM + wn * TN * 16 + 16 * j + r16];
+      for (int j = 0; j < TN; ++j) sb[j] = sb_next[j];
     }
-    v8i fb[TN];
-#pragma unroll
-    for (int j = 0; j < TN; ++j) fb[j] = load(buf, BM + wn * TN * 16 + 16 * j);
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const v8i fa = load(buf, wm * TM * 16 + 16 * i);
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa, acc[i][j], 0, 0, 0, (int)sb[j], 0,
-                                                                     (int)sa[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) sa[i] >>= 8;
-#pragma unroll
-    for (int j = 0; j < TN; ++j) sb[j] >>= 8;
   };
 
-  // One barrier a step: after it every wave has its share of step k in LDS and
-  // has done with step k - 1, whose buffer step k + 1 then fills.  k0 is a
-  // multiple of 4.
-  issue_scales(k0 >> 2, (k0 >> 2) & 1);
-  issue(k0, 0);
-  for (int k = k0; k < k1; ++k) {
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    if (k + 1 < k1) {
-      issue(k + 1, (k + 1) & 1);
-      if (((k + 1) & 3) == 0) issue_scales((k + 1) >> 2, ((k + 1) >> 2) & 1);
-    }
-    compute(k, k & 1);
+  // k0 is a multiple of 4
+  issue_scales(k0 >> 2);
+#pragma unroll
+  for (int i = 0; i < PA + PB; ++i) issue(k0, i, codes0);
+#pragma unroll
+  for (int i = 0; i < PA + PB; ++i) issue(k0 + 1, i, codes1);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    first[h] = half(codes0, row_a, h);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[j][h] = half(codes0, row_b + 16 * j, h);
   }
+#pragma unroll
+  for (int i = 0; i < TM + TN; ++i) read_scale(k0 >> 2, i);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) sa[i] = sa_next[i];
+#pragma unroll
+  for (int j = 0; j < TN; ++j) sb[j] = sb_next[j];
+
+  int k = k0;
+  for (; k + 4 <= k1; k += 4) {
+    step(k, Constant<0>{}, codes0, codes1);
+    step(k + 1, Constant<1>{}, codes1, codes0);
+    step(k + 2, Constant<2>{}, codes0, codes1);
+    step(k + 3, Constant<3>{}, codes1, codes0);
+  }
+  if (k < k1) step(k, Constant<0>{}, codes0, codes1);
+  if (k + 1 < k1) step(k + 1, Constant<1>{}, codes1, codes0);
+  if (k + 2 < k1) step(k + 2, Constant<2>{}, codes0, codes1);
+  __builtin_amdgcn_s_waitcnt(0);  // loads into this block's LDS end before it does
+  settle(acc);
 
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
@@ -316,7 +428,7 @@ fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_m
   hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)tiles, (unsigned)p.splits);
   if (p.tile == 0)
-    hipLaunchKernelGGL((gemm_fp8_kernel<256, 256, 2, 4, 1>), grid, dim3(512), 0, s, g);
+    hipLaunchKernelGGL((gemm_fp8_kernel<256, 256, 2, 2, 1>), grid, dim3(256), 0, s, g);
   else if (p.tile == 1)
     hipLaunchKernelGGL((gemm_fp8_kernel<128, 128, 2, 2, 2>), grid, dim3(256), 0, s, g);
   else

@@ -101,6 +101,7 @@ struct Gemm {
 // Row of C from column n on, four values (fewer at the end of a row).
 __device__ inline void store4(const Gemm& g, int64_t m, int64_t n, v4f v, int split) {
   const int count = (int)min((int64_t)4, g.N - n);
+  if (count <= 0) return;
   if (g.parts) {
     float* p = g.parts + ((int64_t)split * g.M + m) * g.N + n;
     if (count == 4)
@@ -152,7 +153,7 @@ __device__ inline void tile_of(const Gemm& g, int id, int& tm, int& tn) {
   tn = in / rows;
 }
 
-template <int BM, int BN, int WM, int WN, int BLOCKS>
+template <int BM, int BN, int WM, int WN, int BLOCKS, int AHEAD>
 __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) {
 #if defined(__HIP_DEVICE_COMPILE__)  // LDS-DMA and buffer-descriptor code: device pass only
   constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
@@ -163,6 +164,7 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   __shared__ __attribute__((aligned(16))) uint8_t codes0[(BM + BN) * 128];
   __shared__ __attribute__((aligned(16))) uint8_t codes1[(BM + BN) * 128];
   __shared__ uint32_t scales[2 * (BM + BN)];
+  __shared__ uint32_t asked[AHEAD ? 64 : 1];  // never read
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wm = wave % WM, wn = wave / WM;
@@ -185,6 +187,19 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
     const __amdgpu_buffer_rsrc_t r = rsrc(of_a ? base_a : base_b, k < k1 ? (of_a ? bytes_a : bytes_b) : 0u);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)&codes[((of_a ? 0 : BM / 8) + p * WAVES + wave) * 1024], 16,
                                              at + (uint32_t)(p * WAVES * 8) * ld, (uint32_t)k * 128u, 0, 0);
+  };
+  // One line of each row a few steps on, into the L2: the tiles that run beside this
+  // one on its XCD (four in a row of tiles, eight in a column) share the rows out.
+  const uint32_t ask_a =
+      lane < BM / 4 / WAVES ? (uint32_t)(BM / 4 * (tn & 3) + BM / 4 / WAVES * wave + lane) * ld : 0xFFFFFFF0u;
+  const uint32_t ask_b =
+      lane < BN / 8 / WAVES ? (uint32_t)(BN / 8 * (tm & 7) + BN / 8 / WAVES * wave + lane) * ld : 0xFFFFFFF0u;
+  auto ask = [&](int k) {
+    const bool there = k < k1;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(base_a, there ? bytes_a : 0u), (lds_ptr_t)&asked[0], 4, ask_a,
+                                             (uint32_t)k * 128u, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(base_b, there ? bytes_b : 0u), (lds_ptr_t)&asked[0], 4, ask_b,
+                                             (uint32_t)k * 128u, 0, 0);
   };
   // Scales of four steps, a dword a row: 64 rows a load.
   auto issue_scales = [&](int k4) {
@@ -258,12 +273,13 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
         }
         if constexpr (U == 3)
           some<TM + TN, IN, t>([&](auto r) __attribute__((always_inline)) { read_scale((k >> 2) + 1, decltype(r)::value); });
-        if constexpr (U == 0 && s == SLOTS - 1) issue_scales((k >> 2) + 1);
+        if constexpr (U == 0 && s == SLOTS - 2) issue_scales((k >> 2) + 1);
+        if constexpr (AHEAD && s == SLOTS - 1) ask(k + AHEAD);
       }
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (s == HALF - 1) {
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(0);
+        __builtin_amdgcn_s_waitcnt(AHEAD ? 0x72 : 0x70);  // all LDS reads and all loads but ask()'s two
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
@@ -283,8 +299,13 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   for (int i = 0; i < PA + PB; ++i) issue(k0, i, codes0);
 #pragma unroll
   for (int i = 0; i < PA + PB; ++i) issue(k0 + 1, i, codes1);
+  if constexpr (AHEAD > 0) {
+#pragma unroll
+    for (int k = 2; k < AHEAD; ++k) ask(k0 + k);
+  }
+  constexpr int LATER = PA + PB + (AHEAD > 0 ? 2 * (AHEAD - 2) : 0);  // than step k0's
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0);
+  __builtin_amdgcn_s_waitcnt(0x70 | (LATER & 15) | (LATER >> 4 << 14));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
@@ -313,16 +334,51 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   __builtin_amdgcn_s_waitcnt(0);  // loads into this block's LDS end before it does
   settle(acc);
 
+  // A lane holds four neighbours of a row in each tile.  Whole tiles in bf16 go out
+  // two at a time, lanes 16 apart exchanging halves: 16 bytes a lane, 64 of a row
+  // at a time, half the stores.
+  const int64_t nw = n0 + wn * TN * 16;
+  if (m0 + BM <= g.M && n0 + BN <= g.N && !g.parts && g.bf16 && !g.accumulate) {
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t m = m0 + wm * TM * 16 + 16 * i + r16;
-    if (m >= g.M) continue;
+    for (int i = 0; i < TM; ++i) {
+      uint16_t* p = static_cast<uint16_t*>(g.c) + (m0 + row_a + 16 * i + r16) * g.ldc + nw + (q & 1 ? 16 + 4 * (q - 1) : 4 * q);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int64_t n = n0 + wn * TN * 16 + 16 * j + 4 * q;
-      if (n < g.N) store4(g, m, n, acc[i][j], split);
+      for (int j = 0; j < TN; j += 2) {
+        uint32_t w[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const v4f& c = acc[i][j + h];
+          w[h][0] = bf16_pair(c[0], c[1]);
+          w[h][1] = bf16_pair(c[2], c[3]);
+        }
+        const auto x = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false);
+        const auto y = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
+        *reinterpret_cast<u32x4_any*>(p + 16 * j) = u32x4_any{x[0], y[0], x[1], y[1]};
+      }
     }
+    return;
   }
+  // Everything else goes through LDS, 16 rows of the wave's tiles at a time.
+  constexpr int LD = TN * 16 + 4, PER_ROW = TN * 2;  // floats of a row there, groups of eight
+  __syncthreads();                                   // the other waves' fragments were here
+  float* rows = reinterpret_cast<float*>(codes0) + wave * 16 * LD;
+  each<TM>([&](auto tile) __attribute__((always_inline)) {
+    constexpr int i = decltype(tile)::value;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) *reinterpret_cast<v4f*>(&rows[r16 * LD + 16 * j + 4 * q]) = acc[i][j];
+    wave_sync();
+#pragma unroll 1
+    for (int e = lane; e < 16 * PER_ROW; e += 64) {
+      const int64_t m = m0 + row_a + 16 * i + e / PER_ROW;
+      const int n = e % PER_ROW * 8;
+      const float* v = &rows[e / PER_ROW * LD + n];
+      if (m < g.M) {
+        store4(g, m, nw + n, *reinterpret_cast<const v4f*>(v), split);
+        store4(g, m, nw + n + 4, *reinterpret_cast<const v4f*>(v + 4), split);
+      }
+    }
+    wave_sync();
+  });
 #endif
 }
 
@@ -428,11 +484,11 @@ fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_m
   hipStream_t s = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)tiles, (unsigned)p.splits);
   if (p.tile == 0)
-    hipLaunchKernelGGL((gemm_fp8_kernel<256, 256, 2, 2, 1>), grid, dim3(256), 0, s, g);
+    hipLaunchKernelGGL((gemm_fp8_kernel<256, 256, 2, 2, 1, 4>), grid, dim3(256), 0, s, g);
   else if (p.tile == 1)
-    hipLaunchKernelGGL((gemm_fp8_kernel<128, 128, 2, 2, 2>), grid, dim3(256), 0, s, g);
+    hipLaunchKernelGGL((gemm_fp8_kernel<128, 128, 2, 2, 2, 0>), grid, dim3(256), 0, s, g);
   else
-    hipLaunchKernelGGL((gemm_fp8_kernel<64, 64, 2, 2, 2>), grid, dim3(256), 0, s, g);
+    hipLaunchKernelGGL((gemm_fp8_kernel<64, 64, 2, 2, 2, 0>), grid, dim3(256), 0, s, g);
   if (p.splits > 1) {
     const int64_t groups = M * ((N + 3) / 4);
     const unsigned blocks = (unsigned)std::min<int64_t>((groups + 255) / 256, 4096);

@@ -933,7 +933,7 @@ fairy2i_status fairy2i_fp8_dequantize(const fairy2i_fp8_matrix* in, void* out, v
  * 4-byte aligned, contents ignored; calls that share one must not overlap.
  * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for sizes out of range or that
  * disagree, ldc < N; FAIRY2I_ERR_DTYPE; FAIRY2I_ERR_UNSUPPORTED for misaligned
- * operands or 2^22 or more tiles of C; FAIRY2I_ERR_WORKSPACE.
+ * operands or 2^24 or more tiles of C; FAIRY2I_ERR_WORKSPACE.
  */
 size_t fairy2i_gemm_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_matrix* B, void* C, int32_t dtype,

@@ -170,15 +170,17 @@ def _check(status: int, where: str):
 
 _torch_module = None
 _raw_stream = None  # device index -> handle of torch's current stream there
+_current_device = None  # -> index of torch's current device
 
 
 def _torch():
-    global _torch_module, _raw_stream
+    global _torch_module, _raw_stream, _current_device
     if _torch_module is None:
         import torch
         # the handle alone (0.07 us); torch.cuda.current_stream builds a Stream object for it (1.9 us)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         _torch_module = torch  # last: another thread that sees the module calls _raw_stream
     return _torch_module
 
@@ -1211,13 +1213,13 @@ class PagedKv:
 def _call(name, index, *args):
     """A library call on the current stream of device `index`, which is made the current one for it."""
     fn = getattr(_lib, name)
-    torch = _torch_module
-    if torch.cuda.current_device() == index:
+    if _current_device() == index:
         status = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(index):
+        with _torch_module.cuda.device(index):
             status = fn(*args, _raw_stream(index))
-    _check(status, name)
+    if status != OK:
+        raise Fairy2iError(status, name)
 
 
 class Fp8Matrix:
@@ -1236,6 +1238,11 @@ class Fp8Matrix:
         if not (1 <= rows <= 1 << 22 and 1 <= cols <= 1 << 22):
             raise ValueError("rows and cols must be in [1, 2^22]")
         shape, scale_shape = (rows, -(-cols // 128) * 128), (-(-cols // 512), rows, 4)
+        self.rows, self.cols = rows, cols
+        if codes is None and scales is None:
+            codes = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
+            self._set(codes, torch.empty(scale_shape, dtype=torch.uint8, device=codes.device))
+            return
         if codes is None:
             codes = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device if scales is None else scales.device)
         if scales is None:
@@ -1244,18 +1251,23 @@ class Fp8Matrix:
         _require(scales, torch.uint8, "scales", codes.device)
         if codes.shape != shape or scales.shape != scale_shape:
             raise ValueError(f"codes must be {shape} and scales {scale_shape}")
-        self.rows, self.cols, self.codes, self.scales = rows, cols, codes, scales
+        self._set(codes, scales)
+
+    def _set(self, codes, scales):
+        self.codes, self.scales, self.device = codes, scales, codes.device
         self._index = codes.get_device()
-        self._desc = Fp8Desc(codes.data_ptr(), scales.data_ptr(), rows, cols)
+        if self._index < 0:
+            raise ValueError("a Fp8Matrix lives on a GPU")
+        self._desc = Fp8Desc(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols)
         self._ref = ctypes.byref(self._desc)
 
     def dequantize(self, out=None):
         """What the matrix stands for: bf16 [rows, cols], exact (out: such a tensor to write)."""
         torch = _torch_module
         if out is None:
-            out = torch.empty((self.rows, self.cols), dtype=torch.bfloat16, device=self.codes.device)
+            out = torch.empty((self.rows, self.cols), dtype=torch.bfloat16, device=self.device)
         else:
-            _require(out, torch.bfloat16, "out", self.codes.device)
+            _require(out, torch.bfloat16, "out", self.device)
             if out.shape != (self.rows, self.cols):
                 raise ValueError(f"out must have shape {(self.rows, self.cols)}")
         _call("fairy2i_fp8_dequantize", self._index, self._ref, out.data_ptr())
@@ -1264,7 +1276,7 @@ class Fp8Matrix:
     def transpose(self, out=None):
         """The transposed matrix, scales along the other axis (fairy2i_fp8_transpose;
         out: a Fp8Matrix to write)."""
-        out = _fp8_out(out, self.cols, self.rows, self.codes.device, "out")
+        out = _fp8_out(out, self.cols, self.rows, self.device, "out")
         if out.codes.data_ptr() == self.codes.data_ptr() or out.scales.data_ptr() == self.scales.data_ptr():
             raise ValueError("out must be other memory than the matrix itself")
         _call("fairy2i_fp8_transpose", self._index, self._ref, out._ref)
@@ -1276,8 +1288,8 @@ def _fp8_out(out, rows, cols, device, name):
         return Fp8Matrix(rows, cols, device=device)
     if not isinstance(out, Fp8Matrix):
         raise TypeError(f"{name} must be a Fp8Matrix")
-    if out.codes.device != device:
-        raise ValueError(f"{name} is on {out.codes.device}, expected {device}")
+    if out.device != device:
+        raise ValueError(f"{name} is on {out.device}, expected {device}")
     if (out.rows, out.cols) != (rows, cols):
         raise ValueError(f"{name} must be {rows} x {cols}, got {out.rows} x {out.cols}")
     return out
@@ -1364,18 +1376,18 @@ def gemm_fp8(A, B, out=None, dtype=None, accumulate=False, workspace=None):
         raise ValueError(f"A has {A.cols} columns, B {B.cols}")
     index = A._index
     if B._index != index:
-        raise ValueError(f"B is on {B.codes.device}, expected {A.codes.device}")
+        raise ValueError(f"B is on {B.device}, expected {A.device}")
     M, N = A.rows, B.rows
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty((M, N), dtype=torch.bfloat16 if dtype is None else dtype, device=A.codes.device)
+        out = torch.empty((M, N), dtype=torch.bfloat16 if dtype is None else dtype, device=A.device)
         ldc = N
     else:
         if not isinstance(out, torch.Tensor):
             raise TypeError("out must be a torch.Tensor")
         if out.get_device() != index:
-            raise ValueError(f"out is on {out.device}, expected {A.codes.device}")
+            raise ValueError(f"out is on {out.device}, expected {A.device}")
         if dtype is not None and out.dtype is not dtype:
             raise TypeError(f"out must be {dtype}, got {out.dtype}")
         if out.shape != (M, N) or (N > 1 and out.stride(1) != 1):
@@ -1468,17 +1480,52 @@ def layernorm_backward(dz, h, stats, gain, dh=None, center=True, bias=True, out=
     bias=False."""
     torch = _torch_module or _torch()
     lib = _lib or load()
+    # launch latency counts: everything is looked over in one expression, _check_backward names what is wrong
+    try:
+        index = h.get_device()
+        B, n = h.shape
+        c64, f32 = torch.complex64, torch.float32
+        dt = ACT_BF16 if dz.dtype is torch.bfloat16 else ACT_F32
+        ok = (index >= 0 and h.dtype is c64 and h.is_contiguous() and not h.is_conj()
+              and dz.get_device() == index and dz.is_contiguous()
+              and (dz.shape == (B, n, 2) if dt == ACT_BF16 else
+                   dz.dtype is c64 and dz.shape == (B, n) and not dz.is_conj())
+              and stats.dtype is f32 and stats.get_device() == index and stats.is_contiguous() and stats.shape == (B, 2)
+              and gain.dtype is f32 and gain.get_device() == index and gain.is_contiguous() and gain.shape == (2 * n,))
+        for t in (dh, out):
+            ok = ok and (t is None or (t.dtype is c64 and t.get_device() == index and t.is_contiguous()
+                                       and not t.is_conj() and t.shape == h.shape))
+    except (AttributeError, TypeError, ValueError):
+        ok = False
+    if not ok:
+        _check_backward(dz, h, stats, gain, dh, out)
+    dev = h.device
+    dx = torch.empty_like(h) if out is None else out
+    sums = torch.empty(4 * n if bias else 2 * n, dtype=torch.float32, device=dev)
+    dgain, dbias = sums[:2 * n], sums[2 * n:] if bias else None
+    if workspace is None:
+        need = lib.fairy2i_layernorm_backward_workspace_bytes(B, n)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    else:  # its size is the library's to check
+        _require(workspace, torch.uint8, "workspace", dev)
+    _call("fairy2i_layernorm_backward", index, dz.data_ptr(), dt, h.data_ptr(), stats.data_ptr(), gain.data_ptr(),
+          None if dh is None else dh.data_ptr(), int(bool(center)), B, n, dx.data_ptr(), dgain.data_ptr(),
+          dbias.data_ptr() if bias else None, None if workspace is None else workspace.data_ptr(),
+          0 if workspace is None else workspace.numel())
+    return dx, dgain, dbias
+
+
+def _check_backward(dz, h, stats, gain, dh, out):
+    torch = _torch()
     _require(h, torch.complex64, "h")
     if h.dim() != 2:
         raise ValueError("h must be [B, n]")
-    (B, n), dev, index = h.shape, h.device, h.get_device()
+    (B, n), dev = h.shape, h.device
     _require(dz, None, "dz", dev)
-    if dz.dtype is torch.bfloat16:
-        dt, shape = ACT_BF16, (B, n, 2)
-    elif dz.dtype is torch.complex64:
-        dt, shape = ACT_F32, (B, n)
-    else:
+    if dz.dtype not in (torch.bfloat16, torch.complex64):
         raise TypeError(f"dz must be bfloat16 or complex64, got {dz.dtype}")
+    shape = (B, n, 2) if dz.dtype is torch.bfloat16 else (B, n)
     if dz.shape != shape:
         raise ValueError(f"dz must have shape {shape}, got {tuple(dz.shape)}")
     _require(stats, torch.float32, "stats", dev)
@@ -1495,17 +1542,3 @@ def layernorm_backward(dz, h, stats, gain, dh=None, center=True, bias=True, out=
     for t, name in ((dz, "dz"), (h, "h"), (dh, "dh"), (out, "out")):
         if t is not None and t.is_conj():
             raise ValueError(f"{name} is a conjugated view: resolve_conj() it first")
-    dx = torch.empty_like(h) if out is None else out
-    sums = torch.empty(4 * n if bias else 2 * n, dtype=torch.float32, device=dev)
-    dgain, dbias = sums[:2 * n], sums[2 * n:] if bias else None
-    if workspace is None:
-        need = lib.fairy2i_layernorm_backward_workspace_bytes(B, n)
-        if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    else:  # its size is the library's to check
-        _require(workspace, torch.uint8, "workspace", dev)
-    _call("fairy2i_layernorm_backward", index, dz.data_ptr(), dt, h.data_ptr(), stats.data_ptr(), gain.data_ptr(),
-          None if dh is None else dh.data_ptr(), int(bool(center)), B, n, dx.data_ptr(), dgain.data_ptr(),
-          dbias.data_ptr() if bias else None, None if workspace is None else workspace.data_ptr(),
-          0 if workspace is None else workspace.numel())
-    return dx, dgain, dbias

@@ -83,6 +83,9 @@ __device__ __attribute__((always_inline)) inline void settle(v4f (&acc)[TM][TN])
     for (int j = 0; j < TN; ++j) asm volatile("" : "+a"(acc[i][j]));
 }
 
+// Operand of s_waitcnt: no LDS operation under way, `loads` loads at most.
+constexpr int wait_loads(int loads) { return 0x70 | (loads & 15) | loads >> 4 << 14; }
+
 struct Gemm {
   const uint8_t* a;
   const uint8_t* a_scales;
@@ -153,21 +156,33 @@ __device__ inline void tile_of(const Gemm& g, int id, int& tm, int& tn) {
   tn = in / rows;
 }
 
-template <int BM, int BN, int WM, int WN, int BLOCKS, int AHEAD>
+// BM x BN of C by WM x WN waves, BLOCKS blocks a CU; STAGES steps in LDS (2 or 4);
+// AHEAD: how many steps ahead lines are asked for (0: not).
+template <int BM, int BN, int WM, int WN, int STAGES, int BLOCKS, int AHEAD>
 __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) {
 #if defined(__HIP_DEVICE_COMPILE__)  // LDS-DMA and buffer-descriptor code: device pass only
   constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr int PA = BM / 8 / WAVES, PB = BN / 8 / WAVES;  // 1 KB loads of a wave and step
   constexpr int SCALE_LOADS = (BM + BN) / 64;              // of 64 rows
   constexpr int SLOTS = TM * TN, HALF = SLOTS / 2;
-  // two arrays and not one of two: loads into one never order reads of the other
-  __shared__ __attribute__((aligned(16))) uint8_t codes0[(BM + BN) * 128];
-  __shared__ __attribute__((aligned(16))) uint8_t codes1[(BM + BN) * 128];
+  constexpr int STAGE = (BM + BN) * 128;
+  // several arrays and not one of several: loads into one never order reads of another
+  __shared__ __attribute__((aligned(16))) uint8_t codes0[STAGE];
+  __shared__ __attribute__((aligned(16))) uint8_t codes1[STAGE];
+  __shared__ __attribute__((aligned(16))) uint8_t codes2[STAGES > 2 ? STAGE : 16];
+  __shared__ __attribute__((aligned(16))) uint8_t codes3[STAGES > 2 ? STAGE : 16];
   __shared__ uint32_t scales[2 * (BM + BN)];
   __shared__ uint32_t asked[AHEAD ? 64 : 1];  // never read
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int wm = wave % WM, wn = wave / WM;
+  auto buffer = [&](auto k) __attribute__((always_inline)) {  // of step k
+    constexpr int b = decltype(k)::value % STAGES;
+    if constexpr (b == 0) return &codes0[0];
+    else if constexpr (b == 1) return &codes1[0];
+    else if constexpr (b == 2) return &codes2[0];
+    else return &codes3[0];
+  };
   int tm, tn;
   tile_of(g, (int)blockIdx.x, tm, tn);
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
@@ -248,8 +263,9 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   // place.  A product keeps the matrix core busy for 32 cycles, an instruction or
   // two stand between two of them.
   v4i fb[TN][2], first[2];
-  auto step = [&](int k, auto which, uint8_t* mine, uint8_t* other) __attribute__((always_inline)) {
+  auto step = [&](int k, auto which) __attribute__((always_inline)) {
     constexpr int U = decltype(which)::value;
+    uint8_t *mine = buffer(which), *other = buffer(Constant<U + 1>{});
     v4i fa[TM][2];
     fa[0][0] = first[0];
     fa[0][1] = first[1];
@@ -265,7 +281,7 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
         });
       } else {
         constexpr int IN = HALF - 1;
-        some<PA + PB, IN, t>([&](auto r) __attribute__((always_inline)) { issue(k + 2, decltype(r)::value, mine); });
+        some<PA + PB, IN, t>([&](auto r) __attribute__((always_inline)) { issue(k + STAGES, decltype(r)::value, mine); });
         if constexpr (t < 2) first[t] = half(other, row_a, t);
         if constexpr (t % R == R - 1) {
           fb[j][0] = half(other, row_b + 16 * j, 0);
@@ -279,7 +295,8 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (s == HALF - 1) {
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_waitcnt(AHEAD ? 0x72 : 0x70);  // all LDS reads and all loads but ask()'s two
+        // all LDS reads; all loads but the later steps' and ask()'s last two
+        __builtin_amdgcn_s_waitcnt(wait_loads((STAGES - 2) * (PA + PB) + (AHEAD > 0 ? 2 : 0)));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
@@ -295,24 +312,21 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
 
   // k0 is a multiple of 4
   issue_scales(k0 >> 2);
+  each<STAGES>([&](auto stage) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < PA + PB; ++i) issue(k0, i, codes0);
+    for (int i = 0; i < PA + PB; ++i) issue(k0 + decltype(stage)::value, i, buffer(stage));
+  });
 #pragma unroll
-  for (int i = 0; i < PA + PB; ++i) issue(k0 + 1, i, codes1);
-  if constexpr (AHEAD > 0) {
-#pragma unroll
-    for (int k = 2; k < AHEAD; ++k) ask(k0 + k);
-  }
-  constexpr int LATER = PA + PB + (AHEAD > 0 ? 2 * (AHEAD - 2) : 0);  // than step k0's
+  for (int k = STAGES; k < AHEAD; ++k) ask(k0 + k);
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(0x70 | (LATER & 15) | (LATER >> 4 << 14));
+  __builtin_amdgcn_s_waitcnt(wait_loads((STAGES - 1) * (PA + PB) + (AHEAD > 0 ? 2 * (AHEAD - STAGES) : 0)));
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    first[h] = half(codes0, row_a, h);
+    first[h] = half(buffer(Constant<0>{}), row_a, h);
 #pragma unroll
-    for (int j = 0; j < TN; ++j) fb[j][h] = half(codes0, row_b + 16 * j, h);
+    for (int j = 0; j < TN; ++j) fb[j][h] = half(buffer(Constant<0>{}), row_b + 16 * j, h);
   }
 #pragma unroll
   for (int i = 0; i < TM + TN; ++i) read_scale(k0 >> 2, i);
@@ -323,16 +337,17 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
 
   int k = k0;
   for (; k + 4 <= k1; k += 4) {
-    step(k, Constant<0>{}, codes0, codes1);
-    step(k + 1, Constant<1>{}, codes1, codes0);
-    step(k + 2, Constant<2>{}, codes0, codes1);
-    step(k + 3, Constant<3>{}, codes1, codes0);
+    step(k, Constant<0>{});
+    step(k + 1, Constant<1>{});
+    step(k + 2, Constant<2>{});
+    step(k + 3, Constant<3>{});
   }
-  if (k < k1) step(k, Constant<0>{}, codes0, codes1);
-  if (k + 1 < k1) step(k + 1, Constant<1>{}, codes1, codes0);
-  if (k + 2 < k1) step(k + 2, Constant<2>{}, codes0, codes1);
+  if (k < k1) step(k, Constant<0>{});
+  if (k + 1 < k1) step(k + 1, Constant<1>{});
+  if (k + 2 < k1) step(k + 2, Constant<2>{});
   __builtin_amdgcn_s_waitcnt(0);  // loads into this block's LDS end before it does
   settle(acc);
+  __syncthreads();  // every wave has done with LDS
 
   // A lane holds four neighbours of a row in each tile.  Whole tiles in bf16 go out
   // two at a time, lanes 16 apart exchanging halves: 16 bytes a lane, 64 of a row
@@ -360,7 +375,7 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   }
   // Everything else goes through LDS, 16 rows of the wave's tiles at a time.
   constexpr int LD = TN * 16 + 4, PER_ROW = TN * 2;  // floats of a row there, groups of eight
-  __syncthreads();                                   // the other waves' fragments were here
+  static_assert(WAVES * 16 * LD * 4 <= STAGE, "");
   float* rows = reinterpret_cast<float*>(codes0) + wave * 16 * LD;
   each<TM>([&](auto tile) __attribute__((always_inline)) {
     constexpr int i = decltype(tile)::value;
@@ -406,27 +421,73 @@ __global__ __launch_bounds__(256) void gemm_fp8_join_kernel(Gemm g, int splits) 
   }
 }
 
-// Tile sizes, and how many splits of K: see plan_of.
+// A block's time is a fixed part (launch apart: the first loads, the stores) and a
+// part a step.  `room` blocks run at once; with two a CU each has half of it, so
+// up to 256 blocks a step takes `alone`.
+struct Variant {
+  int bm, bn, room;
+  float alone, step, fixed;  // us
+  void (*kernel)(Gemm);
+};
+
+// us measured with one bf16 C, all of the variants for each size (the least is what plan_of takes):
+//   M, N, K            256x256  256x128  128x128  128x128x2  64x128  64x64x2
+//   77, 4096, 4096        41.4     28.8     16.5       23.3    11.2      9.1
+//   512, 4096, 4096       39.7     26.6     15.7       22.1    13.1     15.0
+//   1024, 4096, 4096      40.5     27.2     18.7       23.8    23.2     26.9
+//   1400, 4096, 4096      44.6     31.5     32.4       28.9    33.8     37.8
+//   2048, 4096, 4096      41.9     31.9     34.7       32.3    44.5     50.7
+//   4096, 4096, 4096      53.6     61.2     66.7       61.8    87.6     99.0
+//   4096, 11008, 4096    146.7    183.3    203.4      191.2   263.4    277.0
+//   4096, 4096, 512       16.3     16.8     20.4       16.6    27.4     27.5
+//   1500, 1500, 1500      26.0     19.0     11.4       13.2    12.9     11.0
+// Smaller tiles read LDS more often for a product (256 x 256: 0.75 of its rate, 64 x
+// 64 three times it); more stages hide a longer way to memory where a step is short.
+const Variant kVariants[] = {
+    {256, 256, 256, 1.3f, 1.3f, 8.0f, gemm_fp8_kernel<256, 256, 2, 2, 2, 1, 4>},
+    {256, 128, 256, 0.8f, 0.8f, 4.5f, gemm_fp8_kernel<256, 128, 2, 2, 2, 1, 4>},
+    {128, 128, 256, 0.43f, 0.43f, 2.2f, gemm_fp8_kernel<128, 128, 2, 2, 4, 1, 0>},
+    {128, 128, 512, 0.55f, 0.85f, 2.5f, gemm_fp8_kernel<128, 128, 2, 2, 2, 2, 0>},
+    {64, 128, 256, 0.28f, 0.28f, 1.4f, gemm_fp8_kernel<64, 128, 2, 2, 4, 1, 0>},
+    {64, 64, 512, 0.17f, 0.34f, 0.9f, gemm_fp8_kernel<64, 64, 2, 2, 4, 2, 0>},
+};
+
 struct Plan {
-  int tile;  // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+  const Variant* v;
+  int64_t tiles_m, tiles_n;
   int splits, steps_per_split;
 };
 
-constexpr int kSide[3] = {256, 128, 64};
-
+// The variant, and how many parts K is cut into, with the least expected time: the
+// rounds of blocks, and for a split K the second launch (4 us of a call) and the parts'
+// way to memory and back (8 bytes each at 2.5 TB/s).  16 x 16 x 16384: 25.1 us in
+// one part, 10.7 in four, 8.7 in eight, 9.6 in sixteen; 300 x 300 x 16384: 26.2,
+// 13.5, 13.4, 16.9.
 Plan plan_of(int64_t M, int64_t N, int64_t K) {
-  const int steps = (int)((K + 127) / 128);
-  auto tiles = [&](int side) { return ((M + side - 1) / side) * ((N + side - 1) / side); };
-  Plan p;
-  p.tile = tiles(256) >= 192 ? 0 : tiles(128) >= 128 ? 1 : 2;
-  const int64_t t = tiles(kSide[p.tile]);
-  int64_t splits = 1;
-  if (p.tile > 0) splits = std::max<int64_t>(1, std::min<int64_t>(512 / t, steps / 8));
-  const int64_t quads = (steps + 3) / 4;
-  splits = std::min(splits, quads);
-  p.steps_per_split = (int)((quads + splits - 1) / splits * 4);
-  p.splits = (steps + p.steps_per_split - 1) / p.steps_per_split;
-  return p;
+  const int steps = (int)((K + 127) / 128), quads = (steps + 3) / 4;
+  Plan best{};
+  double least = 0;
+  for (const Variant& v : kVariants) {
+    Plan p{&v, (M + v.bm - 1) / v.bm, (N + v.bn - 1) / v.bn, 1, 0};
+    for (int want = 1; want <= 32 && want <= quads; want *= 2) {
+      p.steps_per_split = (quads + want - 1) / want * 4;
+      p.splits = (steps + p.steps_per_split - 1) / p.steps_per_split;
+      const int64_t blocks = p.tiles_m * p.tiles_n * p.splits, rounds = blocks / v.room, rest = blocks % v.room;
+      const int run = std::min(p.steps_per_split, steps);
+      double us = (double)rounds * (run * v.step + v.fixed);
+      if (rest > 0) us += run * (rest > 256 ? v.step : v.alone) + v.fixed;
+      if (p.splits > 1) us += 4.0 + (double)p.splits * (double)M * (double)N * 8e-6 / 2.5;
+      if (!best.v || us < least) {
+        best = p;
+        least = us;
+      }
+    }
+  }
+  return best;
+}
+
+size_t parts_bytes(const Plan& p, int64_t M, int64_t N) {
+  return p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)M * (size_t)N : 0;
 }
 
 bool sizes_ok(int64_t M, int64_t N, int64_t K) {
@@ -443,8 +504,7 @@ extern "C" {
 
 size_t fairy2i_gemm_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   if (!sizes_ok(M, N, K)) return 0;
-  const Plan p = plan_of(M, N, K);
-  return p.splits > 1 ? sizeof(float) * (size_t)p.splits * (size_t)M * (size_t)N : 0;
+  return parts_bytes(plan_of(M, N, K), M, N);
 }
 
 fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_matrix* B, void* C, int32_t dtype,
@@ -459,36 +519,29 @@ fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_m
   if (dtype != FAIRY2I_ACT_F32 && dtype != FAIRY2I_ACT_BF16) return FAIRY2I_ERR_DTYPE;
   const int64_t M = A->rows, N = B->rows, K = A->cols;
   const Plan p = plan_of(M, N, K);
-  const size_t need = fairy2i_gemm_fp8_workspace_bytes(M, N, K);
+  const size_t need = parts_bytes(p, M, N);
   if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 3)))
     return FAIRY2I_ERR_WORKSPACE;
-  const int side = kSide[p.tile];
-  Gemm g{A->codes,
-         A->scales,
-         B->codes,
-         B->scales,
-         M,
-         N,
-         fp8_ld(K),
-         (int)(fp8_ld(K) / 128),
-         p.steps_per_split,
-         (int)((M + side - 1) / side),
-         (int)((N + side - 1) / side),
-         C,
-         ldc,
-         dtype == FAIRY2I_ACT_BF16,
-         accumulate,
-         need > 0 ? static_cast<float*>(workspace) : nullptr};
-  const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n;
-  if (tiles >= ((int64_t)1 << 22)) return FAIRY2I_ERR_UNSUPPORTED;  // a launch takes fewer than 2^32 threads
+  const int64_t tiles = p.tiles_m * p.tiles_n;
+  if (tiles * p.splits >= ((int64_t)1 << 24)) return FAIRY2I_ERR_UNSUPPORTED;  // a launch takes fewer than 2^32 threads
+  const Gemm g{A->codes,
+               A->scales,
+               B->codes,
+               B->scales,
+               M,
+               N,
+               fp8_ld(K),
+               (int)(fp8_ld(K) / 128),
+               p.steps_per_split,
+               (int)p.tiles_m,
+               (int)p.tiles_n,
+               C,
+               ldc,
+               dtype == FAIRY2I_ACT_BF16,
+               accumulate,
+               need > 0 ? static_cast<float*>(workspace) : nullptr};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const dim3 grid((unsigned)tiles, (unsigned)p.splits);
-  if (p.tile == 0)
-    hipLaunchKernelGGL((gemm_fp8_kernel<256, 256, 2, 2, 1, 4>), grid, dim3(256), 0, s, g);
-  else if (p.tile == 1)
-    hipLaunchKernelGGL((gemm_fp8_kernel<128, 128, 2, 2, 2, 0>), grid, dim3(256), 0, s, g);
-  else
-    hipLaunchKernelGGL((gemm_fp8_kernel<64, 64, 2, 2, 2, 0>), grid, dim3(256), 0, s, g);
+  hipLaunchKernelGGL(p.v->kernel, dim3((unsigned)tiles, (unsigned)p.splits), dim3(256), 0, s, g);
   if (p.splits > 1) {
     const int64_t groups = M * ((N + 3) / 4);
     const unsigned blocks = (unsigned)std::min<int64_t>((groups + 255) / 256, 4096);

@@ -48,18 +48,25 @@ __device__ inline int fp8_scale_byte(uint32_t top) {
 
 __device__ inline float fp8_power(int byte) { return __uint_as_float((uint32_t)byte << 23); }  // 2^(byte - 127)
 
-// v / 2^e for the conversion: exact, at most 448 (only the largest scale's
-// blocks hold more: up to 512, which saturate), NaN for what is not finite.
-__device__ inline float fp8_scaled(float v, float inv) {
-  const float u = v * inv;
-  const float c = fabsf(u) > 448.0f ? copysignf(448.0f, u) : u;
-  return fabsf(v) < INFINITY ? c : __builtin_nanf("");
+// Above this lie what e = 119 cannot hold and what is not finite (as bits of an absolute value).
+constexpr uint32_t kFp8Most = 0x7F600000u;  // 448 * 2^119
+
+// A value as it is held: beyond the largest that one, a NaN for what is not
+// finite.  Only blocks with a magnitude past kFp8Most need it.
+__device__ inline float fp8_tame(float v) {
+  const uint32_t a = __float_as_uint(v) & 0x7FFFFFFFu;
+  if (a >= 0x7F800000u) return __builtin_nanf("");
+  return a > kFp8Most ? copysignf(__uint_as_float(kFp8Most), v) : v;
 }
 
-// Four reals of a block -> four codes, rounded to nearest even by the hardware.
-__device__ inline uint32_t fp8_codes4(float a, float b, float c, float d, float inv) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(fp8_scaled(a, inv), fp8_scaled(b, inv), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_scaled(c, inv), fp8_scaled(d, inv), w, true);
+// Four reals of a block of scale 2^e -> four codes, rounded to nearest even by the
+// conversion instruction, which divides by the power of two on its way.
+__device__ inline uint32_t fp8_codes4(float a, float b, float c, float d, float scale) {
+  typedef short v2s __attribute__((ext_vector_type(2)));
+  v2s w = {0, 0};
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, scale, false);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, w);
 }
 
 // Maximum over the 16 lanes of a DPP row, in all of them.

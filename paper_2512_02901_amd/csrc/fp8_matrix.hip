@@ -26,27 +26,30 @@ struct Source {
   int64_t ld;             // elements of a row
 };
 
-// Eight neighbours of row r from column c on; zeros outside.
-template <int SRC>
+// Eight neighbours of row r from column c on; zeros outside.  WHOLE: none are outside.
+template <int SRC, bool WHOLE>
 __device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_t r, int64_t c, float v[8]) {
+  if constexpr (!WHOLE) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-  if (r >= rows) return;
+    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+    if (r >= rows) return;
+  }
   if constexpr (SRC == kFp8) {  // rows are padded with zeros to whole blocks
     const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.x) + r * s.ld + c);
     const float unit = fp8_power(s.scales[fp8_scale_at(rows, r, c / kFp8Block)]);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int word = (int)(h ? w.y : w.x);
-      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(word, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(word, true);
-      v[4 * h] = lo[0] * unit;
-      v[4 * h + 1] = lo[1] * unit;
-      v[4 * h + 2] = hi[0] * unit;
-      v[4 * h + 3] = hi[1] * unit;
+      const uint32_t word = h ? w.y : w.x;
+      const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, false);
+      const auto hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(word, unit, true);
+      v[4 * h] = lo[0];
+      v[4 * h + 1] = lo[1];
+      v[4 * h + 2] = hi[0];
+      v[4 * h + 3] = hi[1];
     }
   } else if constexpr (SRC == kF32) {
     const float* p = static_cast<const float*>(s.x) + r * s.ld + c;
-    if (c + 8 <= cols) {
+    if (WHOLE || c + 8 <= cols) {
       const f32x4_any a = reinterpret_cast<const f32x4_any*>(p)[0], b = reinterpret_cast<const f32x4_any*>(p)[1];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -60,7 +63,7 @@ __device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_
     }
   } else {
     const uint16_t* p = static_cast<const uint16_t*>(s.x) + r * s.ld + c;
-    if (c + 8 <= cols) {
+    if (WHOLE || c + 8 <= cols) {
       const u32x4_any a = *reinterpret_cast<const u32x4_any*>(p);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -76,71 +79,112 @@ __device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_
 }
 
 template <int SRC, bool DIRECT, bool TURNED>
-__global__ __launch_bounds__(256) void fp8_quantize_kernel(Source src, int64_t rows, int64_t cols, int col_tiles,
-                                                           uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
-                                                           uint8_t* __restrict__ codes_t,
-                                                           uint8_t* __restrict__ scales_t) {
+__global__ __launch_bounds__(256, 3) void fp8_quantize_kernel(Source src, int64_t rows, int64_t cols, int col_tiles,
+                                                              uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                                                              uint8_t* __restrict__ codes_t,
+                                                              uint8_t* __restrict__ scales_t) {
   __shared__ __attribute__((aligned(16))) uint2 tile[TURNED ? 128 * 16 : 1];
-  __shared__ uint32_t tops[TURNED ? 4 * 128 : 1];
+  __shared__ __attribute__((aligned(16))) uint32_t tops[TURNED ? 4 * 128 : 4];
   const int t = threadIdx.x, cg = t & 15, rg = t >> 4;
   const int64_t rb = blockIdx.x / (uint32_t)col_tiles, cb = blockIdx.x % (uint32_t)col_tiles;
   const int64_t r0 = rb * 128 + 8 * rg, c0 = cb * 128 + 8 * cg;
   float v[8][8];
+  if (rb * 128 + 128 <= rows && cb * 128 + 128 <= cols) {
 #pragma unroll
-  for (int p = 0; p < 8; ++p) load8<SRC>(src, rows, cols, r0 + p, c0, v[p]);
+    for (int p = 0; p < 8; ++p) load8<SRC, true>(src, rows, cols, r0 + p, c0, v[p]);
+  } else {
+#pragma unroll
+    for (int p = 0; p < 8; ++p) load8<SRC, false>(src, rows, cols, r0 + p, c0, v[p]);
+  }
 
+  uint32_t row[8], col[8], all = 0;  // largest magnitudes of this thread's rows and columns
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    row[p] = col[p] = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) row[p] = max(row[p], __float_as_uint(v[p][j]) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) col[p] = max(col[p], __float_as_uint(v[j][p]) & 0x7FFFFFFFu);
+    all = max(all, row[p]);
+  }
+  if (__any(all > kFp8Most)) {
+#pragma unroll
+    for (int p = 0; p < 8; ++p) row[p] = col[p] = 0;
+#pragma unroll
+    for (int p = 0; p < 8; ++p)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[p][j] = fp8_tame(v[p][j]);
+        const uint32_t a = fp8_magnitude(v[p][j]);
+        row[p] = max(row[p], a);
+        col[j] = max(col[j], a);
+      }
+  }
   if constexpr (TURNED) {
-    uint32_t top[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      top[j] = 0;
-#pragma unroll
-      for (int p = 0; p < 8; ++p) top[j] = max(top[j], fp8_magnitude(v[p][j]));
-      top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 16));
-      top[j] = max(top[j], (uint32_t)__shfl_xor((int)top[j], 32));
+      col[j] = max(col[j], (uint32_t)__shfl_xor((int)col[j], 16));
+      col[j] = max(col[j], (uint32_t)__shfl_xor((int)col[j], 32));
     }
     if ((t & 63) < 16) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) tops[(t >> 6) * 128 + 8 * cg + j] = top[j];
+      uint4* to = reinterpret_cast<uint4*>(&tops[(t >> 6) * 128 + 8 * cg]);
+      to[0] = make_uint4(col[0], col[1], col[2], col[3]);
+      to[1] = make_uint4(col[4], col[5], col[6], col[7]);
     }
   }
   if constexpr (DIRECT) {
     const int64_t ld = (cols + 127) / 128 * 128;
+    uint8_t* to = codes + r0 * ld + c0;
+    uint8_t* scale_to = scales + fp8_scale_at(rows, r0, cb);
+    const int there = (int)min(rows - r0, (int64_t)8);
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
-      uint32_t top = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, fp8_magnitude(v[p][j]));
-      const int byte = fp8_scale_byte(row16_max(top));
-      const float inv = fp8_power(254 - byte);
-      const uint2 w = make_uint2(fp8_codes4(v[p][0], v[p][1], v[p][2], v[p][3], inv),
-                                 fp8_codes4(v[p][4], v[p][5], v[p][6], v[p][7], inv));
-      if (r0 + p < rows) {
-        *reinterpret_cast<uint2*>(codes + (r0 + p) * ld + c0) = w;
-        if (cg == 0) scales[fp8_scale_at(rows, r0 + p, cb)] = (uint8_t)byte;
+      const int byte = fp8_scale_byte(row16_max(row[p]));
+      const float scale = fp8_power(byte);
+      const uint2 w = make_uint2(fp8_codes4(v[p][0], v[p][1], v[p][2], v[p][3], scale),
+                                 fp8_codes4(v[p][4], v[p][5], v[p][6], v[p][7], scale));
+      if (p < there) {
+        *reinterpret_cast<uint2*>(to) = w;
+        if (cg == 0) scale_to[4 * p] = (uint8_t)byte;
       }
+      to += ld;
     }
   }
   if constexpr (TURNED) {
     __syncthreads();
     const int64_t ld = (rows + 127) / 128 * 128;
+    uint8_t* scale_to = scales_t + fp8_scale_at(cols, c0, rb);
+    const int there = (int)min(max(cols - c0, (int64_t)0), (int64_t)8);
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint4 o = *reinterpret_cast<const uint4*>(&tops[w * 128 + 8 * cg + 4 * h]);
+        col[4 * h] = max(col[4 * h], o.x);
+        col[4 * h + 1] = max(col[4 * h + 1], o.y);
+        col[4 * h + 2] = max(col[4 * h + 2], o.z);
+        col[4 * h + 3] = max(col[4 * h + 3], o.w);
+      }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int c = 8 * cg + j;
-      const int byte = fp8_scale_byte(max(max(tops[c], tops[128 + c]), max(tops[256 + c], tops[384 + c])));
-      const float inv = fp8_power(254 - byte);
-      tile[c * 16 + (rg ^ cg)] = make_uint2(fp8_codes4(v[0][j], v[1][j], v[2][j], v[3][j], inv),
-                                            fp8_codes4(v[4][j], v[5][j], v[6][j], v[7][j], inv));
-      if (rg == j && cb * 128 + c < cols) scales_t[fp8_scale_at(cols, cb * 128 + c, rb)] = (uint8_t)byte;
+      const int byte = fp8_scale_byte(col[j]);
+      const float scale = fp8_power(byte);
+      tile[(8 * cg + j) * 16 + (rg ^ cg)] = make_uint2(fp8_codes4(v[0][j], v[1][j], v[2][j], v[3][j], scale),
+                                                       fp8_codes4(v[4][j], v[5][j], v[6][j], v[7][j], scale));
+      if (rg == j && j < there) scale_to[4 * j] = (uint8_t)byte;
     }
     __syncthreads();
+    // a row of turned codes is eight lanes' 16 bytes: two of the 8-byte slots
+    const int c = t >> 3, pair = t & 7;
+    const int64_t left = cols - cb * 128 - c;
+    uint8_t* to = codes_t + (cb * 128 + c) * ld + rb * 128 + 16 * pair;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int c = 32 * i + (t >> 3), pair = t & 7, swap = (c >> 3) & 1;
-      const uint4 w = *reinterpret_cast<const uint4*>(&tile[c * 16 + 2 * (pair ^ (c >> 4))]);
-      if (cb * 128 + c < cols)
-        *reinterpret_cast<uint4*>(codes_t + (cb * 128 + c) * ld + rb * 128 + 16 * pair) =
-            swap ? make_uint4(w.z, w.w, w.x, w.y) : w;
+      const int at = c + 32 * i;
+      const uint4 w = *reinterpret_cast<const uint4*>(&tile[at * 16 + 2 * (pair ^ (at >> 4))]);
+      const bool swap = (at >> 3) & 1;
+      if (32 * i < left) *reinterpret_cast<uint4*>(to) = swap ? make_uint4(w.z, w.w, w.x, w.y) : w;
+      to += 32 * ld;
     }
   }
 }
@@ -173,7 +217,7 @@ __global__ __launch_bounds__(256) void fp8_dequantize_kernel(Source src, int64_t
     const int64_t r = i / groups, c = i % groups * 8;
     if (c >= cols) continue;
     float v[8];
-    load8<kFp8>(src, rows, cols, r, c, v);
+    load8<kFp8, true>(src, rows, cols, r, c, v);
     uint16_t* p = out + r * cols + c;
     if (c + 8 <= cols) {
       *reinterpret_cast<u32x4_any*>(p) =

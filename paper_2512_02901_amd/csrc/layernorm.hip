@@ -159,13 +159,21 @@ __device__ inline void write_z(const Forward& a, int64_t row, int64_t g, int cou
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     if (j >= 2 * count) z.v[j] = 0.0f;
-    top = max(top, fp8_magnitude(z.v[j]));
+    top = max(top, __float_as_uint(z.v[j]) & 0x7FFFFFFFu);
+  }
+  if (top > kFp8Most) {
+    top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      z.v[j] = fp8_tame(z.v[j]);
+      top = max(top, fp8_magnitude(z.v[j]));
+    }
   }
   const int byte = fp8_scale_byte(row16_max(top));
-  const float inv = fp8_power(254 - byte);
+  const float scale = fp8_power(byte);
   const int64_t ld = (2 * a.n + 127) / 128 * 128, r = a.row0 + row;
   *reinterpret_cast<uint2*>(a.codes + r * ld + 8 * g) =
-      make_uint2(fp8_codes4(z.v[0], z.v[1], z.v[2], z.v[3], inv), fp8_codes4(z.v[4], z.v[5], z.v[6], z.v[7], inv));
+      make_uint2(fp8_codes4(z.v[0], z.v[1], z.v[2], z.v[3], scale), fp8_codes4(z.v[4], z.v[5], z.v[6], z.v[7], scale));
   if ((g & 15) == 0) a.scales[fp8_scale_at(a.rows, r, g >> 4)] = (uint8_t)byte;
 }
 

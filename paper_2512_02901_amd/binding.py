@@ -1237,29 +1237,45 @@ class Fp8Matrix:
             load()
         if not (1 <= rows <= 1 << 22 and 1 <= cols <= 1 << 22):
             raise ValueError("rows and cols must be in [1, 2^22]")
-        shape, scale_shape = (rows, -(-cols // 128) * 128), (-(-cols // 512), rows, 4)
         self.rows, self.cols = rows, cols
-        if codes is None and scales is None:
-            codes = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
-            self._set(codes, torch.empty(scale_shape, dtype=torch.uint8, device=codes.device))
+        ld, groups = -(-cols // 128) * 128, -(-cols // 512)
+        if codes is None and scales is None:  # one piece of memory, seen as codes and scales when they are asked for
+            self._data = torch.empty(rows * (ld + 4 * groups), dtype=torch.uint8, device=device)
+            self._codes = self._scales = None
+            at = self._data.data_ptr()
+            self._set(self._data, at, at + rows * ld)
             return
         if codes is None:
-            codes = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device if scales is None else scales.device)
+            codes = torch.empty((rows, ld), dtype=torch.float8_e4m3fn, device=scales.device)
         if scales is None:
-            scales = torch.empty(scale_shape, dtype=torch.uint8, device=codes.device)
+            scales = torch.empty((groups, rows, 4), dtype=torch.uint8, device=codes.device)
         _require(codes, torch.float8_e4m3fn, "codes")
         _require(scales, torch.uint8, "scales", codes.device)
-        if codes.shape != shape or scales.shape != scale_shape:
-            raise ValueError(f"codes must be {shape} and scales {scale_shape}")
-        self._set(codes, scales)
+        if codes.shape != (rows, ld) or scales.shape != (groups, rows, 4):
+            raise ValueError(f"codes must be {(rows, ld)} and scales {(groups, rows, 4)}")
+        self._codes, self._scales = codes, scales
+        self._set(codes, codes.data_ptr(), scales.data_ptr())
 
-    def _set(self, codes, scales):
-        self.codes, self.scales, self.device = codes, scales, codes.device
-        self._index = codes.get_device()
+    def _set(self, data, codes, scales):
+        self.device, self._index = data.device, data.get_device()
         if self._index < 0:
             raise ValueError("a Fp8Matrix lives on a GPU")
-        self._desc = Fp8Desc(codes.data_ptr(), scales.data_ptr(), self.rows, self.cols)
+        self._desc = Fp8Desc(codes, scales, self.rows, self.cols)
         self._ref = ctypes.byref(self._desc)
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            n = self.rows * (-(-self.cols // 128) * 128)
+            self._codes = self._data[:n].view(_torch_module.float8_e4m3fn).view(self.rows, -1)
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            n = self.rows * (-(-self.cols // 128) * 128)
+            self._scales = self._data[n:].view(-1, self.rows, 4)
+        return self._scales
 
     def dequantize(self, out=None):
         """What the matrix stands for: bf16 [rows, cols], exact (out: such a tensor to write)."""
@@ -1277,7 +1293,7 @@ class Fp8Matrix:
         """The transposed matrix, scales along the other axis (fairy2i_fp8_transpose;
         out: a Fp8Matrix to write)."""
         out = _fp8_out(out, self.cols, self.rows, self.device, "out")
-        if out.codes.data_ptr() == self.codes.data_ptr() or out.scales.data_ptr() == self.scales.data_ptr():
+        if out._desc.codes == self._desc.codes or out._desc.scales == self._desc.scales:
             raise ValueError("out must be other memory than the matrix itself")
         _call("fairy2i_fp8_transpose", self._index, self._ref, out._ref)
         return out

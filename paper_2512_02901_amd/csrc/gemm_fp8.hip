@@ -144,13 +144,13 @@ __device__ inline void store4(const Gemm& g, int64_t m, int64_t n, v4f v, int sp
 }
 
 // Which tile of C a block takes: the blocks that one XCD runs at a time
-// (every eighth of the grid) take neighbouring tiles, eight rows of tiles deep,
+// (every eighth of the grid) take neighbouring tiles, four rows of tiles deep,
 // so they meet each other's operands in their L2.
 __device__ inline void tile_of(const Gemm& g, int id, int& tm, int& tn) {
   const int total = g.tiles_m * g.tiles_n;
   const int per = total / 8, left = total % 8, xcd = id % 8;
   const int t = xcd * per + min(xcd, left) + id / 8;
-  const int deep = 8, band = t / (deep * g.tiles_n), in = t % (deep * g.tiles_n);
+  const int deep = 4, band = t / (deep * g.tiles_n), in = t % (deep * g.tiles_n);
   const int rows = min(deep, g.tiles_m - band * deep);
   tm = band * deep + in % rows;
   tn = in / rows;
@@ -204,11 +204,11 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
                                              at + (uint32_t)(p * WAVES * 8) * ld, (uint32_t)k * 128u, 0, 0);
   };
   // One line of each row a few steps on, into the L2: the tiles that run beside this
-  // one on its XCD (four in a row of tiles, eight in a column) share the rows out.
+  // one on its XCD (eight in a row of tiles, four in a column) share the rows out.
   const uint32_t ask_a =
-      lane < BM / 4 / WAVES ? (uint32_t)(BM / 4 * (tn & 3) + BM / 4 / WAVES * wave + lane) * ld : 0xFFFFFFF0u;
+      lane < BM / 8 / WAVES ? (uint32_t)(BM / 8 * (tn & 7) + BM / 8 / WAVES * wave + lane) * ld : 0xFFFFFFF0u;
   const uint32_t ask_b =
-      lane < BN / 8 / WAVES ? (uint32_t)(BN / 8 * (tm & 7) + BN / 8 / WAVES * wave + lane) * ld : 0xFFFFFFF0u;
+      lane < BN / 4 / WAVES ? (uint32_t)(BN / 4 * (tm & 3) + BN / 4 / WAVES * wave + lane) * ld : 0xFFFFFFF0u;
   auto ask = [&](int k) {
     const bool there = k < k1;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(base_a, there ? bytes_a : 0u), (lds_ptr_t)&asked[0], 4, ask_a,
@@ -444,8 +444,8 @@ struct Variant {
 // Smaller tiles read LDS more often for a product (256 x 256: 0.75 of its rate, 64 x
 // 64 three times it); more stages hide a longer way to memory where a step is short.
 const Variant kVariants[] = {
-    {256, 256, 256, 1.3f, 1.3f, 8.0f, gemm_fp8_kernel<256, 256, 2, 2, 2, 1, 4>},
-    {256, 128, 256, 0.8f, 0.8f, 4.5f, gemm_fp8_kernel<256, 128, 2, 2, 2, 1, 4>},
+    {256, 256, 256, 1.3f, 1.3f, 8.0f, gemm_fp8_kernel<256, 256, 2, 2, 2, 1, 3>},
+    {256, 128, 256, 0.8f, 0.8f, 4.5f, gemm_fp8_kernel<256, 128, 2, 2, 2, 1, 3>},
     {128, 128, 256, 0.43f, 0.43f, 2.2f, gemm_fp8_kernel<128, 128, 2, 2, 4, 1, 0>},
     {128, 128, 512, 0.55f, 0.85f, 2.5f, gemm_fp8_kernel<128, 128, 2, 2, 2, 2, 0>},
     {64, 128, 256, 0.28f, 0.28f, 1.4f, gemm_fp8_kernel<64, 128, 2, 2, 4, 1, 0>},

@@ -531,23 +531,23 @@ __global__ __launch_bounds__(256) void layernorm_backward_long_kernel(Backward a
   }
 }
 
-// Sums of the blocks' parts: 64 columns a block, 16 threads a column.
+// Sums of the blocks' parts: 32 columns a block, 32 threads a column.
 __global__ __launch_bounds__(1024) void layernorm_join_kernel(const float* __restrict__ parts, int64_t blocks,
                                                               int64_t width, int64_t n2, float* __restrict__ dgain,
                                                               float* __restrict__ dbias) {
-  __shared__ double sums[16][64];
-  const int c = threadIdx.x & 63, k = threadIdx.x >> 6;
-  const int64_t col = (int64_t)blockIdx.x * 64 + c;
+  __shared__ double sums[32][32];
+  const int c = threadIdx.x & 31, k = threadIdx.x >> 5;
+  const int64_t col = (int64_t)blockIdx.x * 32 + c;
   double s = 0.0;
   if (col < width) {
-#pragma unroll 4
-    for (int64_t b = k; b < blocks; b += 16) s += (double)parts[b * width + col];
+#pragma unroll 8
+    for (int64_t b = k; b < blocks; b += 32) s += (double)parts[b * width + col];
   }
   sums[k][c] = s;
   __syncthreads();
   if (k == 0 && col < width) {
 #pragma unroll
-    for (int i = 1; i < 16; ++i) s += sums[i][c];
+    for (int i = 1; i < 32; ++i) s += sums[i][c];
     if (col < n2)
       dgain[col] = (float)s;
     else
@@ -621,7 +621,7 @@ hipError_t backward(Backward a, float* dgain, float* dbias, float* workspace, hi
   }
   if (c.blocks > 1) {
     const int64_t width = (BIAS ? 4 : 2) * a.n;
-    hipLaunchKernelGGL(layernorm_join_kernel, dim3((unsigned)((width + 63) / 64)), dim3(1024), 0, s, workspace,
+    hipLaunchKernelGGL(layernorm_join_kernel, dim3((unsigned)((width + 31) / 32)), dim3(1024), 0, s, workspace,
                        c.blocks, width, 2 * a.n, dgain, dbias);
   }
   return hipGetLastError();

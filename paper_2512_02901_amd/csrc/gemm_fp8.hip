@@ -163,7 +163,7 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
 #if defined(__HIP_DEVICE_COMPILE__)  // LDS-DMA and buffer-descriptor code: device pass only
   constexpr int WAVES = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   constexpr int PA = BM / 8 / WAVES, PB = BN / 8 / WAVES;  // 1 KB loads of a wave and step
-  constexpr int SCALE_LOADS = (BM + BN) / 64;              // of 64 rows
+  constexpr int SA = (BM + 63) / 64, SB = (BN + 63) / 64, SCALES = 64 * (SA + SB);  // loads of 64 rows' scales
   constexpr int SLOTS = TM * TN, HALF = SLOTS / 2;
   constexpr int STAGE = (BM + BN) * 128;
   // several arrays and not one of several: loads into one never order reads of another
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   __shared__ __attribute__((aligned(16))) uint8_t codes1[STAGE];
   __shared__ __attribute__((aligned(16))) uint8_t codes2[STAGES > 2 ? STAGE : 16];
   __shared__ __attribute__((aligned(16))) uint8_t codes3[STAGES > 2 ? STAGE : 16];
-  __shared__ uint32_t scales[2 * (BM + BN)];
+  __shared__ uint32_t scales[2 * SCALES];
   __shared__ uint32_t asked[AHEAD ? 64 : 1];  // never read
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -219,16 +219,15 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   // Scales of four steps, a dword a row: 64 rows a load.
   auto issue_scales = [&](int k4) {
 #pragma unroll
-    for (int i = 0; i < (SCALE_LOADS + WAVES - 1) / WAVES; ++i) {
+    for (int i = 0; i < (SA + SB + WAVES - 1) / WAVES; ++i) {
       const int p = wave + i * WAVES;
-      const bool of_a = p < BM / 64;
+      const bool of_a = p < SA;
       const int64_t rows = of_a ? g.M : g.N, first = of_a ? m0 : n0;
-      const bool there = p < SCALE_LOADS && 4 * k4 < k1;
       const __amdgpu_buffer_rsrc_t r = rsrc((of_a ? g.a_scales : g.b_scales) + (k4 * rows + first) * 4,
-                                            there ? (uint32_t)min(rows - first, (int64_t)256) * 4u : 0u);
-      if (SCALE_LOADS % WAVES == 0 || p < SCALE_LOADS)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)&scales[(k4 & 1) * (BM + BN) + p * 64], 4,
-                                                 4u * (uint32_t)(64 * (of_a ? p : p - BM / 64) + lane), 0, 0, 0);
+                                            4 * k4 < k1 ? (uint32_t)min(rows - first, (int64_t)256) * 4u : 0u);
+      if ((SA + SB) % WAVES == 0 || p < SA + SB)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)&scales[(k4 & 1) * SCALES + p * 64], 4,
+                                                 4u * (uint32_t)(64 * (of_a ? p : p - SA) + lane), 0, 0, 0);
     }
   };
 
@@ -249,11 +248,11 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
 
   uint32_t sa[TM], sb[TN], sa_next[TM], sb_next[TN];
   auto read_scale = [&](int k4, int i) {
-    const uint32_t* f = &scales[(k4 & 1) * (BM + BN)];
+    const uint32_t* f = &scales[(k4 & 1) * SCALES];
     if (i < TM)
       sa_next[i] = f[row_a + 16 * i + r16];
     else
-      sb_next[i - TM] = f[row_b + 16 * (i - TM) + r16];
+      sb_next[i - TM] = f[64 * SA + wn * TN * 16 + 16 * (i - TM) + r16];
   };
   // Step k, whose first fragments (A's first, B's all) are in registers and whose
   // codes are in `mine`.  First half, rows of tiles 0 .. TM / 2 - 1: reads of the
@@ -281,6 +280,7 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
         });
       } else {
         constexpr int IN = HALF - 1;
+        if constexpr (t == 0 && (U + STAGES) % 4 == 0) issue_scales((k + STAGES) >> 2);
         some<PA + PB, IN, t>([&](auto r) __attribute__((always_inline)) { issue(k + STAGES, decltype(r)::value, mine); });
         if constexpr (t < 2) first[t] = half(other, row_a, t);
         if constexpr (t % R == R - 1) {
@@ -289,7 +289,6 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
         }
         if constexpr (U == 3)
           some<TM + TN, IN, t>([&](auto r) __attribute__((always_inline)) { read_scale((k >> 2) + 1, decltype(r)::value); });
-        if constexpr (U == 0 && s == SLOTS - 2) issue_scales((k >> 2) + 1);
         if constexpr (AHEAD && s == SLOTS - 1) ask(k + AHEAD);
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -302,7 +301,7 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
         __builtin_amdgcn_sched_barrier(0);
       }
     });
-    if (U == 3) {
+    if constexpr (U == 3) {
 #pragma unroll
       for (int i = 0; i < TM; ++i) sa[i] = sa_next[i];
 #pragma unroll
@@ -311,10 +310,11 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   };
 
   // k0 is a multiple of 4
-  issue_scales(k0 >> 2);
   each<STAGES>([&](auto stage) __attribute__((always_inline)) {
+    constexpr int k = decltype(stage)::value;
+    if constexpr (k == 0) issue_scales(k0 >> 2);
 #pragma unroll
-    for (int i = 0; i < PA + PB; ++i) issue(k0 + decltype(stage)::value, i, buffer(stage));
+    for (int i = 0; i < PA + PB; ++i) issue(k0 + k, i, buffer(stage));
   });
 #pragma unroll
   for (int k = STAGES; k < AHEAD; ++k) ask(k0 + k);
@@ -336,15 +336,11 @@ __global__ __launch_bounds__(64 * WM * WN, BLOCKS) void gemm_fp8_kernel(Gemm g) 
   for (int j = 0; j < TN; ++j) sb[j] = sb_next[j];
 
   int k = k0;
-  for (; k + 4 <= k1; k += 4) {
-    step(k, Constant<0>{});
-    step(k + 1, Constant<1>{});
-    step(k + 2, Constant<2>{});
-    step(k + 3, Constant<3>{});
-  }
-  if (k < k1) step(k, Constant<0>{});
-  if (k + 1 < k1) step(k + 1, Constant<1>{});
-  if (k + 2 < k1) step(k + 2, Constant<2>{});
+  for (; k + 4 <= k1; k += 4)
+    each<4>([&](auto u) __attribute__((always_inline)) { step(k + decltype(u)::value, u); });
+  each<3>([&](auto u) __attribute__((always_inline)) {
+    if (k + decltype(u)::value < k1) step(k + decltype(u)::value, u);
+  });
   __builtin_amdgcn_s_waitcnt(0);  // loads into this block's LDS end before it does
   settle(acc);
   __syncthreads();  // every wave has done with LDS
@@ -425,14 +421,17 @@ __global__ __launch_bounds__(256) void gemm_fp8_join_kernel(Gemm g, int splits) 
 // part a step.  `room` blocks run at once; with two a CU each has half of it, so
 // up to 256 blocks a step takes `alone`.
 struct Variant {
-  int bm, bn, room;
+  int bm, bn, threads, room;
   float alone, step, fixed;  // us
   void (*kernel)(Gemm);
 };
 
-// us measured with one bf16 C, all of the variants for each size (the least is what plan_of takes):
-//   M, N, K            256x256  256x128  128x128  128x128x2  64x128  64x64x2
-//   77, 4096, 4096        41.4     28.8     16.5       23.3    11.2      9.1
+// us on the GPU with C in bf16, every variant at some sizes (plan_of takes the least but for a few %):
+//   M, N, K            256x256  256x128  128x128  128x128x2  64x128  64x64x2  64x32x3
+//   1, 4096, 4096         37.9     26.4     14.3       20.9    10.6      9.0      8.1
+//   77, 4096, 4096        41.4     28.8     16.5       23.3    11.2      9.1      8.4
+//   500, 500, 500         16.8     10.6      7.5        7.3     5.1      4.2      4.1
+//   256, 4096, 4096       39.6     26.6     15.4       21.8    11.5      9.4
 //   512, 4096, 4096       39.7     26.6     15.7       22.1    13.1     15.0
 //   1024, 4096, 4096      40.5     27.2     18.7       23.8    23.2     26.9
 //   1400, 4096, 4096      44.6     31.5     32.4       28.9    33.8     37.8
@@ -441,15 +440,17 @@ struct Variant {
 //   4096, 11008, 4096    146.7    183.3    203.4      191.2   263.4    277.0
 //   4096, 4096, 512       16.3     16.8     20.4       16.6    27.4     27.5
 //   1500, 1500, 1500      26.0     19.0     11.4       13.2    12.9     11.0
-// Smaller tiles read LDS more often for a product (256 x 256: 0.75 of its rate, 64 x
-// 64 three times it); more stages hide a longer way to memory where a step is short.
+// A smaller tile moves more bytes a product into LDS (some 43 a clock arrive on a CU,
+// whatever the number of stages) and reads LDS more often; a larger one leaves CUs
+// without work.
 const Variant kVariants[] = {
-    {256, 256, 256, 1.3f, 1.3f, 8.0f, gemm_fp8_kernel<256, 256, 2, 2, 2, 1, 3>},
-    {256, 128, 256, 0.8f, 0.8f, 4.5f, gemm_fp8_kernel<256, 128, 2, 2, 2, 1, 3>},
-    {128, 128, 256, 0.43f, 0.43f, 2.2f, gemm_fp8_kernel<128, 128, 2, 2, 4, 1, 0>},
-    {128, 128, 512, 0.55f, 0.85f, 2.5f, gemm_fp8_kernel<128, 128, 2, 2, 2, 2, 0>},
-    {64, 128, 256, 0.28f, 0.28f, 1.4f, gemm_fp8_kernel<64, 128, 2, 2, 4, 1, 0>},
-    {64, 64, 512, 0.17f, 0.34f, 0.9f, gemm_fp8_kernel<64, 64, 2, 2, 4, 2, 0>},
+    {256, 256, 256, 256, 1.3f, 1.3f, 8.0f, gemm_fp8_kernel<256, 256, 2, 2, 2, 1, 3>},
+    {256, 128, 256, 256, 0.8f, 0.8f, 4.5f, gemm_fp8_kernel<256, 128, 2, 2, 2, 1, 3>},
+    {128, 128, 256, 256, 0.43f, 0.43f, 2.2f, gemm_fp8_kernel<128, 128, 2, 2, 4, 1, 0>},
+    {128, 128, 256, 512, 0.55f, 0.85f, 2.5f, gemm_fp8_kernel<128, 128, 2, 2, 2, 2, 0>},
+    {64, 128, 256, 256, 0.28f, 0.28f, 1.4f, gemm_fp8_kernel<64, 128, 2, 2, 4, 1, 0>},
+    {64, 64, 256, 512, 0.17f, 0.34f, 0.9f, gemm_fp8_kernel<64, 64, 2, 2, 4, 2, 0>},
+    {64, 32, 128, 768, 0.14f, 0.26f, 0.9f, gemm_fp8_kernel<64, 32, 2, 1, 4, 3, 0>},
 };
 
 struct Plan {
@@ -541,7 +542,7 @@ fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_m
                accumulate,
                need > 0 ? static_cast<float*>(workspace) : nullptr};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(p.v->kernel, dim3((unsigned)tiles, (unsigned)p.splits), dim3(256), 0, s, g);
+  hipLaunchKernelGGL(p.v->kernel, dim3((unsigned)tiles, (unsigned)p.splits), dim3(p.v->threads), 0, s, g);
   if (p.splits > 1) {
     const int64_t groups = M * ((N + 3) / 4);
     const unsigned blocks = (unsigned)std::min<int64_t>((groups + 255) / 256, 4096);

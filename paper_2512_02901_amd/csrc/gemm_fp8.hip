@@ -400,6 +400,7 @@ __global__ __launch_bounds__(256) void gemm_fp8_join_kernel(Gemm g, int splits) 
     const int64_t m = i / groups, n = i % groups * 4;
     const int count = (int)min((int64_t)4, g.N - n);
     v4f v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) {
       const float* p = g.parts + ((int64_t)s * g.M + m) * g.N + n;
       if (count == 4) {
@@ -450,7 +451,7 @@ const Variant kVariants[] = {
     {128, 128, 256, 512, 0.55f, 0.85f, 2.5f, gemm_fp8_kernel<128, 128, 2, 2, 2, 2, 0>},
     {64, 128, 256, 256, 0.28f, 0.28f, 1.4f, gemm_fp8_kernel<64, 128, 2, 2, 4, 1, 0>},
     {64, 64, 256, 512, 0.17f, 0.34f, 0.9f, gemm_fp8_kernel<64, 64, 2, 2, 4, 2, 0>},
-    {64, 32, 128, 768, 0.14f, 0.26f, 0.9f, gemm_fp8_kernel<64, 32, 2, 1, 4, 3, 0>},
+    {64, 32, 128, 768, 0.14f, 0.32f, 1.2f, gemm_fp8_kernel<64, 32, 2, 1, 4, 3, 0>},
 };
 
 struct Plan {
@@ -460,8 +461,8 @@ struct Plan {
 };
 
 // The variant, and how many parts K is cut into, with the least expected time: the
-// rounds of blocks, and for a split K the second launch (4 us of a call) and the parts'
-// way to memory and back (8 bytes each at 2.5 TB/s).  16 x 16 x 16384: 25.1 us in
+// rounds of blocks, and for a split K the second launch (4 us of a call), a chain of
+// loads and the parts' way to memory and back (8 bytes each at 2.5 TB/s).  16 x 16 x 16384: 25.1 us in
 // one part, 10.7 in four, 8.7 in eight, 9.6 in sixteen; 300 x 300 x 16384: 26.2,
 // 13.5, 13.4, 16.9.
 Plan plan_of(int64_t M, int64_t N, int64_t K) {
@@ -477,7 +478,7 @@ Plan plan_of(int64_t M, int64_t N, int64_t K) {
       const int run = std::min(p.steps_per_split, steps);
       double us = (double)rounds * (run * v.step + v.fixed);
       if (rest > 0) us += run * (rest > 256 ? v.step : v.alone) + v.fixed;
-      if (p.splits > 1) us += 4.0 + (double)p.splits * (double)M * (double)N * 8e-6 / 2.5;
+      if (p.splits > 1) us += 4.0 + p.splits * (0.35 + (double)M * (double)N * 8e-6 / 2.5);
       if (!best.v || us < least) {
         best = p;
         least = us;

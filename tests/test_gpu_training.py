@@ -272,6 +272,45 @@ def test_gemm_of_small_integers_is_exact(gpu, M, N, K):
     np.testing.assert_array_equal(host(got), want)
 
 
+# sizes that take each of the product's tile sizes (256 x 256 down to 64 x 32), whole and ragged tiles, every number of
+# steps of K left over by groups of four, K in one part and in several
+TILES = [(3000, 4100, 2100), (3584, 3840, 1250), (3584, 3840, 1300), (4096, 3840, 512), (1800, 2600, 6000), (1792, 2560, 6100),
+         (700, 4000, 1000), (1500, 4000, 1000), (1536, 3968, 1152), (704, 1800, 2000), (704, 1792, 2200), (700, 1000, 1100),
+         (130, 70, 9000), (3, 30, 8000), (100, 1000, 9000), (20, 20, 16300), (4100, 37, 1000), (61, 5000, 130)]
+
+
+@pytest.mark.parametrize("M, N, K", TILES)
+def test_gemm_of_every_tile_size_is_exact(gpu, M, N, K):
+    """As above, against the product in 64 bits on the GPU; the workspace holds NaN before."""
+    import torch
+    import paper_2512_02901_amd as f2
+    g = torch.Generator(device=gpu)
+    g.manual_seed(M * 31 + N * 7 + K)
+    code = torch.tensor([0x00, 0x38, 0x40, 0x44, 0xB8, 0xC0, 0xC4], dtype=torch.uint8, device=gpu)
+    value = torch.tensor([0.0, 1, 2, 3, -1, -2, -3], dtype=torch.float64, device=gpu)
+
+    def one(rows):
+        cp, ng = -(-K // 128) * 128, -(-K // 512)
+        pick = torch.randint(0, 7, (rows, K), generator=g, device=gpu)
+        codes = torch.zeros((rows, cp), dtype=torch.uint8, device=gpu)
+        codes[:, :K] = code[pick]
+        e = torch.randint(126, 129, (ng, rows, 4), generator=g, device=gpu, dtype=torch.uint8)
+        unit = torch.exp2(e.double() - 127).transpose(0, 1).reshape(rows, -1).repeat_interleave(128, 1)[:, :K]
+        e[-1, :, (-(-K // 128) - 1) % 4 + 1:] = 255  # bytes of blocks that are not there
+        return f2.Fp8Matrix(rows, K, codes.view(torch.float8_e4m3fn), e), value[pick] * unit
+
+    (A, a), (B, b) = one(M), one(N)
+    want = a @ b.t().contiguous()
+    need = f2.load().fairy2i_gemm_fp8_workspace_bytes(M, N, K)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device=gpu) if need else None
+    assert torch.equal(f2.gemm_fp8(A, B, dtype=torch.float32, workspace=ws).double(), want)
+    assert torch.equal(f2.gemm_fp8(A, B, workspace=ws), want.to(torch.bfloat16))
+    out = torch.full((M, N + 3), 5.0, device=gpu)
+    f2.gemm_fp8(A, B, out=out[:, 1:N + 1], accumulate=True, workspace=ws)
+    assert torch.equal(out[:, 1:N + 1].double(), want + 5)
+    assert (out[:, 0] == 5).all() and (out[:, N + 1:] == 5).all()
+
+
 def test_gemm_scales_far_apart(gpu):
     import torch
     import paper_2512_02901_amd as f2
@@ -293,6 +332,62 @@ def test_gemm_ignores_scale_bytes_past_the_columns(gpu):
     m = fp8(gpu, codes, scales, 200)
     v = tr.dequantize(codes, scales, 200)
     gemm_check(f2.gemm_fp8(m, m, dtype=torch.float32), v, v, "float32")
+
+
+def test_offsets_past_32_bits(gpu):
+    """Codes, turned codes and inputs of more than 2^31 elements: the last rows and columns are where they should be."""
+    import torch
+    import paper_2512_02901_amd as f2
+    rows, cols = 70001, 32768
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device=gpu)
+    last = dev(reals(3, cols, 14), gpu).bfloat16()
+    x[-3:] = last
+    a, b = f2.quantize_fp8(x, transposed="both")
+    del x
+    v = host(last).astype(np.float64)
+    want = tr.quantize(v)
+    np.testing.assert_array_equal(host(a.codes.view(torch.uint8)[-3:]), want[0])
+    np.testing.assert_array_equal(host(a.scales[:, -3:]), want[1])
+    assert (host(a.codes.view(torch.uint8)[:1000]) == 0).all()
+    near = np.zeros((cols, rows - rows // 128 * 128))  # the last block of turned columns
+    near[:, -3:] = v.T
+    codes, scales = tr.quantize(near)
+    np.testing.assert_array_equal(host(b.codes.view(torch.uint8)[-5:, rows // 128 * 128:]), codes[-5:])
+    nb = rows // 128
+    np.testing.assert_array_equal(host(b.scales[nb // 4, :, nb % 4]), scales[0, :, 0])
+    t = a.transpose()
+    np.testing.assert_array_equal(host(t.dequantize()[-5:, -3:]), tr.dequantize(*want, cols)[:, -5:].T)
+    del t
+    w, wv = operand(gpu, 5, cols, 15)
+    c = f2.gemm_fp8(a, w, dtype=torch.float32)
+    gemm_check(c[-3:], tr.dequantize(*want, cols), wv, "float32")
+    assert (c[:-3] == 0).all()
+    c = f2.gemm_fp8(w, a)
+    gemm_check(c[:, -3:], wv, tr.dequantize(*want, cols), "bfloat16")
+    w, wv = operand(gpu, 3, rows, 16)
+    c = f2.gemm_fp8(b, w, dtype=torch.float32)
+    gemm_check(c[-5:], host(b.dequantize()[-5:]).astype(np.float64), wv, "float32")
+
+
+def test_norm_offsets_past_32_bits(gpu):
+    import torch
+    import paper_2512_02901_amd as f2
+    B, n = 300007, 2000  # 4.8 GB of tokens
+    x = torch.zeros((B, n), dtype=torch.complex64, device=gpu)
+    last, _, gain, bias = norm_inputs(3, n, 23)
+    x[-3:] = dev(last, gpu)
+    for fp8 in (False, True):
+        h, z, s = f2.add_layernorm(x, dev(gain, gpu), bias=dev(bias, gpu), fp8=fp8)
+        want_h, want, _ = tr.layernorm(last, None, gain, bias)
+        v = host((z.dequantize().view(B, n, 2) if fp8 else z)[-3:])
+        tol = 2.0 ** -3 if fp8 else 2.0 ** -7  # which rows they are is what counts here
+        np.testing.assert_allclose(v, want, atol=tol * np.abs(want).max())
+        del z, v
+    dz = torch.zeros((B, n, 2), dtype=torch.bfloat16, device=gpu)
+    dz[-3:] = dev(norm_inputs(3, n, 24)[0].view(np.float32).reshape(3, n, 2), gpu).bfloat16()
+    got = f2.layernorm_backward(dz, x, s, dev(gain, gpu))
+    backward_check((got[0][-3:], got[1], got[2]), host(dz[-3:]), last, host(s[-3:]), gain, None, True)
+    assert (torch.view_as_real(got[0][:-3]) == 0).all()
 
 
 # -------------------------------------------------------------------- norm

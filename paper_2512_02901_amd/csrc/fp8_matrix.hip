@@ -26,17 +26,14 @@ struct Source {
   int64_t ld;             // elements of a row
 };
 
-// Eight neighbours of row r from column c on; zeros outside.  WHOLE: none are outside.
+// Eight neighbours of row r from column c on; zeros outside.  WHOLE: the columns
+// are all there.  What is outside is asked for at the last row or column.
 template <int SRC, bool WHOLE>
 __device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_t r, int64_t c, float v[8]) {
-  if constexpr (!WHOLE) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-    if (r >= rows) return;
-  }
+  const int64_t at = min(r, rows - 1) * s.ld;
   if constexpr (SRC == kFp8) {  // rows are padded with zeros to whole blocks
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.x) + r * s.ld + c);
-    const float unit = fp8_power(s.scales[fp8_scale_at(rows, r, c / kFp8Block)]);
+    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.x) + at + c);
+    const float unit = fp8_power(s.scales[fp8_scale_at(rows, min(r, rows - 1), c / kFp8Block)]);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint32_t word = h ? w.y : w.x;
@@ -48,9 +45,9 @@ __device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_
       v[4 * h + 3] = hi[1];
     }
   } else if constexpr (SRC == kF32) {
-    const float* p = static_cast<const float*>(s.x) + r * s.ld + c;
-    if (WHOLE || c + 8 <= cols) {
-      const f32x4_any a = reinterpret_cast<const f32x4_any*>(p)[0], b = reinterpret_cast<const f32x4_any*>(p)[1];
+    const float* p = static_cast<const float*>(s.x) + at;
+    if constexpr (WHOLE) {
+      const f32x4_any a = reinterpret_cast<const f32x4_any*>(p + c)[0], b = reinterpret_cast<const f32x4_any*>(p + c)[1];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         v[j] = a[j];
@@ -58,13 +55,12 @@ __device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c + j < cols) v[j] = p[j];
+      for (int j = 0; j < 8; ++j) v[j] = p[min(c + j, cols - 1)];
     }
   } else {
-    const uint16_t* p = static_cast<const uint16_t*>(s.x) + r * s.ld + c;
-    if (WHOLE || c + 8 <= cols) {
-      const u32x4_any a = *reinterpret_cast<const u32x4_any*>(p);
+    const uint16_t* p = static_cast<const uint16_t*>(s.x) + at;
+    if constexpr (WHOLE) {
+      const u32x4_any a = *reinterpret_cast<const u32x4_any*>(p + c);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         v[2 * j] = bf16_lo(a[j]);
@@ -72,10 +68,11 @@ __device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (c + j < cols) v[j] = __uint_as_float((uint32_t)p[j] << 16);
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float((uint32_t)p[min(c + j, cols - 1)] << 16);
     }
   }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = r < rows && (WHOLE || c + j < cols) ? v[j] : 0.0f;
 }
 
 template <int SRC, bool DIRECT, bool TURNED>
@@ -89,7 +86,7 @@ __global__ __launch_bounds__(256, 3) void fp8_quantize_kernel(Source src, int64_
   const int64_t rb = blockIdx.x / (uint32_t)col_tiles, cb = blockIdx.x % (uint32_t)col_tiles;
   const int64_t r0 = rb * 128 + 8 * rg, c0 = cb * 128 + 8 * cg;
   float v[8][8];
-  if (rb * 128 + 128 <= rows && cb * 128 + 128 <= cols) {
+  if (SRC == kFp8 || cb * 128 + 128 <= cols) {
 #pragma unroll
     for (int p = 0; p < 8; ++p) load8<SRC, true>(src, rows, cols, r0 + p, c0, v[p]);
   } else {
@@ -97,16 +94,17 @@ __global__ __launch_bounds__(256, 3) void fp8_quantize_kernel(Source src, int64_
     for (int p = 0; p < 8; ++p) load8<SRC, false>(src, rows, cols, r0 + p, c0, v[p]);
   }
 
-  uint32_t row[8], col[8], all = 0;  // largest magnitudes of this thread's rows and columns
+  uint32_t row[8] = {}, col[8] = {}, all = 0;  // largest magnitudes of this thread's rows and columns
 #pragma unroll
-  for (int p = 0; p < 8; ++p) {
-    row[p] = col[p] = 0;
+  for (int p = 0; p < 8; ++p)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) row[p] = max(row[p], __float_as_uint(v[p][j]) & 0x7FFFFFFFu);
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t a = __float_as_uint(v[p][j]) & 0x7FFFFFFFu;
+      if constexpr (DIRECT) row[p] = max(row[p], a);
+      if constexpr (TURNED) col[j] = max(col[j], a);
+    }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) col[p] = max(col[p], __float_as_uint(v[j][p]) & 0x7FFFFFFFu);
-    all = max(all, row[p]);
-  }
+  for (int p = 0; p < 8; ++p) all = max(all, DIRECT ? row[p] : col[p]);
   if (__any(all > kFp8Most)) {
 #pragma unroll
     for (int p = 0; p < 8; ++p) row[p] = col[p] = 0;

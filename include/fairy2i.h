@@ -950,7 +950,7 @@ fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_m
  * (as in fairy2i_add_rmsnorm_i8); bias may be NULL.  One of z (bf16 pairs
  * [B][n][2]) and z8 (B x 2n, as fairy2i_fp8_quantize would write z) is given.
  * stats: float32 [B][2] = (mu, r), what the backward pass takes.  Both sums are
- * taken in double, the rest is float32.  x, delta, gain, bias, h, z and stats
+ * taken in double; z8 is formed in double and rounded once, z in float32.  x, delta, gain, bias, h, z and stats
  * may begin at any of their elements.
  * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for B < 1 or above 2^31 - 1, n < 1
  * or above 2^24 (with z8: the matrix's own limits), a matrix of other sizes, eps

@@ -10,6 +10,14 @@
 // rows and four waves.  The turned codes go through 16 KB of LDS (8-byte slots
 // exchanged by column so that neither side conflicts) and leave as whole
 // 128-byte rows.
+//
+// Bound by memory: bf16 of 11008 x 4096 in, both forms out, is 182 MB in 39.5
+// us, 4.6 TB/s of the 5.06 that a large copy reaches, at a third of the VALU's
+// issue.  The 149 registers of a thread allow three waves a SIMD; held to 128
+// (four waves) it spills: 65 us.  Read once a form instead, 4096 x 4096 takes
+// 9.8 + 11.4 us where both at once take 14.8.  What the last columns cost: 5.1
+// -> 6.3 us at 1003 x 1378 of bf16 against 1003 x 1376 (a multiple of 8
+// columns costs nothing more).
 #include <algorithm>
 
 #include "fp8.h"
@@ -26,14 +34,12 @@ struct Source {
   int64_t ld;             // elements of a row
 };
 
-// Eight neighbours of row r from column c on; zeros outside.  WHOLE: the columns
-// are all there.  What is outside is asked for at the last row or column.
-template <int SRC, bool WHOLE>
-__device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_t r, int64_t c, float v[8]) {
-  const int64_t at = min(r, rows - 1) * s.ld;
+// Eight neighbours of row r from column c on.
+template <int SRC>
+__device__ inline void load8_at(const Source& s, int64_t rows, int64_t r, int64_t c, float v[8]) {
   if constexpr (SRC == kFp8) {  // rows are padded with zeros to whole blocks
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.x) + at + c);
-    const float unit = fp8_power(s.scales[fp8_scale_at(rows, min(r, rows - 1), c / kFp8Block)]);
+    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(s.x) + r * s.ld + c);
+    const float unit = fp8_power(s.scales[fp8_scale_at(rows, r, c / kFp8Block)]);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint32_t word = h ? w.y : w.x;
@@ -45,34 +51,63 @@ __device__ inline void load8(const Source& s, int64_t rows, int64_t cols, int64_
       v[4 * h + 3] = hi[1];
     }
   } else if constexpr (SRC == kF32) {
-    const float* p = static_cast<const float*>(s.x) + at;
-    if constexpr (WHOLE) {
-      const f32x4_any a = reinterpret_cast<const f32x4_any*>(p + c)[0], b = reinterpret_cast<const f32x4_any*>(p + c)[1];
+    const f32x4_any* p = reinterpret_cast<const f32x4_any*>(static_cast<const float*>(s.x) + r * s.ld + c);
+    const f32x4_any a = p[0], b = p[1];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = a[j];
-        v[4 + j] = b[j];
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = p[min(c + j, cols - 1)];
+    for (int j = 0; j < 4; ++j) {
+      v[j] = a[j];
+      v[4 + j] = b[j];
     }
   } else {
-    const uint16_t* p = static_cast<const uint16_t*>(s.x) + at;
-    if constexpr (WHOLE) {
-      const u32x4_any a = *reinterpret_cast<const u32x4_any*>(p + c);
+    const u32x4_any a = *reinterpret_cast<const u32x4_any*>(static_cast<const uint16_t*>(s.x) + r * s.ld + c);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[2 * j] = bf16_lo(a[j]);
-        v[2 * j + 1] = bf16_hi(a[j]);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float((uint32_t)p[min(c + j, cols - 1)] << 16);
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = bf16_lo(a[j]);
+      v[2 * j + 1] = bf16_hi(a[j]);
     }
   }
+}
+
+// One element's bits, bf16's in the low half.
+template <int SRC>
+__device__ inline uint32_t load1_at(const Source& s, int64_t r, int64_t c) {
+  if constexpr (SRC == kF32) return static_cast<const uint32_t*>(s.x)[r * s.ld + c];
+  return static_cast<const uint16_t*>(s.x)[r * s.ld + c];
+}
+
+// Eight rows of eight from (r, c) on, zeros outside; rows and columns outside are
+// asked for at the last ones.
+template <int SRC>
+__device__ inline void load64(const Source& s, int64_t rows, int64_t cols, int64_t r, int64_t c, float v[8][8]) {
+  const int there = (int)min(rows - r, (int64_t)8), left = (int)min(cols - c, (int64_t)8);  // below 1: none
+  if (SRC == kFp8 || cols >= 8) {
+    const int64_t first = SRC == kFp8 ? c : min(c, cols - 8);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = r < rows && (WHOLE || c + j < cols) ? v[j] : 0.0f;
+    for (int p = 0; p < 8; ++p) {
+      load8_at<SRC>(s, rows, min(r + p, rows - 1), first, v[p]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[p][j] = p < there && (SRC == kFp8 || left > 0) ? v[p][j] : 0.0f;
+    }
+  }
+  if constexpr (SRC != kFp8) {
+    // the lanes whose group the matrix ends in, value by value: 64 loads on the way at once
+    if (cols < 8 || (left > 0 && left < 8)) {
+      uint32_t w[8][8];
+#pragma unroll
+      for (int p = 0; p < 8; ++p)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[p][j] = load1_at<SRC>(s, min(r + p, rows - 1), min(c + j, cols - 1));
+#pragma unroll
+      for (int p = 0; p < 8; ++p)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          // else the compiler loads bf16 into upper halves, each after a wait for the load before it: 9.3 us
+          // instead of 6.3 at 1003 x 1378
+          asm volatile("" : "+v"(w[p][j]));
+          v[p][j] = p < there && j < left ? __uint_as_float(SRC == kF32 ? w[p][j] : w[p][j] << 16) : 0.0f;
+        }
+    }
+  }
 }
 
 template <int SRC, bool DIRECT, bool TURNED>
@@ -86,13 +121,7 @@ __global__ __launch_bounds__(256, 3) void fp8_quantize_kernel(Source src, int64_
   const int64_t rb = blockIdx.x / (uint32_t)col_tiles, cb = blockIdx.x % (uint32_t)col_tiles;
   const int64_t r0 = rb * 128 + 8 * rg, c0 = cb * 128 + 8 * cg;
   float v[8][8];
-  if (SRC == kFp8 || cb * 128 + 128 <= cols) {
-#pragma unroll
-    for (int p = 0; p < 8; ++p) load8<SRC, true>(src, rows, cols, r0 + p, c0, v[p]);
-  } else {
-#pragma unroll
-    for (int p = 0; p < 8; ++p) load8<SRC, false>(src, rows, cols, r0 + p, c0, v[p]);
-  }
+  load64<SRC>(src, rows, cols, r0, c0, v);
 
   uint32_t row[8] = {}, col[8] = {}, all = 0;  // largest magnitudes of this thread's rows and columns
 #pragma unroll
@@ -215,7 +244,7 @@ __global__ __launch_bounds__(256) void fp8_dequantize_kernel(Source src, int64_t
     const int64_t r = i / groups, c = i % groups * 8;
     if (c >= cols) continue;
     float v[8];
-    load8<kFp8, true>(src, rows, cols, r, c, v);
+    load8_at<kFp8>(src, rows, r, c, v);
     uint16_t* p = out + r * cols + c;
     if (c + 8 <= cols) {
       *reinterpret_cast<u32x4_any*>(p) =

@@ -16,8 +16,8 @@
 // Both are bound by memory; a copy of 1 GiB reaches 5.06 TB/s.  4096 tokens of 2048
 // entries: forward with delta and h into an 8-bit matrix 45.4 us (219 MB, 4.8 TB/s),
 // backward with dh, dbias and dz in bf16 45.6 us (235 MB, 5.15 TB/s) and 5.0 for the
-// join of 512 blocks' parts.  One token takes 3.2 us, five tokens' gradients 3.5 and
-// 2.6: a launch, a chain of loads and two sums over a block.
+// join of 512 blocks' parts.  One token takes 3.2 us: a
+// launch, a chain of loads and two sums over a block.
 #include <float.h>
 
 #include <algorithm>
@@ -575,6 +575,11 @@ __global__ __launch_bounds__(1024) void layernorm_join_kernel(const float* __res
   }
 }
 
+// Up to this many tokens a team one block does them all, without a join: us of one
+// block / a block for each step, 2 tokens of 2048 4.6 / 5.9, 5 of 512 4.5 / 5.7, 2 of
+// 4096 6.5 / 7.2; with three tokens a team 5.6 / 5.8, 6.0 / 5.8 and 8.4 / 7.2.
+constexpr int64_t kOneBlock = 2;
+
 // How the tokens are cut over blocks.
 struct Cut {
   int64_t blocks, rows_per_block;
@@ -592,7 +597,7 @@ Cut cut_of(int64_t B, int64_t n) {
     // tokens of 2048 54.7 / 51.5, 4096 of 1024 30.8 / 26.9, 4096 of 512 15.2 / 14.9;
     // 1024 of 2048 16.6 / 17.5, 2048 of 512 11.3 / 11.9.
     const int64_t teams = teams_of(n), steps = (B + teams - 1) / teams;
-    const int64_t most = n <= 2048 && steps > 1024 ? 512 : 256;
+    const int64_t most = steps <= kOneBlock ? 1 : n <= 2048 && steps > 1024 ? 512 : 256;
     const int64_t rows = (steps + most - 1) / most * teams;
     return {(B + rows - 1) / rows, rows};
   }

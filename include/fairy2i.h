@@ -898,7 +898,7 @@ size_t fairy2i_fp8_scales_bytes(int64_t rows, int64_t cols);
  * which is asked for.
  * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for sizes out of range or that
  * disagree, ld < cols; FAIRY2I_ERR_DTYPE; FAIRY2I_ERR_UNSUPPORTED for misaligned
- * codes or scales, or 2^24 or more tiles of 128 x 128.
+ * codes or scales, matrices that overlap, or 2^24 or more tiles of 128 x 128.
  */
 fairy2i_status fairy2i_fp8_quantize(const void* x, int32_t dtype, int64_t ld, const fairy2i_fp8_matrix* direct,
                                     const fairy2i_fp8_matrix* turned, void* stream);
@@ -950,8 +950,8 @@ fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_m
  * (as in fairy2i_add_rmsnorm_i8); bias may be NULL.  One of z (bf16 pairs
  * [B][n][2]) and z8 (B x 2n, as fairy2i_fp8_quantize would write z) is given.
  * stats: float32 [B][2] = (mu, r), what the backward pass takes.  Both sums are
- * taken in double; z8 is formed in double and rounded once, z in float32.  x, delta, gain, bias, h, z and stats
- * may begin at any of their elements.
+ * taken in double; z8 is formed in double and rounded once, z in float32.  x,
+ * delta, gain, bias, h, z and stats may begin at any of their elements.
  * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for B < 1 or above 2^31 - 1, n < 1
  * or above 2^24 (with z8: the matrix's own limits), a matrix of other sizes, eps
  * not positive and finite, center not 0 or 1; FAIRY2I_ERR_UNSUPPORTED for both of

@@ -1360,18 +1360,16 @@ def quantize_fp8(x, transposed=False, out=None):
         load()
     if transposed not in (False, True, "both"):
         raise ValueError('transposed must be False, True or "both"')
-    if transposed == "both":
-        a, b = (None, None) if out is None else out
-    else:
-        a = b = out
+    both = transposed == "both"
+    a, b = out if both and out is not None else (out, out)
     direct = turned = None
-    if transposed is not True:
+    if both or not transposed:
         direct = _fp8_out(a, rows, cols, x.device, "out")
-    if transposed is not False:
+    if transposed:
         turned = _fp8_out(b, cols, rows, x.device, "out")
     _call("fairy2i_fp8_quantize", x.get_device(), x.data_ptr(), dt, ld, None if direct is None else direct._ref,
           None if turned is None else turned._ref)
-    if transposed == "both":
+    if both:
         return direct, turned
     return turned if transposed else direct
 
@@ -1406,6 +1404,8 @@ def gemm_fp8(A, B, out=None, dtype=None, accumulate=False, workspace=None):
             raise ValueError(f"out is on {out.device}, expected {A.device}")
         if dtype is not None and out.dtype is not dtype:
             raise TypeError(f"out must be {dtype}, got {out.dtype}")
+        if out.is_neg():
+            raise ValueError("out is a negated view")
         if out.shape != (M, N) or (N > 1 and out.stride(1) != 1):
             raise ValueError(f"out must have shape ({M}, {N}), each row contiguous")
         ldc = out.stride(0) if M > 1 else N

@@ -2,6 +2,8 @@
 // codes with one power of two for 128 neighbours of a row.
 #pragma once
 
+#include <initializer_list>
+
 #include "common.h"
 
 namespace fairy2i {
@@ -25,6 +27,25 @@ inline fairy2i_status fp8_check(const fairy2i_fp8_matrix* m) {
   if ((reinterpret_cast<uintptr_t>(m->codes) & 15) || (reinterpret_cast<uintptr_t>(m->scales) & 3))
     return FAIRY2I_ERR_UNSUPPORTED;
   return FAIRY2I_OK;
+}
+
+// Whether two matrices share memory.
+inline bool fp8_overlap(const fairy2i_fp8_matrix* a, const fairy2i_fp8_matrix* b) {
+  struct Range {
+    uintptr_t first, last;
+  };
+  auto codes = [](const fairy2i_fp8_matrix* m) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(m->codes);
+    return Range{p, p + (uintptr_t)(m->rows * fp8_ld(m->cols))};
+  };
+  auto scales = [](const fairy2i_fp8_matrix* m) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(m->scales);
+    return Range{p, p + (uintptr_t)((m->cols + 511) / 512 * m->rows * 4)};
+  };
+  for (const Range& x : {codes(a), scales(a)})
+    for (const Range& y : {codes(b), scales(b)})
+      if (x.first < y.last && y.first < x.last) return true;
+  return false;
 }
 
 // Byte of block `kb` of row r in the scales of a matrix of `rows` rows.

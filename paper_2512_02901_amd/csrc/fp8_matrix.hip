@@ -15,9 +15,9 @@
 // us, 4.6 TB/s of the 5.06 that a large copy reaches, at a third of the VALU's
 // issue.  The 149 registers of a thread allow three waves a SIMD; held to 128
 // (four waves) it spills: 65 us.  Turning an 8-bit matrix fits in 128 but for one
-// register: 4096 x 4096 9.6 us, with three waves 10.5.  Read once a form instead, 4096 x 4096 takes
-// 9.8 + 11.4 us where both at once take 14.8.  What the last columns cost: 5.1
-// -> 6.3 us at 1003 x 1378 of bf16 against 1003 x 1376 (a multiple of 8
+// register: 4096 x 4096 9.6 us, with three waves 10.5.  Read once a form instead,
+// 4096 x 4096 takes 9.8 + 11.4 us where both at once take 14.8.  What the last
+// columns cost: 1003 x 1376 of bf16 5.1 us, 1003 x 1378 6.1 (a multiple of 8
 // columns costs nothing more).
 #include <algorithm>
 
@@ -103,7 +103,7 @@ __device__ inline void load64(const Source& s, int64_t rows, int64_t cols, int64
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           // else the compiler loads bf16 into upper halves, each after a wait for the load before it: 9.3 us
-          // instead of 6.3 at 1003 x 1378
+          // instead of 6.1 at 1003 x 1378
           asm volatile("" : "+v"(w[p][j]));
           v[p][j] = p < there && j < left ? __uint_as_float(SRC == kF32 ? w[p][j] : w[p][j] << 16) : 0.0f;
         }

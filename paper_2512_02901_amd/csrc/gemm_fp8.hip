@@ -12,7 +12,7 @@
 // arrange, so neither side of LDS meets a bank conflict.  Scales come four
 // steps at a time, a dword a row.
 //
-// 4096 x 4096 over 11008: 122-127 us, 2.9-3.0 PFLOP/s (a library product of codes
+// 4096 x 4096 over 11008: 122-132 us on different cards, 2.8-3.0 PFLOP/s (a library product of codes
 // without scales: 114-118); 8192^3: 363 us, 3.0 PFLOP/s (341).  The matrix cores are
 // busy for 70 and 76 % of the cycles, at the 1.9-1.96 GHz that the card holds under
 // them; no LDS conflicts.  What is left are the barrier of each step and the codes'

@@ -474,7 +474,8 @@ __global__ __launch_bounds__(512) void layernorm_backward_kernel(Backward a) {
 }
 
 // Tokens too long for registers: a token's two means first, then the entries,
-// a thread one entry of a run of tokens.
+// a thread one entry of a run of tokens.  The run is as long as the grid makes it
+// (all tokens from 2^19 entries on), so a thread's sums are in double.
 template <bool BF16>
 __global__ __launch_bounds__(512) void layernorm_backward_means_kernel(Backward a) {
   __shared__ float2 slots[8];
@@ -515,7 +516,7 @@ __global__ __launch_bounds__(256) void layernorm_backward_long_kernel(Backward a
   if (j >= a.n) return;
   const int64_t first = blockIdx.y * a.rows_per_block, last = min(first + a.rows_per_block, a.B);
   const float gr = a.gain[j], gi = a.gain[a.n + j];
-  float sgr = 0.0f, sgi = 0.0f, sbr = 0.0f, sbi = 0.0f;
+  double sgr = 0.0, sgi = 0.0, sbr = 0.0, sbi = 0.0;
   for (int64_t row = first; row < last; ++row) {
     const int64_t e = row * a.n + j;
     const float mu = a.stats[2 * row], r = a.stats[2 * row + 1], m1 = a.coef[2 * row], m2 = a.coef[2 * row + 1];
@@ -531,10 +532,10 @@ __global__ __launch_bounds__(256) void layernorm_backward_long_kernel(Backward a
       di = w[1];
     }
     const float yr = (h[0] - mu) * r, yi = (h[1] - mu) * r;
-    sgr += dr * yr;
-    sgi += di * yi;
-    sbr += dr;
-    sbi += di;
+    sgr += (double)dr * (double)yr;
+    sgi += (double)di * (double)yi;
+    sbr += (double)dr;
+    sbi += (double)di;
     f32x2_any d = {0.0f, 0.0f};
     if (a.dh) d = *reinterpret_cast<const f32x2_any*>(a.dh + 2 * e);
     d[0] += ((dr * gr - m1) - yr * m2) * r;
@@ -542,12 +543,12 @@ __global__ __launch_bounds__(256) void layernorm_backward_long_kernel(Backward a
     *reinterpret_cast<f32x2_any*>(a.dx + 2 * e) = d;
   }
   float* part = a.parts + blockIdx.y * (BIAS ? 4 : 2) * a.n;
-  part[j] = sgr;
-  part[a.n + j] = sgi;
+  part[j] = (float)sgr;
+  part[a.n + j] = (float)sgi;
   if constexpr (BIAS) {
     float* part_b = gridDim.y == 1 ? a.dbias : part + 2 * a.n;
-    part_b[j] = sbr;
-    part_b[a.n + j] = sbi;
+    part_b[j] = (float)sbr;
+    part_b[a.n + j] = (float)sbi;
   }
 }
 

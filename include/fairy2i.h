@@ -970,9 +970,10 @@ fairy2i_status fairy2i_add_layernorm(const float* x, const float* delta, const f
  * the forward pass left them; dh: complex64 [B][n], the gradient that reaches h by
  * the residual, or NULL; dx: complex64 [B][n] output (dL/dRe + i dL/dIm), may be
  * dh or h; dgain, dbias: float32 [2n] outputs, dbias may be NULL.  dx is also the
- * gradient of the forward pass's x and of its delta.  The sums over a block's
- * tokens are float32 for n up to 8192 and double above, blocks' are joined in
- * double in a fixed order: repeated calls give the same bits.
+ * gradient of the forward pass's x and of its delta.  For n up to 8192 tokens are
+ * summed in float32 64 at a time (up to eight such sums are added in float32),
+ * above in double; the rest is joined in double in a fixed order: repeated calls
+ * give the same bits.
  * workspace: fairy2i_layernorm_backward_workspace_bytes(B, n) bytes (none where
  * that is 0), 4-byte aligned, contents ignored; calls that share one must not
  * overlap.

@@ -581,6 +581,13 @@ __global__ __launch_bounds__(1024) void layernorm_join_kernel(const float* __res
 // 4096 6.5 / 7.2; with three tokens a team 5.6 / 5.8, 6.0 / 5.8 and 8.4 / 7.2.
 constexpr int64_t kOneBlock = 2;
 
+// A team adds up to this many tokens in float32; what is above is the join's, in
+// double, so an error does not grow with the tokens.  us with 256 or 512 blocks for
+// any number of tokens / with 64 a team: 65536 of 2048 725 / 722, 65536 of 4096 1596 /
+// 1506, 262144 of 300 455 / 458, 524288 of 130 497 / 504.
+constexpr int64_t kMostSteps = 64;
+constexpr int64_t kMostBlocks = 1 << 22;  // a launch takes fewer than 2^32 threads
+
 // How the tokens are cut over blocks.
 struct Cut {
   int64_t blocks, rows_per_block;
@@ -598,7 +605,8 @@ Cut cut_of(int64_t B, int64_t n) {
     // tokens of 2048 54.7 / 51.5, 4096 of 1024 30.8 / 26.9, 4096 of 512 15.2 / 14.9;
     // 1024 of 2048 16.6 / 17.5, 2048 of 512 11.3 / 11.9.
     const int64_t teams = teams_of(n), steps = (B + teams - 1) / teams;
-    const int64_t most = steps <= kOneBlock ? 1 : n <= 2048 && steps > 1024 ? 512 : 256;
+    int64_t most = steps <= kOneBlock ? 1 : n <= 2048 && steps > 1024 ? 512 : 256;
+    most = std::max(most, std::min((steps + kMostSteps - 1) / kMostSteps, kMostBlocks));
     const int64_t rows = (steps + most - 1) / most * teams;
     return {(B + rows - 1) / rows, rows};
   }

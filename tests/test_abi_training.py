@@ -129,3 +129,15 @@ def test_layernorm_backward_validation(lib):
         assert f(B=B, n=n, ws=None) == ERR_WORKSPACE
         assert f(B=B, n=n, ws=ctypes.c_void_p(0x1002)) == ERR_WORKSPACE
     assert lib.fairy2i_layernorm_backward_workspace_bytes(0, 8) == lib.fairy2i_layernorm_backward_workspace_bytes(8, 0) == 0
+
+
+def test_layernorm_backward_workspace_follows_the_tokens(lib):
+    """16 bytes an entry for each block; a block's teams take 64 tokens at most; a launch keeps below 2^32 threads."""
+    for n, teams in ((1, 8), (16, 8), (256, 8), (300, 4), (700, 2), (1500, 1), (3000, 1), (8192, 1)):
+        for B in (100, 1000, 1 << 14, 1 << 16, 100003, 1 << 20, 1 << 22):
+            need = lib.fairy2i_layernorm_backward_workspace_bytes(B, n)
+            assert need % (16 * n) == 0
+            blocks = max(1, need // (16 * n))
+            assert B <= blocks * teams * 64, (B, n)
+            assert blocks <= B
+        assert lib.fairy2i_layernorm_backward_workspace_bytes((1 << 31) - 1, n) // (16 * n) <= 1 << 22

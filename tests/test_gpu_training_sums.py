@@ -1,8 +1,10 @@
 """The gradient of the training norm (layernorm_backward) where its sums are long.
 Tolerances, from the arithmetic (u = 2^-24, half a step of float32):
 
-sums over   of more than 8192 entries: double, one rounding of a block's part and
-tokens      one of the result, 2 u of the sum of |dz y|.
+sums over   of up to 8192 entries: float32 over at most 64 tokens of a team, 7
+tokens      additions to join a block's teams, then double and one rounding: 72 u
+            of the sum of |dz y|; of more entries: double, one rounding of a
+            block's part and one of the result, 2 u.
 """
 import numpy as np
 import pytest
@@ -38,3 +40,13 @@ def test_sums_over_many_long_tokens(gpu, B, n, bf16):
     *got, want = sums_of_one_and_many_small(gpu, B, n, 1, bf16)
     for g in got:
         assert np.abs(g - want).max() <= 2 * u * want
+
+
+@pytest.mark.parametrize("B, n, teams", [(1 << 20, 16, 8), (1 << 19, 300, 4), (1 << 18, 700, 2), (1 << 17, 1500, 1), (1 << 16, 3000, 1),
+                                         (1 << 16, 5000, 1)])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_sums_over_many_short_tokens(gpu, B, n, teams, bf16):
+    """256 tokens for each team of 256 or 512 blocks; a team adds 64 at most.  Every term is exact."""
+    *got, want = sums_of_one_and_many_small(gpu, B, n, teams, bf16)
+    for g in got:
+        assert np.abs(g - want).max() <= (64 + 7 + 1) * u * want

@@ -970,7 +970,9 @@ fairy2i_status fairy2i_add_layernorm(const float* x, const float* delta, const f
  * the forward pass left them; dh: complex64 [B][n], the gradient that reaches h by
  * the residual, or NULL; dx: complex64 [B][n] output (dL/dRe + i dL/dIm), may be
  * dh or h; dgain, dbias: float32 [2n] outputs, dbias may be NULL.  dx is also the
- * gradient of the forward pass's x and of its delta.  For n up to 8192 tokens are
+ * gradient of the forward pass's x and of its delta.  mu's rounding to float32
+ * moves y by up to 2^-24 |mu| r; with center = 1 and |mu| r above 64 the token's
+ * mean of y, 0 but for that, is taken off y.  For n up to 8192 tokens are
  * summed in float32 64 at a time (up to eight such sums are added in float32),
  * above in double; the rest is joined in double in a fixed order: repeated calls
  * give the same bits.

@@ -328,7 +328,7 @@ struct Backward {
   float* dx;
   float* parts;  // [blocks][dgain 2n, dbias 2n where wanted]; the outputs themselves where one block does all
   float* dbias;  // with one block
-  float* coef;   // tokens too long for registers: [B][2]
+  float* coef;   // tokens too long for registers: [B][3], the two means and what is taken off y
   int64_t rows_per_block;
 };
 
@@ -360,11 +360,17 @@ __device__ inline float wave_sum(float v) {
   return v;
 }
 
+// The forward pass takes its mean off in double, stats hold it in float32: y is
+// off by up to 2^-24 |mu| r, the same for the whole token.  Where that is above
+// 2^-18 the mean of y, which ought to be 0, is taken off y.
+constexpr float kFarMean = 64.0f;  // |mu| r
+
 // NT threads take a token, 512 / NT tokens a block at a time.
 template <int NT, int GROUPS, bool BF16, bool BIAS>
 __global__ __launch_bounds__(512) void layernorm_backward_kernel(Backward a) {
   constexpr int TEAMS = 512 / NT, WAVES = NT / 64;
   __shared__ float2 slots[2][8];
+  __shared__ float offsets[2][8];
   __shared__ float others[TEAMS > 1 ? (TEAMS - 1) * NT * GROUPS * 8 * (BIAS ? 2 : 1) : 1];
   const int team = threadIdx.x / NT, t = threadIdx.x % NT;
   const float over = 1.0f / (float)(2 * a.n);
@@ -390,7 +396,8 @@ __global__ __launch_bounds__(512) void layernorm_backward_kernel(Backward a) {
       mu = a.stats[2 * row];
       r = a.stats[2 * row + 1];
     }
-    float s1 = 0.0f, s2 = 0.0f;
+    const bool far = a.center && fabsf(mu) * r > kFarMean;  // the whole team
+    float s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
       const int64_t e = row * a.n + 4 * (int64_t)(t + i * NT);
@@ -412,8 +419,19 @@ __global__ __launch_bounds__(512) void layernorm_backward_kernel(Backward a) {
       }
     s1 = wave_sum(s1);
     s2 = wave_sum(s2);
+    if (far) {
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < 2 * count[i]) s3 += y[i].v[j];
+      s3 = wave_sum(s3);
+    }
     if constexpr (WAVES > 1) {
-      if ((threadIdx.x & 63) == 0) slots[parity][threadIdx.x >> 6] = make_float2(s1, s2);
+      if ((threadIdx.x & 63) == 0) {
+        slots[parity][threadIdx.x >> 6] = make_float2(s1, s2);
+        offsets[parity][threadIdx.x >> 6] = s3;
+      }
       __syncthreads();  // the other parity's slots are free: they were read before the last barrier
       s1 = s2 = 0.0f;
 #pragma unroll
@@ -423,7 +441,24 @@ __global__ __launch_bounds__(512) void layernorm_backward_kernel(Backward a) {
         s2 += v.y;
       }
     }
-    const float m1 = a.center ? s1 * over : 0.0f, m2 = s2 * over;
+    const float m1 = a.center ? s1 * over : 0.0f;
+    float m2 = s2 * over;
+    if (far) {
+      if constexpr (WAVES > 1) {
+        s3 = 0.0f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) s3 += offsets[parity][team * WAVES + w];
+      }
+      const float off = s3 * over;
+      m2 -= m1 * off;
+#pragma unroll
+      for (int i = 0; i < GROUPS; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sum_g[i].v[j] -= dz[i].v[j] * off;
+          y[i].v[j] -= off;
+        }
+    }
     if (there) {
 #pragma unroll
       for (int i = 0; i < GROUPS; ++i) {
@@ -473,40 +508,50 @@ __global__ __launch_bounds__(512) void layernorm_backward_kernel(Backward a) {
   }
 }
 
-// Tokens too long for registers: a token's two means first, then the entries,
+// Tokens too long for registers: a token's means first, then the entries,
 // a thread one entry of a run of tokens.  The run is as long as the grid makes it
 // (all tokens from 2^19 entries on), so a thread's sums are in double.
 template <bool BF16>
 __global__ __launch_bounds__(512) void layernorm_backward_means_kernel(Backward a) {
-  __shared__ float2 slots[8];
+  __shared__ float slots[3][8];
   const int64_t row = blockIdx.x;
   const float mu = a.stats[2 * row], r = a.stats[2 * row + 1];
-  double s1 = 0.0, s2 = 0.0;
+  double s1 = 0.0, s2 = 0.0, s3 = 0.0;
   for (int64_t g = threadIdx.x; 4 * g < a.n; g += 512) {
     const int count = count_of(a.n, g);
     const Group h = load_group(a.h + 2 * (row * a.n + 4 * g), count);
     const Group dz = load_dz<BF16>(a.dz, row * a.n + 4 * g, count), gain = load_gain(a.gain, a.n, 4 * g, count);
-    float p1 = 0.0f, p2 = 0.0f;
+    float p1 = 0.0f, p2 = 0.0f, p3 = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float w = dz.v[j] * gain.v[j];
+      const float w = dz.v[j] * gain.v[j], y = (h.v[j] - mu) * r;
       p1 += w;
-      p2 += w * ((h.v[j] - mu) * r);
+      p2 += w * y;
+      p3 += j < 2 * count ? y : 0.0f;
     }
     s1 += (double)p1;
     s2 += (double)p2;
+    s3 += (double)p3;
   }
-  const float f1 = wave_sum((float)s1), f2 = wave_sum((float)s2);
-  if ((threadIdx.x & 63) == 0) slots[threadIdx.x >> 6] = make_float2(f1, f2);
+  const float f1 = wave_sum((float)s1), f2 = wave_sum((float)s2), f3 = wave_sum((float)s3);
+  if ((threadIdx.x & 63) == 0) {
+    slots[0][threadIdx.x >> 6] = f1;
+    slots[1][threadIdx.x >> 6] = f2;
+    slots[2][threadIdx.x >> 6] = f3;
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
-    double m1 = 0.0, m2 = 0.0;
-    for (int w = 0; w < 8; ++w) {
-      m1 += (double)slots[w].x;
-      m2 += (double)slots[w].y;
+    double m[3] = {};
+    for (int i = 0; i < 3; ++i) {
+      for (int w = 0; w < 8; ++w) m[i] += (double)slots[i][w];
+      m[i] /= (double)(2 * a.n);
     }
-    a.coef[2 * row] = a.center ? (float)(m1 / (double)(2 * a.n)) : 0.0f;
-    a.coef[2 * row + 1] = (float)(m2 / (double)(2 * a.n));
+    if (!a.center) m[0] = 0.0;
+    const bool far = a.center && fabsf(mu) * r > kFarMean;
+    if (far) m[1] -= m[0] * m[2];
+    a.coef[3 * row] = (float)m[0];
+    a.coef[3 * row + 1] = (float)m[1];
+    a.coef[3 * row + 2] = far ? (float)m[2] : 0.0f;
   }
 }
 
@@ -519,7 +564,8 @@ __global__ __launch_bounds__(256) void layernorm_backward_long_kernel(Backward a
   double sgr = 0.0, sgi = 0.0, sbr = 0.0, sbi = 0.0;
   for (int64_t row = first; row < last; ++row) {
     const int64_t e = row * a.n + j;
-    const float mu = a.stats[2 * row], r = a.stats[2 * row + 1], m1 = a.coef[2 * row], m2 = a.coef[2 * row + 1];
+    const float mu = a.stats[2 * row], r = a.stats[2 * row + 1];
+    const float m1 = a.coef[3 * row], m2 = a.coef[3 * row + 1], off = a.coef[3 * row + 2];
     const f32x2_any h = *reinterpret_cast<const f32x2_any*>(a.h + 2 * e);
     float dr, di;
     if constexpr (BF16) {
@@ -531,7 +577,7 @@ __global__ __launch_bounds__(256) void layernorm_backward_long_kernel(Backward a
       dr = w[0];
       di = w[1];
     }
-    const float yr = (h[0] - mu) * r, yi = (h[1] - mu) * r;
+    const float yr = (h[0] - mu) * r - off, yi = (h[1] - mu) * r - off;
     sgr += (double)dr * (double)yr;
     sgi += (double)di * (double)yi;
     sbr += (double)dr;
@@ -655,7 +701,7 @@ hipError_t backward(Backward a, float* dgain, float* dbias, float* workspace, hi
       p.dz = static_cast<const char*>(a.dz) + 2 * b * a.n * (BF16 ? 2 : 4);
       p.h += 2 * b * a.n;
       p.stats += 2 * b;
-      p.coef += 2 * b;
+      p.coef += 3 * b;
       hipLaunchKernelGGL((layernorm_backward_means_kernel<BF16>), dim3((unsigned)p.B), dim3(512), 0, s, p);
     }
     hipLaunchKernelGGL((layernorm_backward_long_kernel<BF16, BIAS>),
@@ -713,7 +759,7 @@ fairy2i_status fairy2i_add_layernorm(const float* x, const float* delta, const f
 
 size_t fairy2i_layernorm_backward_workspace_bytes(int64_t B, int64_t n) {
   if (!sizes_ok(B, n)) return 0;
-  return sizeof(float) * (size_t)(parts_floats(B, n) + (n > kMostInRegisters ? 2 * B : 0));
+  return sizeof(float) * (size_t)(parts_floats(B, n) + (n > kMostInRegisters ? 3 * B : 0));
 }
 
 fairy2i_status fairy2i_layernorm_backward(const void* dz, int32_t dtype, const float* h, const float* stats,

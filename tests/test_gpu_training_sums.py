@@ -1,15 +1,22 @@
-"""The gradient of the training norm (layernorm_backward) where its sums are long.
+"""The gradient of the training norm (layernorm_backward) where its sums are long
+or its tokens far from zero, against oracle/training.py in 64 bits.
 Tolerances, from the arithmetic (u = 2^-24, half a step of float32):
 
 sums over   of up to 8192 entries: float32 over at most 64 tokens of a team, 7
 tokens      additions to join a block's teams, then double and one rounding: 72 u
             of the sum of |dz y|; of more entries: double, one rounding of a
             block's part and one of the result, 2 u.
+far tokens  (|mu| r above 64) y: the difference from the float32 mean is exact or
+            rounded once, r and the factor are two more: 3 u |y|, |y| before the
+            token's mean of it is taken off; that mean: at most 32 additions of a
+            thread, 14 over threads and waves, the factor 1 / 2n and y's own: 50 u
+            of the mean of |y|.  Others keep what the mean's rounding moves y by.
 """
 import numpy as np
 import pytest
 
-from test_gpu_training import host
+from oracle import training as tr
+from test_gpu_training import dev, grad_inputs, host
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +57,60 @@ def test_sums_over_many_short_tokens(gpu, B, n, teams, bf16):
     *got, want = sums_of_one_and_many_small(gpu, B, n, teams, bf16)
     for g in got:
         assert np.abs(g - want).max() <= (64 + 7 + 1) * u * want
+
+
+# ------------------------------------------------------- means far from zero
+
+
+def mean_check(got, dz, h, stats, gain, dh):
+    """stats: the means in 64 bits (the kernel was given them in 32), factors that are float32 numbers."""
+    B, n = h.shape
+    dx, dgain, dbias = tr.layernorm_backward(dz, h, stats, gain, dh, True)
+    mu, r = (stats[:, i, None, None] for i in (0, 1))
+    y = np.abs((np.stack([h.real, h.imag], -1).astype(np.float64) - mu) * r)
+    D = np.abs(mu.astype(np.float32) - mu) * r       # what the mean's rounding moves y by
+    far = np.abs(mu) * r > 63.99
+    yf = y + D                                       # bounds y as it is before its mean is taken off
+    # tokens near zero keep D; in the others y: subtraction, factor, the mean's (3 and 50 roundings)
+    E = np.where(far, 3 * u * yf + 50 * u * yf.mean((1, 2), keepdims=True), D + 2 * u * y)
+    w = np.abs(dz.astype(np.float64) * np.asarray(gain, np.float64).reshape(2, n).T)
+    m1, m2 = w.mean((1, 2), keepdims=True), (w * yf).mean((1, 2), keepdims=True)
+    d = np.abs(np.stack([dh.real, dh.imag], -1)).astype(np.float64)
+    # the float32 arithmetic's, as of any token, and what y's error makes of y mean(w y)
+    tol = u * (2 * d + np.abs(r) * (8 * w + 100 * m1 + 200 * yf * m2))
+    tol = tol + np.abs(r) * (E * m2 + yf * (w * E).mean((1, 2), keepdims=True))
+    e = host(got[0]).astype(np.complex128) - dx
+    err = np.abs(np.stack([e.real, e.imag], -1))
+    assert (err <= tol).all(), (err / tol).max()
+    a = np.abs(dz).astype(np.float64)
+    # dz y is added and dz mean(y) taken off: two additions a token
+    ga = ((a * E).sum(0) + (2 * 72 + 3) * u * (a * yf).sum(0)).T.reshape(-1)
+    err = np.abs(host(got[1]) - dgain)
+    assert (err <= ga).all(), (err / ga).max()
+    assert (np.abs(host(got[2]) - dbias) <= 72 * u * a.sum(0).T.reshape(-1)).all()
+
+
+@pytest.mark.parametrize("B, n", [(6, 33), (50, 130), (21, 300), (700, 300), (9, 700), (5, 1500), (4, 3000), (3, 6000), (7, 9001)])
+@pytest.mark.parametrize("bf16", [True, False])
+def test_backward_of_tokens_far_from_zero(gpu, B, n, bf16):
+    """A mean above its spread by up to 10^6, tokens near zero between them: the mean in float32 is off by up to a
+    tenth of the spread."""
+    import torch
+    import paper_2512_02901_amd as f2
+    rng = np.random.default_rng((37, B, n))
+    x, _, gain, dh, dz = grad_inputs(B, n, 37, True, bf16)
+    part = np.stack([x.real, x.imag], -1)
+    offset = np.array([1e4, 0, -1e3, 64, 3e5])[np.arange(B) % 5]
+    spread = np.array([1e-2, 1, 0.1, 0.9, 1])[np.arange(B) % 5]
+    part = (part * spread[:, None, None] + offset[:, None, None] + 1e-3 * rng.standard_normal((B, 1, 1))).astype(np.float32)
+    x = part[..., 0] + 1j * part[..., 1]
+    assert x.dtype == np.complex64
+    _, _, stats = tr.layernorm(x, None, gain, None, 1e-5, True)
+    stats[:, 1] = stats[:, 1].astype(np.float32)
+    h, d = dev(x, gpu), dev(dh, gpu)
+    dzd = dz.to(gpu) if bf16 else torch.view_as_complex(dz.to(gpu))
+    args = dzd, h, dev(stats.astype(np.float32), gpu), dev(gain, gpu)
+    got = f2.layernorm_backward(*args, dh=d)
+    mean_check(got, host(dz), x, stats, gain, dh)
+    again = f2.layernorm_backward(*args, dh=d, out=h)
+    assert all(torch.equal(p, q) for p, q in zip(got, again))

@@ -156,9 +156,9 @@ __device__ inline void write_z(const Forward& a, int64_t row, int64_t g, int cou
   Group z = Group{};
   if (a.bias) z = load_gain(a.bias, a.n, 4 * g, count);
   if (a.z) {
-    const float r = (float)m.r;
+    // h - mean may be beyond the largest float32, and r below its normal numbers
 #pragma unroll
-    for (int j = 0; j < 8; ++j) z.v[j] += (float)((double)h.v[j] - m.mean) * r * gain.v[j];
+    for (int j = 0; j < 8; ++j) z.v[j] += (float)(((double)h.v[j] - m.mean) * m.r) * gain.v[j];
     uint16_t* p = a.z + 2 * (row * a.n + 4 * g);
     if (count >= 4) {
       *reinterpret_cast<u32x4_any*>(p) = u32x4_any{bf16_pair(z.v[0], z.v[1]), bf16_pair(z.v[2], z.v[3]),
@@ -365,6 +365,9 @@ __device__ inline float wave_sum(float v) {
 // 2^-18 the mean of y, which ought to be 0, is taken off y.
 constexpr float kFarMean = 64.0f;  // |mu| r
 
+// (h - mu) r by way of halves: the difference may be beyond the largest float32.
+__device__ inline float scaled(float h, float half_mu, float twice_r) { return fmaf(h, 0.5f, -half_mu) * twice_r; }
+
 // NT threads take a token, 512 / NT tokens a block at a time.
 template <int NT, int GROUPS, bool BF16, bool BIAS>
 __global__ __launch_bounds__(512) void layernorm_backward_kernel(Backward a) {
@@ -409,7 +412,7 @@ __global__ __launch_bounds__(512) void layernorm_backward_kernel(Backward a) {
     for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float v = (y[i].v[j] - mu) * r;
+        const float v = scaled(y[i].v[j], 0.5f * mu, 2.0f * r);
         y[i].v[j] = v;
         sum_g[i].v[j] += dz[i].v[j] * v;
         if constexpr (BIAS) sum_b[i].v[j] += dz[i].v[j];
@@ -524,7 +527,7 @@ __global__ __launch_bounds__(512) void layernorm_backward_means_kernel(Backward 
     float p1 = 0.0f, p2 = 0.0f, p3 = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float w = dz.v[j] * gain.v[j], y = (h.v[j] - mu) * r;
+      const float w = dz.v[j] * gain.v[j], y = scaled(h.v[j], 0.5f * mu, 2.0f * r);
       p1 += w;
       p2 += w * y;
       p3 += j < 2 * count ? y : 0.0f;
@@ -577,7 +580,7 @@ __global__ __launch_bounds__(256) void layernorm_backward_long_kernel(Backward a
       dr = w[0];
       di = w[1];
     }
-    const float yr = (h[0] - mu) * r - off, yi = (h[1] - mu) * r - off;
+    const float yr = scaled(h[0], 0.5f * mu, 2.0f * r) - off, yi = scaled(h[1], 0.5f * mu, 2.0f * r) - off;
     sgr += (double)dr * (double)yr;
     sgi += (double)di * (double)yi;
     sbr += (double)dr;

@@ -1,5 +1,6 @@
 """The gradient of the training norm (layernorm_backward) where its sums are long
-or its tokens far from zero, against oracle/training.py in 64 bits.
+or its tokens far from zero, and the norm near float32's largest numbers, against
+oracle/training.py in 64 bits.
 Tolerances, from the arithmetic (u = 2^-24, half a step of float32):
 
 sums over   of up to 8192 entries: float32 over at most 64 tokens of a team, 7
@@ -114,3 +115,70 @@ def test_backward_of_tokens_far_from_zero(gpu, B, n, bf16):
     mean_check(got, host(dz), x, stats, gain, dh)
     again = f2.layernorm_backward(*args, dh=d, out=h)
     assert all(torch.equal(p, q) for p, q in zip(got, again))
+
+
+# ---------------------------------------------- entries near the largest float32
+
+
+def large_tokens(n):
+    rng = np.random.default_rng((38, n))
+    part = (2e38 * rng.standard_normal((6, n, 2))).clip(-3.3e38, 3.3e38).astype(np.float32)
+    part[1:3] = 3.3e38
+    part[1, 0, 0] = part[2, n - 1, 1] = -3.3e38  # 6.6e38 below the others' mean
+    part[3] *= np.float32(2.0 ** -10)
+    part[4] = np.float32(3e38) + part[4] * np.float32(2.0 ** -8)
+    x = (part[..., 0] + 1j * part[..., 1]).astype(np.complex64)
+    gain = (1 + 0.1 * rng.standard_normal(2 * n)).astype(np.float32)
+    return x, gain, rng.standard_normal(2 * n).astype(np.float32)
+
+
+@pytest.mark.parametrize("n", [64, 1000, 3000, 5001, 9001])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_norm_of_entries_near_the_largest(gpu, n, fp8):
+    """Differences from the mean that are no float32, factors that are no normal one.  z: within 8 u (|t| + |bias|) and
+    half a step of bf16, or of e4m3 as in the other tests of the norm."""
+    import paper_2512_02901_amd as f2
+    x, gain, bias = large_tokens(n)
+    h, z, s = f2.add_layernorm(dev(x, gpu), dev(gain, gpu), bias=dev(bias, gpu), fp8=fp8)
+    _, want, _ = tr.layernorm(x, None, gain, bias)
+    b = np.abs(bias).astype(np.float64).reshape(2, n).T
+    tol = 8 * u * (np.abs(want - bias.astype(np.float64).reshape(2, n).T) + b)
+    v = (host(z.dequantize()).reshape(want.shape) if fp8 else host(z)).astype(np.float64)
+    if fp8:
+        unit = 2.0 ** (host(z.scales).transpose(1, 0, 2).reshape(len(want), -1).astype(np.float64) - 127)
+        unit = np.repeat(unit, 128, 1)[:, :2 * n].reshape(want.shape)
+        tol = tol + np.maximum(2.0 ** -4 * (np.abs(want) + tol), 2.0 ** -10 * unit)
+    else:
+        tol = tol + 2.0 ** -8 * (np.abs(want) + tol)
+    assert (np.abs(v - want) <= tol).all()
+
+
+@pytest.mark.parametrize("n", [64, 300, 700, 1000, 3000, 5001, 9001])
+def test_backward_of_entries_near_the_largest(gpu, n):
+    """Gradients of gain and bias; dx is r ~ 10^-38 times ordinary numbers, to half a step of 2^-149 more a rounding.
+    One entry of 18002 below the others is 67 spreads from zero, so there the mean is the one in 64 bits (far tokens
+    above): 50 u of the mean of |y|, y with what the mean's rounding moves it by."""
+    import torch
+    import paper_2512_02901_amd as f2
+    x, gain, _ = large_tokens(n)
+    _, _, stats = tr.layernorm(x, None, gain, None)
+    s32 = stats.astype(np.float32)
+    keep = np.arange(6) != 4  # 2^8 spreads from zero: the mean's rounding counts there
+    x, s32, stats = x[keep], s32[keep], stats[keep].astype(np.float64)
+    far = np.abs(stats[:, 0]) * stats[:, 1] > 64
+    assert far.any() == (n == 9001)
+    rounded = np.abs(s32[:, 0] - stats[:, 0]) * s32[:, 1]
+    held = np.stack([np.where(far, stats[:, 0], s32[:, 0].astype(np.float64)), s32[:, 1].astype(np.float64)], 1)
+    dz = np.random.default_rng((39, n)).standard_normal((5, n, 2)).astype(np.float32)
+    got = f2.layernorm_backward(torch.view_as_complex(dev(dz, gpu)), dev(x, gpu), dev(s32, gpu), dev(gain, gpu))
+    dx, dgain, dbias = tr.layernorm_backward(dz, x, held, gain)
+    y = np.abs((np.stack([x.real, x.imag], -1).astype(np.float64) - held[:, 0, None, None]) * held[:, 1, None, None])
+    w = np.abs(dz * gain.reshape(2, n).T).astype(np.float64)
+    m1, m2 = w.mean((1, 2), keepdims=True), (w * y).mean((1, 2), keepdims=True)
+    e = host(got[0]).astype(np.complex128) - dx
+    err = np.abs(np.stack([e.real, e.imag], -1))
+    assert (err <= u * s32[:, 1, None, None].astype(np.float64) * (8 * w + 100 * m1 + 100 * y * m2) + 2.0 ** -149).all()
+    E = np.where(far, 50 * u * (y.mean((1, 2)) + rounded), 0)[:, None, None]
+    ga, ba = (np.abs(dz) * (y + E / (15 * u))).sum(0).T.reshape(-1), np.abs(dz).astype(np.float64).sum(0).T.reshape(-1)
+    assert (np.abs(host(got[1]) - dgain) <= 15 * u * ga).all()
+    assert (np.abs(host(got[2]) - dbias) <= 12 * u * ba).all()

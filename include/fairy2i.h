@@ -895,10 +895,10 @@ size_t fairy2i_fp8_scales_bytes(int64_t rows, int64_t cols);
  * entries are rows of 2n reals.  direct: rows x cols, blocks along the rows of
  * x; turned: cols x rows, the transposed matrix with blocks along the columns of
  * x; either may be NULL.  Both together read x once.  Results do not depend on
- * which is asked for.
+ * which is asked for.  Outputs share no memory with x or each other.
  * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for sizes out of range or that
  * disagree, ld < cols; FAIRY2I_ERR_DTYPE; FAIRY2I_ERR_UNSUPPORTED for misaligned
- * codes or scales, matrices that overlap, or 2^24 or more tiles of 128 x 128.
+ * codes or scales, memory that is shared, or 2^24 or more tiles of 128 x 128.
  */
 fairy2i_status fairy2i_fp8_quantize(const void* x, int32_t dtype, int64_t ld, const fairy2i_fp8_matrix* direct,
                                     const fairy2i_fp8_matrix* turned, void* stream);
@@ -911,7 +911,10 @@ fairy2i_status fairy2i_fp8_quantize(const void* x, int32_t dtype, int64_t ld, co
  */
 fairy2i_status fairy2i_fp8_transpose(const fairy2i_fp8_matrix* in, const fairy2i_fp8_matrix* out, void* stream);
 
-/* out: bf16 [rows][cols], what the matrix stands for, exact.  Errors: as above. */
+/*
+ * out: bf16 [rows][cols], what the matrix stands for, exact; shares no memory with
+ * it.  Errors: as above.
+ */
 fairy2i_status fairy2i_fp8_dequantize(const fairy2i_fp8_matrix* in, void* out, void* stream);
 
 /*
@@ -933,7 +936,7 @@ fairy2i_status fairy2i_fp8_dequantize(const fairy2i_fp8_matrix* in, void* out, v
  * 4-byte aligned, contents ignored; calls that share one must not overlap.
  * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for sizes out of range or that
  * disagree, ldc < N; FAIRY2I_ERR_DTYPE; FAIRY2I_ERR_UNSUPPORTED for misaligned
- * operands or 2^24 or more tiles of C; FAIRY2I_ERR_WORKSPACE.
+ * operands, a C that shares memory with one, or 2^24 or more tiles of C; FAIRY2I_ERR_WORKSPACE.
  */
 size_t fairy2i_gemm_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K);
 fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_matrix* B, void* C, int32_t dtype,

@@ -2,6 +2,7 @@
 // codes with one power of two for 128 neighbours of a row.
 #pragma once
 
+#include <algorithm>
 #include <initializer_list>
 
 #include "common.h"
@@ -20,7 +21,7 @@ typedef uint32_t u32_any __attribute__((aligned(2)));
 
 inline int64_t fp8_ld(int64_t cols) { return (cols + kFp8Block - 1) / kFp8Block * kFp8Block; }
 
-// Sizes, pointers and alignment; `nullable` fields are the caller's to check.
+// Sizes, pointers and alignment.
 inline fairy2i_status fp8_check(const fairy2i_fp8_matrix* m) {
   if (!m || !m->codes || !m->scales) return FAIRY2I_ERR_NULL;
   if (m->rows < 1 || m->cols < 1 || m->rows > kFp8MostSide || m->cols > kFp8MostSide) return FAIRY2I_ERR_SHAPE;
@@ -29,22 +30,39 @@ inline fairy2i_status fp8_check(const fairy2i_fp8_matrix* m) {
   return FAIRY2I_OK;
 }
 
+// Memory of a matrix: codes, scales.
+struct Fp8Range {
+  uint64_t first, last;
+};
+inline Fp8Range fp8_codes_range(const fairy2i_fp8_matrix* m) {
+  const uint64_t p = reinterpret_cast<uintptr_t>(m->codes);
+  return {p, p + (uint64_t)(m->rows * fp8_ld(m->cols))};
+}
+inline Fp8Range fp8_scales_range(const fairy2i_fp8_matrix* m) {
+  const uint64_t p = reinterpret_cast<uintptr_t>(m->scales);
+  return {p, p + (uint64_t)((m->cols + 511) / 512 * m->rows * 4)};
+}
+
 // Whether two matrices share memory.
 inline bool fp8_overlap(const fairy2i_fp8_matrix* a, const fairy2i_fp8_matrix* b) {
-  struct Range {
-    uintptr_t first, last;
-  };
-  auto codes = [](const fairy2i_fp8_matrix* m) {
-    const uintptr_t p = reinterpret_cast<uintptr_t>(m->codes);
-    return Range{p, p + (uintptr_t)(m->rows * fp8_ld(m->cols))};
-  };
-  auto scales = [](const fairy2i_fp8_matrix* m) {
-    const uintptr_t p = reinterpret_cast<uintptr_t>(m->scales);
-    return Range{p, p + (uintptr_t)((m->cols + 511) / 512 * m->rows * 4)};
-  };
-  for (const Range& x : {codes(a), scales(a)})
-    for (const Range& y : {codes(b), scales(b)})
+  for (const Fp8Range& x : {fp8_codes_range(a), fp8_scales_range(a)})
+    for (const Fp8Range& y : {fp8_codes_range(b), fp8_scales_range(b)})
       if (x.first < y.last && y.first < x.last) return true;
+  return false;
+}
+
+// Whether a matrix shares memory with `rows` rows of `width` elements of `size`
+// bytes, ld >= width elements apart: what lies between the rows is others'.
+inline bool fp8_overlap(const fairy2i_fp8_matrix* m, const void* p, int64_t rows, int64_t width, int64_t ld, int size) {
+  const uint64_t base = reinterpret_cast<uintptr_t>(p), bytes = (uint64_t)(width * size);
+  // rows further apart than memory is large: the first is all that could
+  const uint64_t pitch = rows > 1 ? (uint64_t)std::min(ld, (int64_t)1 << 56) * (uint64_t)size : bytes;
+  for (const Fp8Range& x : {fp8_codes_range(m), fp8_scales_range(m)}) {
+    if (x.last <= base) continue;
+    // the first row that ends behind x.first
+    const uint64_t row = x.first < base + bytes ? 0 : (x.first - base - bytes) / pitch + 1;
+    if (row < (uint64_t)rows && base + row * pitch < x.last) return true;
+  }
   return false;
 }
 

@@ -298,6 +298,9 @@ fairy2i_status fairy2i_fp8_quantize(const void* x, int32_t dtype, int64_t ld, co
   if (ld < cols) return FAIRY2I_ERR_SHAPE;
   if (dtype != FAIRY2I_ACT_F32 && dtype != FAIRY2I_ACT_BF16) return FAIRY2I_ERR_DTYPE;
   if (too_many_tiles(rows, cols) || (direct && turned && fp8_overlap(direct, turned))) return FAIRY2I_ERR_UNSUPPORTED;
+  const int size = dtype == FAIRY2I_ACT_F32 ? 4 : 2;
+  for (const fairy2i_fp8_matrix* m : {direct, turned})
+    if (m && fp8_overlap(m, x, rows, cols, ld, size)) return FAIRY2I_ERR_UNSUPPORTED;
   const Source src{x, nullptr, ld};
   hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t e = dtype == FAIRY2I_ACT_F32 ? launch<kF32>(src, rows, cols, direct, turned, s)
@@ -321,6 +324,7 @@ fairy2i_status fairy2i_fp8_dequantize(const fairy2i_fp8_matrix* in, void* out, v
   const fairy2i_status st = fp8_check(in);
   if (st != FAIRY2I_OK) return st;
   if (!out) return FAIRY2I_ERR_NULL;
+  if (fp8_overlap(in, out, 1, in->rows * in->cols, 0, 2)) return FAIRY2I_ERR_UNSUPPORTED;
   const Source src{in->codes, in->scales, fp8_ld(in->cols)};
   const int64_t work = in->rows * (src.ld / 8);
   const unsigned blocks = (unsigned)std::min<int64_t>((work + 255) / 256, 1 << 20);

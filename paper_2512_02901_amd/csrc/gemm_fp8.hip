@@ -536,6 +536,8 @@ fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_m
     return FAIRY2I_ERR_WORKSPACE;
   const int64_t tiles = p.tiles_m * p.tiles_n;
   if (tiles * p.splits >= ((int64_t)1 << 24)) return FAIRY2I_ERR_UNSUPPORTED;  // a launch takes fewer than 2^32 threads
+  for (const fairy2i_fp8_matrix* m : {A, B})  // blocks read operands while others store C
+    if (fp8_overlap(m, C, M, N, ldc, dtype == FAIRY2I_ACT_F32 ? 4 : 2)) return FAIRY2I_ERR_UNSUPPORTED;
   const Gemm g{A->codes,
                A->scales,
                B->codes,

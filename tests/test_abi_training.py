@@ -141,3 +141,36 @@ def test_layernorm_backward_workspace_follows_the_tokens(lib):
             assert B <= blocks * teams * 64, (B, n)
             assert blocks <= B
         assert lib.fairy2i_layernorm_backward_workspace_bytes((1 << 31) - 1, n) // (16 * n) <= 1 << 22
+
+
+def test_outputs_that_overlap_inputs(lib):
+    # 4 x 300: 1536 bytes of codes, 16 of scales; every call is refused
+    def quantize(x, m=mat(codes=0x100000, scales=0x200000), dt=ACT_F32, ld=300):
+        return lib.fairy2i_fp8_quantize(ctypes.c_void_p(x), dt, ld, m, None, None)
+    for x in (0x100000, 0x1005FC, 0x100000 - 4796, 0x200000, 0x20000C, 0x200000 - 4796):
+        assert quantize(x) == ERR_UNSUPPORTED, hex(x)
+        turned = mat(300, 4, 0x100000, 0x200000) if x < 0x200000 else mat(300, 4, 0x180000, 0x200000)
+        assert lib.fairy2i_fp8_quantize(ctypes.c_void_p(x), ACT_F32, 300, None, turned, None) == ERR_UNSUPPORTED, hex(x)
+    # bf16 is half as long; rows far apart meet the matrix with each of them
+    assert quantize(0x100000 - 2398, dt=ACT_BF16) == ERR_UNSUPPORTED
+    for row in range(4):
+        for off in (-1196, 0, 1532):
+            assert quantize(0x100000 + off - row * 4 * 0x1000, ld=0x1000) == ERR_UNSUPPORTED, (row, off)
+    # one row's distance to the next says nothing; rows further apart than memory is large
+    assert quantize(0x100000, m=mat(1, 300, 0x100000, 0x200000), ld=(1 << 63) - 1) == ERR_UNSUPPORTED
+    assert quantize(0x100000, ld=(1 << 62)) == ERR_UNSUPPORTED
+    out = lambda p: lib.fairy2i_fp8_dequantize(mat(codes=0x100000, scales=0x200000), ctypes.c_void_p(p), None)  # noqa: E731
+    for p in (0x100000, 0x1005FE, 0x100000 - 2398, 0x200000 - 2398, 0x20000E):
+        assert out(p) == ERR_UNSUPPORTED, hex(p)
+
+    # C is 4 x 7 beside 4 x 300 and 7 x 300 (2688 bytes of codes, 28 of scales)
+    a, b = mat(4, 300, 0x100000, 0x200000), mat(7, 300, 0x300000, 0x400000)
+
+    def gemm(c, dt=ACT_F32, ldc=7, x=a, y=b):
+        return lib.fairy2i_gemm_fp8(x, y, ctypes.c_void_p(c), dt, ldc, 0, P, 1 << 40, None)
+    for c in (0x100000, 0x1005FC, 0x100000 - 108, 0x20000C, 0x300000 - 108, 0x300A7C, 0x400018, 0x400000 - 108):
+        assert gemm(c) == ERR_UNSUPPORTED, hex(c)
+        assert gemm(c, x=b, y=a, ldc=4) == ERR_UNSUPPORTED, hex(c)
+    assert gemm(0x100000 - 54, dt=ACT_BF16) == ERR_UNSUPPORTED
+    for row in range(4):
+        assert gemm(0x300000 - row * 4 * 0x1000 - 24, ldc=0x1000) == ERR_UNSUPPORTED, row

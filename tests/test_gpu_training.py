@@ -761,3 +761,27 @@ def test_refusals(gpu):
         with pytest.raises(error):
             call()
             print("not refused:", i)
+
+
+def test_matrices_between_the_rows_of_an_input_or_output(gpu):
+    """Rows' distance is no part of them: what lies there may be a matrix of the same call."""
+    import torch
+    import paper_2512_02901_amd as f2
+    wide = dev(reals(3, 1000, 17), gpu)
+    x, v = wide[:, :130], host(wide[:, :130])
+    codes = wide[0, 200:392].view(torch.uint8).view(3, 256).view(torch.float8_e4m3fn)
+    scales = wide[1, 200:203].view(torch.uint8).view(1, 3, 4)
+    m = f2.Fp8Matrix(3, 130, codes, scales)
+    f2.quantize_fp8(x, out=m)
+    same(m, tr.quantize(v))
+    np.testing.assert_array_equal(host(x), v)
+    held = host(m.dequantize()).astype(np.float64)
+    out = wide[:, 500:503]
+    f2.gemm_fp8(m, m, out=out)
+    gemm_check(out, held, held, "float32")
+    same(m, tr.quantize(v))
+    for call in (lambda: f2.quantize_fp8(wide[:, 100:230], out=m), lambda: f2.gemm_fp8(m, m, out=wide[:, 389:392]),
+                 lambda: f2.quantize_fp8(wide[:, 73:203], out=m)):
+        with pytest.raises(f2.Fairy2iError):
+            call()
+    same(m, tr.quantize(v))

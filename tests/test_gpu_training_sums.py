@@ -17,7 +17,7 @@ import numpy as np
 import pytest
 
 from oracle import training as tr
-from test_gpu_training import dev, grad_inputs, host
+from test_gpu_training import backward_check, dev, grad_inputs, host
 
 pytestmark = pytest.mark.gpu
 
@@ -58,6 +58,54 @@ def test_sums_over_many_short_tokens(gpu, B, n, teams, bf16):
     *got, want = sums_of_one_and_many_small(gpu, B, n, teams, bf16)
     for g in got:
         assert np.abs(g - want).max() <= (64 + 7 + 1) * u * want
+
+
+# ------------------------------------------- many tokens a block, all forms
+
+
+# Tokens for three steps and more of each team, a last block with fewer and (where a block takes several tokens at a
+# time) a last step with fewer: eight, four, two teams, one of one, two and four groups of entries; blocks of two a CU;
+# tokens too long for registers, the last in one block.
+MANY = [(6203, 130), (3103, 300), (1603, 700), (3001, 700), (1102, 2000), (2103, 1100), (801, 3001), (801, 6000),
+        (200, 8200), (131, 9001), (5, (1 << 19) + 1)]
+
+
+@pytest.mark.parametrize("B, n", MANY)
+@pytest.mark.parametrize("bf16", [True, False])
+def test_backward_of_many_tokens(gpu, B, n, bf16):
+    import torch
+    import paper_2512_02901_amd as f2
+    center, bias = bf16, (B + bf16) % 2 == 0
+    x, stats, gain, dh, dz = grad_inputs(B, n, 34, center, bf16)
+    dzd = dz.to(gpu) if bf16 else torch.view_as_complex(dz.to(gpu))
+    got = f2.layernorm_backward(dzd, dev(x, gpu), dev(stats, gpu), dev(gain, gpu), dh=dev(dh, gpu), center=center, bias=bias)
+    backward_check(got, host(dz), x, stats, gain, dh, center)
+
+
+@pytest.mark.parametrize("B, n", [(1603, 700), (1102, 2000), (801, 6000), (131, 9001), (5, (1 << 19) + 1)])
+@pytest.mark.parametrize("where", ["dh", "h"])
+def test_backward_of_many_tokens_in_place(gpu, B, n, where):
+    import paper_2512_02901_amd as f2
+    x, stats, gain, dh, dz = grad_inputs(B, n, 35, True, True)
+    h, d = dev(x, gpu), dev(dh, gpu)
+    got = f2.layernorm_backward(dz.to(gpu), h, dev(stats, gpu), dev(gain, gpu), dh=d, out=d if where == "dh" else h)
+    assert got[0] is (d if where == "dh" else h)
+    backward_check(got, host(dz), x, stats, gain, dh, True)
+
+
+@pytest.mark.parametrize("n, bf16, bias", [(130, False, False), (300, True, False), (700, False, True), (2000, True, True),
+                                           (3001, False, False), (6000, True, False), (9001, False, False)])
+def test_backward_of_many_tokens_repeats_its_bits(gpu, n, bf16, bias):
+    import torch
+    import paper_2512_02901_amd as f2
+    B = {130: 6203, 300: 3103, 700: 1603}.get(n, 803)
+    x, stats, gain, dh, dz = grad_inputs(B, n, 36, True, bf16)
+    args = (dz.to(gpu) if bf16 else torch.view_as_complex(dz.to(gpu)), dev(x, gpu), dev(stats, gpu), dev(gain, gpu))
+    got = f2.layernorm_backward(*args, bias=bias)
+    backward_check(got, host(dz), x, stats, gain, None, True)
+    for _ in range(3):
+        again = f2.layernorm_backward(*args, bias=bias)
+        assert all(p is None or torch.equal(p, q) for p, q in zip(got, again))
 
 
 # ------------------------------------------------------- means far from zero

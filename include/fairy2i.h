@@ -927,10 +927,14 @@ fairy2i_status fairy2i_fp8_dequantize(const fairy2i_fp8_matrix* in, void* out, v
  *   G_X = G_Y R     A = G_Y, B = R turned,
  *   G_R = G_Y^T X   A = G_Y turned, B = X turned (from the 8-bit X that the
  *                   forward product took: fairy2i_fp8_transpose).
- * Products are exact.  The matrix cores sum them in float32, neighbouring ones
- * in groups whose terms keep 13 bits below the group's largest: with what the
- * operands hold taken as exact, relative L2 1.5e-5 for N(0, 1) values, up to 8e-5
- * where values of a block differ by e^(N(0, 1)); a C in float32 is no closer.
+ * X, R and gradients in e4m3 are other numbers than those that were quantised: each
+ * is off by up to 2^-4 of itself (2^-10 of its block's power of two where that is
+ * more), so Y is the product with R so rounded, not with the sums of the stages'
+ * scales that a decode product takes.  Products of codes are exact.  The matrix
+ * cores sum them in float32, neighbouring ones in groups whose terms keep 13 bits
+ * below the group's largest: with what the operands hold taken as exact, relative
+ * L2 1.5e-5 for N(0, 1) values, up to 8e-5 where values of a block differ by
+ * e^(N(0, 1)); a C in float32 is no closer.
  * Repeated calls give the same bits.  workspace:
  * fairy2i_gemm_fp8_workspace_bytes(M, N, K) bytes (none where that is 0),
  * 4-byte aligned, contents ignored; calls that share one must not overlap.
@@ -952,9 +956,10 @@ fairy2i_status fairy2i_gemm_fp8(const fairy2i_fp8_matrix* A, const fairy2i_fp8_m
  * gain, bias: float32 [2n], the real parts' values, then the imaginary parts'
  * (as in fairy2i_add_rmsnorm_i8); bias may be NULL.  One of z (bf16 pairs
  * [B][n][2]) and z8 (B x 2n, as fairy2i_fp8_quantize would write z) is given.
- * stats: float32 [B][2] = (mu, r), what the backward pass takes.  Both sums are
- * taken in double; z8 is formed in double and rounded once, z in float32.  x,
- * delta, gain, bias, h, z and stats may begin at any of their elements.
+ * stats: float32 [B][2] = (mu, r), what the backward pass takes.  Outputs share no
+ * memory with inputs or each other but h as said.  Both sums and (h - mu) r are
+ * taken in double, z8 is formed in double and rounded once, the rest of z in
+ * float32.  x, delta, gain, bias, h, z and stats may begin at any of their elements.
  * Errors: FAIRY2I_ERR_NULL; FAIRY2I_ERR_SHAPE for B < 1 or above 2^31 - 1, n < 1
  * or above 2^24 (with z8: the matrix's own limits), a matrix of other sizes, eps
  * not positive and finite, center not 0 or 1; FAIRY2I_ERR_UNSUPPORTED for both of
@@ -972,7 +977,8 @@ fairy2i_status fairy2i_add_layernorm(const float* x, const float* delta, const f
  * dz: pairs [B][n][2] of dtype FAIRY2I_ACT_F32 or FAIRY2I_ACT_BF16; h, stats: as
  * the forward pass left them; dh: complex64 [B][n], the gradient that reaches h by
  * the residual, or NULL; dx: complex64 [B][n] output (dL/dRe + i dL/dIm), may be
- * dh or h; dgain, dbias: float32 [2n] outputs, dbias may be NULL.  dx is also the
+ * dh or h; dgain, dbias: float32 [2n] outputs, dbias may be NULL; beside dx outputs
+ * share no memory with inputs or each other.  dx is also the
  * gradient of the forward pass's x and of its delta.  mu's rounding to float32
  * moves y by up to 2^-24 |mu| r; with center = 1 and |mu| r above 64 the token's
  * mean of y, 0 but for that, is taken off y.  For n up to 8192 tokens are

@@ -8,8 +8,9 @@
 // registers once: a thread holds 8 rows x 8 columns, so a row's maximum is 8
 // values and a DPP row of 16 lanes, a column's 8 values, the wave's four DPP
 // rows and four waves.  The turned codes go through 16 KB of LDS (8-byte slots
-// exchanged by column so that neither side conflicts) and leave as whole
-// 128-byte rows.
+// exchanged by column) and leave as whole 128-byte rows.  A wave writes rows
+// 1024 bytes apart, into one span of 128 bytes of the banks: conflicts are 18 % of
+// the LDS cycles, which are 8 % of the kernel's.
 //
 // Bound by memory: bf16 of 11008 x 4096 in, both forms out, is 182 MB in 39.5
 // us, 4.6 TB/s of the 5.06 that a large copy reaches, at a third of the VALU's

@@ -14,10 +14,15 @@
 // registers, blocks' sums are joined by a second kernel in a fixed order.
 //
 // Both are bound by memory; a copy of 1 GiB reaches 5.06 TB/s.  4096 tokens of 2048
-// entries: forward with delta and h into an 8-bit matrix 45.4 us (219 MB, 4.8 TB/s),
-// backward with dh, dbias and dz in bf16 45.6 us (235 MB, 5.15 TB/s) and 5.0 for the
-// join of 512 blocks' parts.  One token takes 3.2 us: a
-// launch, a chain of loads and two sums over a block.
+// entries, under the profiler: forward with delta and h into an 8-bit matrix 46 us
+// (219 MB, 4.7 TB/s), backward with dh and dz in bf16 46 us (235 MB, 5.1 TB/s) and
+// 5.0 for the join of 512 blocks' parts.  In a loop over inputs that no cache holds
+// a call of the forward takes 43.8 us (into bf16 45.2), of the backward with dbias
+// 56.4 (dz in complex64 64.3).  Past 8192 entries the forward reads a token three
+// times, the backward h and dz twice: 1024 tokens of 16384 entries 122 us forward
+// and 144 backward, where one reading would be 86 and 93 at the copy's rate.  One token takes 3.2 us: a launch, a chain of loads and two sums over a
+// block.  The tables below are of loops over three inputs, which the last cache
+// holds in part.
 #include <float.h>
 
 #include <algorithm>
@@ -133,10 +138,11 @@ struct Forward {
   float* stats;
 };
 
-// For e4m3 z is formed in double and rounded once (43.4 us for 4096 tokens of 2048
-// either way): float32 on the way puts some fifty of 16.8 million values on the
-// other side of a midpoint, relative L2 1e-4 against 2e-8.  bf16's own rounding is
-// 1.7e-3 either way.
+// For e4m3 z is formed in double and rounded once, at no cost in time: of 16.8
+// million values (three seeds) none differs from the definition applied to the h
+// that is stored, where float32 on the way puts 19 to 26 on the other side of a
+// midpoint (relative L2 7e-5 to 3e-4).  Against x + delta before h was rounded 6 to 9
+// differ (1e-5 to 4e-5), with float32 17 to 29.  bf16's own rounding is 1.7e-3.
 struct Moments {
   double mean, r;
 };

@@ -20,9 +20,9 @@
 // a call of the forward takes 43.8 us (into bf16 45.2), of the backward with dbias
 // 56.4 (dz in complex64 64.3).  Past 8192 entries the forward reads a token three
 // times, the backward h and dz twice: 1024 tokens of 16384 entries 122 us forward
-// and 144 backward, where one reading would be 86 and 93 at the copy's rate.  One token takes 3.2 us: a launch, a chain of loads and two sums over a
-// block.  The tables below are of loops over three inputs, which the last cache
-// holds in part.
+// and 144 backward, where one reading would be 86 and 93 at the copy's rate.  One
+// token takes 3.2 us: a launch, a chain of loads and two sums over a block.  The
+// tables below are of loops over three inputs, which the last cache holds in part.
 #include <float.h>
 
 #include <algorithm>
